@@ -1,101 +1,172 @@
-// pp_linear_forward, pp_linear_backward_input, pp_linear_backward_weight: products with a packed
-// operand.
-//
-// One kernel for all: tiles of 64 by 64 results, both operands read back to floats on their way
-// into LDS, 16 results to a thread.
-#include "pp_layer_common.h"
+// pp_linear_forward, pp_linear_backward_input, pp_linear_backward_weight: what is checked, how the
+// work is divided, and the passes around the products of pp_product_fp4.hip and pp_product_grad.hip.
+#include "pp_product_fp4.h"
+#include "pp_product_grad.h"
 
 int pp_launch_pack(int format, int type, int64_t rows, int64_t cols, const void *src, int64_t ld, void *codes, void *scales, hipStream_t st);
 
-// Operand elements by (index along the result, index along the sum).
-struct FromFp4 {
-    const uint8_t *codes, *scales;
-    long long groups;
-    __device__ float at(long long r, long long c) const {
-        const unsigned byte = scales[r * groups * 4 + c / PP_BLOCK];
-        const unsigned n = codes[r * groups * PP_GROUP_CODES4 + c / 2] >> (4 * (c & 1)) & 15;
-        const unsigned e = n >> 1 & 3;
-        const float m = e ? pp_bits((126 + e) << 23 | (n & 1) << 22) : 0.5f * (n & 1);
-        return (n & 8 ? -m : m) * pp_unit4(byte);
-    }
-};
-struct FromInt8 {
-    const uint8_t *codes, *scales;
-    long long groups;
-    __device__ float at(long long r, long long c) const {
-        return (float)((const int8_t *)codes)[r * groups * PP_GROUP + c] * pp_unit8(scales[r * groups * 4 + c / PP_BLOCK]);
-    }
-};
-template <class Y> struct FromMatrix {
-    const typename Y::T *p;
-    long long ld;
-    __device__ float at(long long r, long long c) const { return Y::get(p[r * ld + c]); }
-};
-template <class P> struct Flip {
-    P p;
-    __device__ float at(long long r, long long c) const { return p.at(c, r); }
-};
+// ---- gradients as bf16 planes
 
-template <class Y> struct ToMatrix {
-    typename Y::T *p;
-    long long ld;
-    const float *add;
-    long long add_ld;  // 0: one row for all
-    __device__ void put(long long i, long long j, float v) const { p[i * ld + j] = Y::put(add ? v + add[i * add_ld + j] : v); }
-};
+// dy in a form the product can load as it is: rows at multiples of 16 bytes, in bf16.  A type with
+// more bits becomes two (f16) or three (float) planes that add up to it exactly, each the leading
+// eight bits of what the ones before leave; products with all of them are summed.
+static int planes_of(int type) { return type == PP_TYPE_BF16 ? 1 : type == PP_TYPE_F16 ? 2 : 3; }
 
-template <class A, class B, class C>
-__global__ __launch_bounds__(256) void k_product(long long rows, long long cols, long long len, unsigned gx, A a, B b, C c) {
-    __shared__ float sa[16][65], sb[16][65];
-    const long long i0 = (long long)(blockIdx.x / gx) * 64, j0 = (long long)(blockIdx.x % gx) * 64;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    float acc[4][4] = {};
-    for (long long k0 = 0; k0 < len; k0 += 16) {
-        for (int t = threadIdx.x; t < 1024; t += 256) {
-            const int k = t & 15, i = t >> 4;
-            sa[k][i] = i0 + i < rows && k0 + k < len ? a.at(i0 + i, k0 + k) : 0.0f;
-            sb[k][i] = j0 + i < cols && k0 + k < len ? b.at(j0 + i, k0 + k) : 0.0f;
+template <class Y, int PLANES>
+__global__ __launch_bounds__(256) void k_planes(long long rows, long long cols, const typename Y::T *__restrict__ src, long long ld,
+                                                uint16_t *__restrict__ dst, long long ld_dst) {
+    const long long chunks = ld_dst / 8, n = rows * chunks;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < n; t += (long long)gridDim.x * 256) {
+        const long long r = t / chunks, c = (t - r * chunks) * 8;
+        const PpRaw<Y> raw = pp_load8<Y>(src + r * ld + c, cols - c);
+        float v[8];
+        pp_values<Y>(raw, v);
+#pragma unroll
+        for (int k = 0; k < PLANES; ++k) {
+            unsigned h[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const unsigned b = pp_bits(v[j]);
+                const bool finite = (b & 0x7f800000u) != 0x7f800000u;
+                h[j] = (b >> 16) | ((b & 0x7fffffffu) > 0x7f800000u ? 0x40u : 0u);  // a NaN stays one
+                v[j] = finite ? v[j] - pp_bits(b & 0xffff0000u) : 0.0f;
+            }
+            *(pp_u4 *)(dst + (k * rows + r) * ld_dst + c) = pp_u4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
         }
-        __syncthreads();
-        for (int k = 0; k < 16; ++k)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v) acc[u][v] += sa[k][ty + 16 * u] * sb[k][tx + 16 * v];
-        __syncthreads();
     }
-    for (int u = 0; u < 4; ++u)
-        for (int v = 0; v < 4; ++v)
-            if (i0 + ty + 16 * u < rows && j0 + tx + 16 * v < cols) c.put(i0 + ty + 16 * u, j0 + tx + 16 * v, acc[u][v]);
 }
 
-template <class A, class B, class C>
-static int product(long long rows, long long cols, long long len, const A &a, const B &b, const C &c, hipStream_t st) {
-    const unsigned gx = (unsigned)((cols + 63) / 64), gy = (unsigned)((rows + 63) / 64);
-    k_product<<<gx * gy, 256, 0, st>>>(rows, cols, len, gx, a, b, c);
+static int launch_planes(int type, int64_t rows, int64_t cols, const void *src, int64_t ld, void *dst, int64_t ld_dst, hipStream_t st) {
+    const int64_t blocks = (rows * (ld_dst / 8) + 255) / 256;
+    const unsigned grid = (unsigned)(blocks < 8192 ? blocks : 8192);
+    if (type == PP_TYPE_BF16) k_planes<PpBF16, 1><<<grid, 256, 0, st>>>(rows, cols, (const __bf16 *)src, ld, (uint16_t *)dst, ld_dst);
+    else if (type == PP_TYPE_F16) k_planes<PpF16, 2><<<grid, 256, 0, st>>>(rows, cols, (const _Float16 *)src, ld, (uint16_t *)dst, ld_dst);
+    else k_planes<PpF32, 3><<<grid, 256, 0, st>>>(rows, cols, (const float *)src, ld, (uint16_t *)dst, ld_dst);
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
 }
 
+// ---- pieces of a sum, added in their order
+
 template <class Y>
-__global__ void k_column_sums(long long rows, long long cols, const typename Y::T *__restrict__ p, long long ld, float *__restrict__ out) {
-    const long long c = (long long)blockIdx.x * 64 + (threadIdx.x & 63);
-    __shared__ float part[4][64];
-    float s = 0;
-    if (c < cols)
-        for (long long r = threadIdx.x >> 6; r < rows; r += 4) s += Y::get(p[r * ld + c]);
-    part[threadIdx.x >> 6][threadIdx.x & 63] = s;
-    __syncthreads();
-    if (threadIdx.x < 64 && c < cols) out[c] = part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x];
+__global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const float *__restrict__ part_sums, float *__restrict__ sums) {
+    const long long chunks = p.partial_ld / 8, n = p.outer * chunks;
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < n; t += (long long)gridDim.x * 256) {
+        const long long o = t / chunks, i = (t - o * chunks) * 8;
+        const float *q = p.partial + o * p.partial_ld + i;
+        pp_f4 a = {0, 0, 0, 0}, b = a;
+        for (int s = 0; s < p.splits; ++s, q += p.outer * p.partial_ld) {
+            a += *(const pp_f4 *)q;
+            b += *(const pp_f4 *)(q + 4);
+        }
+        float v[8];
+        *(pp_f4 *)v = a;
+        *(pp_f4 *)(v + 4) = b;
+        pr_plan whole = p;
+        whole.splits = 1;
+        pr_put8<Y>(whole, out, o, i, 0, v);
+    }
+    if (sums)
+        for (long long o = (long long)blockIdx.x * 256 + threadIdx.x; o < p.outer; o += (long long)gridDim.x * 256) {
+            float v = 0;
+            for (int s = 0; s < p.splits; ++s) v += part_sums[s * p.outer + o];
+            sums[o] = v;
+        }
 }
+
+static int launch_join(int type, const pr_plan &p, void *out, long long ld, const float *bias, const float *add, const float *part_sums, float *sums,
+                       hipStream_t st) {
+    const long long blocks = (p.outer * (p.partial_ld / 8) + 255) / 256;
+    return pp_by_type(type, [&](auto t) {
+        typedef decltype(t) Y;
+        k_join<Y><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(p, pr_out<Y>{(typename Y::T *)out, ld, bias, add, ld}, part_sums, sums);
+        return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+    });
+}
+
+// ---- how work is divided
+
+// A tile shape: results, workgroups of it that a compute unit holds, microseconds of a step and of
+// a workgroup's start and end.
+struct pr_shape {
+    int ti, to, fit;
+    float step, once;
+};
+static const pr_shape SHAPES_FP4[] = {{256, 256, 1, 0.9f, 4.0f}, {128, 128, 2, 0.55f, 2.5f}, {256, 32, 2, 0.4f, 2.0f}};
+static const pr_shape SHAPES_GRAD[] = {{256, 256, 1, 1.5f, 4.0f}, {128, 128, 2, 0.9f, 2.5f}, {256, 32, 2, 0.8f, 2.0f}};
+#define PR_CUS 256
+
+// The shape and the number of pieces with the least estimated time: rounds of workgroups over the
+// chip, and for more than one piece the pass that adds them.
+static pr_plan plan(const pr_shape *shapes, int n, long long inner, long long outer, long long steps, int *shape) {
+    pr_plan best = {};
+    float least = 0;
+    for (int k = 0; k < n; ++k) {
+        const pr_shape &s = shapes[k];
+        const long long ni = (inner + s.ti - 1) / s.ti, no = (outer + s.to - 1) / s.to, tiles = ni * no;
+        for (int pieces = 1; pieces <= 32; ++pieces) {
+            const long long per = (steps + pieces - 1) / pieces;
+            if (pieces > 1 && ((steps + per - 1) / per != pieces || tiles > PR_CUS * s.fit)) continue;
+            const float rounds = (float)((tiles * pieces + PR_CUS * s.fit - 1) / (PR_CUS * s.fit));
+            float t = rounds * ((float)per * s.step + s.once);
+            if (pieces > 1) t += 4.0f + (float)(pieces + 1) * (float)(inner * outer) * 4.0f / 3.0e6f;
+            if (!best.splits || t < least) {
+                least = t;
+                *shape = k;
+                best.steps = (int)steps;
+                best.per = (int)per;
+                best.splits = pieces;
+            }
+        }
+    }
+    const pr_shape &s = shapes[*shape];
+    best.inner = inner;
+    best.outer = outer;
+    best.ni = (unsigned)((inner + s.ti - 1) / s.ti);
+    best.no = (unsigned)((outer + s.to - 1) / s.to);
+    best.partial_ld = (inner + 7) & ~7ll;
+    return best;
+}
+static size_t partial_bytes(const pr_plan &p) { return p.splits > 1 ? (size_t)p.splits * p.outer * p.partial_ld * 4 : 0; }
+
+// Runs launch(part, first outer index) over the outer index in launches of at most 2^20 tiles.
+template <class F> static int in_turns(const pr_plan &p, int to, F launch) {
+    const long long most = ((1ll << 20) / p.ni < 1 ? 1 : (1ll << 20) / p.ni) * to;
+    for (long long o = 0; o < p.outer; o += most) {
+        pr_plan q = p;
+        q.outer = p.outer - o < most ? p.outer - o : most;
+        q.no = (unsigned)((q.outer + to - 1) / to);
+        if (int rc = launch(q, o)) return rc;
+    }
+    return PP_OK;
+}
+
+static pr_plan plan_forward(int64_t rows, int64_t n_in, int64_t n_out, int *shape) { return plan(SHAPES_FP4, 3, n_out, rows, pp_groups(n_in), shape); }
+static pr_plan plan_input(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
+    return plan(SHAPES_GRAD, 3, n_in, rows, planes_of(type) * ((n_out + 63) / 64), shape);
+}
+static pr_plan plan_weight(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
+    return plan(SHAPES_GRAD, 2, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), shape);
+}
+
+// ---- entry points
 
 static bool bad_layer(int type, int64_t rows, int64_t n_in, int64_t n_out) {
     return pp_bad_sizes(type, rows, n_in) || n_out < 1 || n_out > PP_LAYER_MAX_COLS;
 }
 
+static int64_t planes_ld(int64_t n_out) { return (n_out + 7) & ~(int64_t)7; }
+static size_t planes_bytes(int type, int64_t rows, int64_t n_out) { return pp_align256((size_t)planes_of(type) * rows * planes_ld(n_out) * 2); }
+
 extern "C" size_t pp_linear_workspace_bytes(int call, int type, int64_t rows, int64_t n_in, int64_t n_out) {
     if (call < PP_LINEAR_FORWARD || call > PP_LINEAR_BACKWARD_WEIGHT || bad_layer(type, rows, n_in, n_out)) return 0;
-    if (call != PP_LINEAR_FORWARD) return 256;
-    return 256 + pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4) + pp_align256((size_t)rows * pp_groups(n_in) * 4);
+    int shape;
+    if (call == PP_LINEAR_FORWARD)
+        return 256 + pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4) + pp_align256((size_t)rows * pp_groups(n_in) * 4) +
+               pp_align256(partial_bytes(plan_forward(rows, n_in, n_out, &shape)));
+    if (call == PP_LINEAR_BACKWARD_INPUT)
+        return 256 + planes_bytes(type, rows, n_out) + pp_align256(partial_bytes(plan_input(type, rows, n_in, n_out, &shape)));
+    const pr_plan p = plan_weight(type, rows, n_in, n_out, &shape);
+    return 256 + planes_bytes(type, rows, n_out) + pp_align256(partial_bytes(p)) + pp_align256((size_t)p.splits * n_out * 4);
 }
 
 static int bad_workspace(int call, int type, int64_t rows, int64_t n_in, int64_t n_out, const void *ws, size_t bytes) {
@@ -112,16 +183,32 @@ extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n
     if (int rc = bad_workspace(PP_LINEAR_FORWARD, type, rows, n_in, n_out, workspace, workspace_bytes)) return rc;
     if (!rows) return PP_OK;
     hipStream_t st = (hipStream_t)stream;
-    uint8_t *codes = (uint8_t *)workspace, *scales = codes + pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4);
+    const long long g = pp_groups(n_in);
+    uint8_t *codes = (uint8_t *)workspace, *scales = codes + pp_align256((size_t)rows * g * PP_GROUP_CODES4);
     if (x_codes)
         if (int rc = pp_launch_pack(PP_PACK_INT8, type, rows, n_in, x, ld_x, x_codes, x_scales, st)) return rc;
     if (int rc = pp_launch_pack(PP_PACK_FP4, type, rows, n_in, x, ld_x, codes, scales, st)) return rc;
-    const long long g = pp_groups(n_in);
-    return pp_by_type(type, [&](auto t) {
-        typedef decltype(t) Y;
-        return product(rows, n_out, n_in, FromFp4{codes, scales, g}, FromFp4{(const uint8_t *)w_codes, (const uint8_t *)w_scales, g},
-                       ToMatrix<Y>{(typename Y::T *)y, ld_y, bias, 0}, st);
+    int shape;
+    pr_plan p = plan_forward(rows, n_in, n_out, &shape);
+    p.partial = (float *)(scales + pp_align256((size_t)rows * g * 4));
+    const int rc = in_turns(p, SHAPES_FP4[shape].to, [&](const pr_plan &q, long long o) {
+        return p4_launch(shape, type, q, p4_operands{(const uint8_t *)w_codes, (const uint8_t *)w_scales, codes + o * g * PP_GROUP_CODES4, scales + o * g * 4},
+                         (uint8_t *)y + o * ld_y * pp_type_size(type), ld_y, bias, st);
     });
+    if (rc || p.splits == 1) return rc;
+    return launch_join(type, p, y, ld_y, bias, NULL, NULL, NULL, st);
+}
+
+// dy as the products take it: as it is where it can be loaded so, else copied into `room`.
+static int outer_of(int type, bool along_sum, int64_t rows, int64_t cols, const void *dy, int64_t ld, void *room, pg_outer *out, hipStream_t st) {
+    if (rows < 2) ld = cols;
+    if (type == PP_TYPE_BF16 && !((uintptr_t)dy & 15) && (rows < 2 || !(ld & 7)) && (!along_sum || !(cols & 7))) {
+        *out = pg_outer{(const uint8_t *)dy, rows, cols, ld, 0, 1};
+        return PP_OK;
+    }
+    const int64_t n = planes_ld(cols);
+    *out = pg_outer{(const uint8_t *)room, rows, n, n, rows * n, planes_of(type)};
+    return rows ? launch_planes(type, rows, cols, dy, ld, room, n, st) : PP_OK;
 }
 
 extern "C" int pp_linear_backward_input(int type, int64_t rows, int64_t n_in, int64_t n_out, const void *dy, int64_t ld_dy,
@@ -132,12 +219,21 @@ extern "C" int pp_linear_backward_input(int type, int64_t rows, int64_t n_in, in
     if (pp_bad_packed(w_codes, w_scales, n_out)) return PP_ERR_INVALID_ARG;
     if (int rc = bad_workspace(PP_LINEAR_BACKWARD_INPUT, type, rows, n_in, n_out, workspace, workspace_bytes)) return rc;
     if (!rows) return PP_OK;
-    return pp_by_type(type, [&](auto t) {
-        typedef decltype(t) Y;
-        return product(rows, n_in, n_out, FromMatrix<Y>{(const typename Y::T *)dy, ld_dy},
-                       Flip<FromFp4>{{(const uint8_t *)w_codes, (const uint8_t *)w_scales, pp_groups(n_in)}},
-                       ToMatrix<Y>{(typename Y::T *)dx, ld_dx, NULL, 0}, (hipStream_t)stream);
+    hipStream_t st = (hipStream_t)stream;
+    pg_outer y;
+    if (int rc = outer_of(type, true, rows, n_out, dy, ld_dy, workspace, &y, st)) return rc;
+    int shape;
+    pr_plan p = plan_input(type, rows, n_in, n_out, &shape);
+    p.partial = (float *)((uint8_t *)workspace + planes_bytes(type, rows, n_out));
+    const pg_inner w = {(const uint8_t *)w_codes, (const uint8_t *)w_scales, n_out, pp_groups(n_in)};
+    const int rc = in_turns(p, SHAPES_GRAD[shape].to, [&](const pr_plan &q, long long o) {
+        pg_outer part = y;
+        part.p += o * y.ld * 2;
+        part.rows = q.outer;
+        return pg_launch_input(shape, type, q, w, part, (uint8_t *)dx + o * ld_dx * pp_type_size(type), ld_dx, st);
     });
+    if (rc || p.splits == 1) return rc;
+    return launch_join(type, p, dx, ld_dx, NULL, NULL, NULL, NULL, st);
 }
 
 extern "C" int pp_linear_backward_weight(int type, int64_t rows, int64_t n_in, int64_t n_out, const void *dy, int64_t ld_dy,
@@ -148,15 +244,22 @@ extern "C" int pp_linear_backward_weight(int type, int64_t rows, int64_t n_in, i
     if (pp_bad_matrix(dw, PP_TYPE_F32, n_out, n_in, ld_dw) || ((uintptr_t)dw_in & 3) || ((uintptr_t)db & 3)) return PP_ERR_INVALID_ARG;
     if (int rc = bad_workspace(PP_LINEAR_BACKWARD_WEIGHT, type, rows, n_in, n_out, workspace, workspace_bytes)) return rc;
     hipStream_t st = (hipStream_t)stream;
-    return pp_by_type(type, [&](auto t) {
-        typedef decltype(t) Y;
-        typedef typename Y::T T;
-        if (db) {
-            k_column_sums<Y><<<(unsigned)((n_out + 63) / 64), 256, 0, st>>>(rows, n_out, (const T *)dy, ld_dy, db);
-            if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
-        }
-        return product(n_out, n_in, rows, Flip<FromMatrix<Y>>{{(const T *)dy, ld_dy}},
-                       Flip<FromInt8>{{(const uint8_t *)x_codes, (const uint8_t *)x_scales, pp_groups(n_in)}},
-                       ToMatrix<PpF32>{dw, ld_dw, dw_in, ld_dw}, st);
+    pg_outer y;
+    if (int rc = outer_of(type, false, rows, n_out, dy, ld_dy, workspace, &y, st)) return rc;
+    int shape;
+    pr_plan p = plan_weight(type, rows, n_in, n_out, &shape);
+    p.steps = y.planes * (int)(rows ? (rows + 63) / 64 : 1);
+    uint8_t *room = (uint8_t *)workspace + planes_bytes(type, rows, n_out);
+    p.partial = (float *)room;
+    float *part_sums = (float *)(room + pp_align256(partial_bytes(p)));
+    const pg_inner x = {(const uint8_t *)x_codes, (const uint8_t *)x_scales, rows, pp_groups(n_in)};
+    const int rc = in_turns(p, SHAPES_GRAD[shape].to, [&](const pr_plan &q, long long o) {
+        pg_outer part = y;
+        part.p += o * 2;
+        part.cols -= o;
+        return pg_launch_weight(shape, q, x, part, dw + o * ld_dw, ld_dw, dw_in ? dw_in + o * ld_dw : NULL,
+                                !db ? NULL : p.splits > 1 ? part_sums : db + o, st);
     });
+    if (rc || p.splits == 1) return rc;
+    return launch_join(PP_TYPE_F32, p, dw, ld_dw, NULL, dw_in, part_sums, db, st);
 }
