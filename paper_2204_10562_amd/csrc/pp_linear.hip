@@ -61,9 +61,14 @@ __global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const fl
         float v[8];
         *(pp_f4 *)v = a;
         *(pp_f4 *)(v + 4) = b;
-        pr_plan whole = p;
-        whole.splits = 1;
-        pr_put8<Y>(whole, out, o, i, 0, v);
+        if (out.bias || out.add) {
+            const PpRaw<PpF32> r = pp_load8<PpF32>(out.bias ? out.bias + i : out.add + o * out.add_ld + i, p.inner - i);
+            float w[8];
+            pp_values<PpF32>(r, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += w[j];
+        }
+        pp_store8<Y>(out.p + o * out.ld + i, p.inner - i, v);
     }
     if (sums)
         for (long long o = (long long)blockIdx.x * 256 + threadIdx.x; o < p.outer; o += (long long)gridDim.x * 256) {

@@ -78,51 +78,114 @@ __device__ __forceinline__ void pr_barrier() { asm volatile("s_waitcnt lgkmcnt(0
 
 __device__ __forceinline__ unsigned pr_lds_of(const void *p) { return (unsigned)(uintptr_t)(PR_LDS const void *)p; }
 
-// Row of the inner operand that lane row `i` (0..15) of fragment f takes: a lane's results of two
-// fragments are eight neighbours, 16 bytes of a 16-bit type.
-__device__ __forceinline__ int pr_inner_row(int f, int i) { return 32 * (f >> 1) + 8 * (i >> 2) + 4 * (f & 1) + (i & 3); }
+// The matrix instructions here are those of 32 x 32 results: lane l holds column l % 32 of the outer
+// operand and, of the inner one's 32 rows, 8 q + 4 (l / 32) + 0..3 for q = 0..3.  Row i of a fragment
+// is therefore read from row pr_inner_row(i) of the tile (bits 2 and 3 exchanged), which makes a lane's
+// results two runs of eight neighbours, 16 bytes of a 16-bit type each.
+__device__ __forceinline__ int pr_inner_row(int i) { return (i & ~12) | (i & 4) << 1 | (i & 8) >> 1; }
+typedef float pr_f16 __attribute__((ext_vector_type(16)));
 
-// Eight results of a lane, inner index i on, row o.
-template <class Y> __device__ __forceinline__ void pr_put8(const pr_plan &p, const pr_out<Y> &out, long long o, long long i, int piece, float *v) {
-    if (o >= p.outer || i >= p.inner) return;
-    const long long n = p.inner - i;
-    if (p.splits > 1) {
-        float *q = p.partial + ((long long)piece * p.outer + o) * p.partial_ld + i;  // rows padded to 8
-        *(pp_f4 *)q = *(pp_f4 *)v;
-        *(pp_f4 *)(q + 4) = *(pp_f4 *)(v + 4);
-        return;
-    }
-    if (out.bias || out.add) {
-        const float *a = out.bias ? out.bias + i : out.add + o * out.add_ld + i;
-        const PpRaw<PpF32> r = pp_load8<PpF32>(a, n);
-        float w[8];
-        pp_values<PpF32>(r, w);
+// How results leave.  A lane holds runs of eight neighbours of a row, a wave's fragments 32 rows of
+// 32 WI of them: stored as they are, a wave would write 32 bytes here and there, which costs four times
+// what whole lines do.  So a wave turns its fragments round in LDS (16-byte units exchanged by the row,
+// an exclusive or, so that neighbouring rows fall on different banks) and writes rows of them.
+// `room` is the wave's own, 32 rows of 32 WI results in 32 bits; no other wave reads there any more.
+template <class Y, int WI> struct PrRows {
+    static const int SIZE = sizeof(typename Y::T), UNITS = 32 * WI * SIZE / 16, VALUES = 16 / SIZE;
+    static const int ROWS = 64 / UNITS;  // that 64 lanes take at once
+    static __device__ __forceinline__ int at(int row, int unit) { return (row * UNITS + (unit ^ (row & (UNITS - 1)))) * 16; }
+    static __device__ __forceinline__ void put(uint8_t *room, int row, int col, const float *v) {
+        typename Y::T t[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += w[j];
+        for (int i = 0; i < 8; ++i) t[i] = Y::put(v[i]);
+        PpRaw<Y> r;
+        __builtin_memcpy(&r, t, sizeof(r));
+#pragma unroll
+        for (int i = 0; i < PpRaw<Y>::W; ++i) *(pp_u4 *)(room + at(row, col / VALUES + i)) = r.w[i];
     }
-    pp_store8<Y>(out.p + o * out.ld + i, n, v);
+    // rows o0.. of the result, columns i0..; `add` in the same places, where Y is float
+    static __device__ __forceinline__ void store(const uint8_t *room, int lane, typename Y::T *p, long long ld, long long o0, long long outer,
+                                                 long long i0, long long inner, const float *add, long long add_ld) {
+        const long long i = i0 + lane % UNITS * VALUES;
+#pragma unroll 4
+        for (int t = 0; t < 32 / ROWS; ++t) {
+            const int row = t * ROWS + lane / UNITS;
+            const long long o = o0 + row;
+            pp_u4 w = *(const pp_u4 *)(room + at(row, lane % UNITS));
+            if (o >= outer || i >= inner) continue;
+            typename Y::T *q = p + o * ld + i;
+            if (i + VALUES <= inner) {
+                if constexpr (SIZE == 4)
+                    if (add) {
+                        const pp_u4 d = ((const pp_any16<4> *)(add + o * add_ld + i))->v;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = pp_bits(pp_bits(w[j]) + pp_bits(d[j]));
+                    }
+                ((pp_any16<SIZE> *)q)->v = w;
+            } else {
+                typename Y::T v[VALUES];
+                __builtin_memcpy(v, &w, 16);
+#pragma unroll
+                for (int j = 0; j < VALUES; ++j)
+                    if (i + j < inner) {
+                        if constexpr (SIZE == 4)
+                            if (add) v[j] += add[o * add_ld + i + j];
+                        q[j] = v[j];
+                    }
+            }
+        }
+    }
+};
+
+// A wave's results: columns i0.., rows o0...
+template <class Y, int WI, int WO, class ACC>
+__device__ __forceinline__ void pr_leave(const pr_plan &p, const pr_out<Y> &out, ACC &acc, uint8_t *room, int lane, long long i0, long long o0, int piece) {
+    const int r = lane & 31, g = lane >> 5;
+    const bool whole = p.splits == 1;
+#pragma unroll
+    for (int j = 0; j < WO; ++j) {
+#pragma unroll
+        for (int i = 0; i < WI; ++i) {
+            float v[16];
+            *(pr_f16 *)v = acc[i][j];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int col = 32 * i + 16 * h + 8 * g;
+                if (!whole) {
+                    PrRows<PpF32, WI>::put(room, r, col, v + 8 * h);
+                    continue;
+                }
+                if (out.bias) {
+                    const PpRaw<PpF32> b = pp_load8<PpF32>(out.bias + i0 + col, p.inner - i0 - col);
+                    float w[8];
+                    pp_values<PpF32>(b, w);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) v[8 * h + k] += w[k];
+                }
+                PrRows<Y, WI>::put(room, r, col, v + 8 * h);
+            }
+        }
+        if (whole)
+            PrRows<Y, WI>::store(room, lane, out.p, out.ld, o0 + 32 * j, p.outer, i0, p.inner, out.add, out.add_ld);
+        else
+            PrRows<PpF32, WI>::store(room, lane, p.partial + (long long)piece * p.outer * p.partial_ld, p.partial_ld, o0 + 32 * j, p.outer, i0, p.inner, NULL, 0);
+    }
 }
 
-// acc[j] += a b[j] for N fragments of the outer operand, 16 x 16 x 32 in bf16.  Written as one block
-// because the results have to stay in their registers: where the compiler chooses, it gives every
-// product new ones and moves sums about.  What the compiler then does not see is waited for here: two
-// wait states from a register's writing to its use as an operand, and pr_settle before a sum is read.
-template <int N> __device__ __forceinline__ void pr_multiply(pp_f4 *acc, pr_bf8 a, const pr_bf8 *b) {
-    if constexpr (N == 4)
-        asm volatile("s_nop 1\n\t"
-                     "v_mfma_f32_16x16x32_bf16 %0, %4, %5, %0\n\t"
-                     "v_mfma_f32_16x16x32_bf16 %1, %4, %6, %1\n\t"
-                     "v_mfma_f32_16x16x32_bf16 %2, %4, %7, %2\n\t"
-                     "v_mfma_f32_16x16x32_bf16 %3, %4, %8, %3"
-                     : "+a"(acc[0]), "+a"(acc[1]), "+a"(acc[2]), "+a"(acc[3]) : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]));
-    else
-#pragma unroll
-        for (int j = 0; j < N; ++j) asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(acc[j]) : "v"(a), "v"(b[j]));
+// Products are written in assembly because their results have to stay in their registers: where the
+// compiler chooses, it gives every product new ones and moves sums about.  They stand one by one, with
+// what else there is to do between them: a wave has a matrix unit to itself and issues in order, so
+// a product's 32 cycles leave room for seven other instructions, and what comes in a heap leaves the
+// unit idle.  What the compiler does not see has to be right as it stands: operands come from loads
+// (which it waits for), never from an instruction less than two ahead, and sums are read behind
+// pr_settle.
+__device__ __forceinline__ void pr_multiply(pr_f16 &acc, pr_bf8 a, pr_bf8 b) {
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
 }
+#define PR_PIN __builtin_amdgcn_sched_barrier(0)  // instructions stay on their side
 
 // Behind a loop's last products (where s == end): the matrix units have written their results.  The
-// branch around the two waits is in here so that it stays within the loop, before any use of a sum.
+// branch around the waits is in here so that it stays within the loop, before any use of a sum.
 __device__ __forceinline__ void pr_settle(int s, int end) {
     asm volatile("s_cmp_lg_u32 %0, %1\n\ts_cbranch_scc1 2\n\ts_nop 15\n\ts_nop 15" ::"s"(s), "s"(end) : "scc", "memory");
 }
-

@@ -7,8 +7,9 @@
 // their rows are read transposed (four values of a column to a lane, two reads to a fragment).
 #include "pp_product_grad.h"
 
+// WI x WO fragments of 32 x 32 to a wave, NI x NO waves
 template <int WI, int WO, int NI, int NO> struct PgTile {
-    static const int TI = 16 * WI * NI, TO = 16 * WO * NO;
+    static const int TI = 32 * WI * NI, TO = 32 * WO * NO;
     static const int SI = TI * 128, SO = TO * 128;  // bytes of a stage: 64 values of the sum
     static const int LDS = 2 * (SI + SO);
 };
@@ -23,33 +24,36 @@ __device__ __forceinline__ pr_bf8 pg_read_t(const uint8_t *p, int second) {  // 
     return __builtin_bit_cast(pr_bf8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Sixteen packed values as bf16: exact, NaN where the block is.
-template <int FMT> __device__ __forceinline__ void pg_convert(pp_u4 raw, unsigned byte, pp_u4 *out) {
-    if constexpr (FMT == PP_PACK_INT8) {
-        const float unit = pp_unit8(byte);
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-            const unsigned c = raw[w >> 1] >> (16 * (w & 1));
-            const pp_bf2 v = {(__bf16)((float)(signed char)c * unit), (__bf16)((float)(signed char)(c >> 8) * unit)};
-            out[w >> 2][w & 3] = __builtin_bit_cast(unsigned, v);
-        }
-    } else {
-        const float unit = pp_unit4(byte == 255 ? 0 : byte);
-        const unsigned nan = byte == 255 ? 0x7fc07fc0u : 0;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            out[w][0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw[w], unit, 0)) | nan;
-            out[w][1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw[w], unit, 1)) | nan;
-            out[w][2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw[w], unit, 2)) | nan;
-            out[w][3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw[w], unit, 3)) | nan;
+// Two packed values, the w-th of a piece of sixteen, as bf16: exact, NaN where the block is.
+template <int FMT> struct PgUnit {  // of a block
+    float unit;
+    unsigned nan;
+    __device__ __forceinline__ void set(unsigned byte) {
+        if constexpr (FMT == PP_PACK_INT8) unit = pp_unit8(byte);
+        else {
+            unit = pp_unit4(byte == 255 ? 0 : byte);
+            nan = byte == 255 ? 0x7fc07fc0u : 0;
         }
     }
-}
+    __device__ __forceinline__ unsigned two(pp_u4 raw, int w) const {
+        if constexpr (FMT == PP_PACK_INT8) {
+            const unsigned c = raw[w >> 1] >> (16 * (w & 1));
+            const pp_bf2 v = {(__bf16)((float)(signed char)c * unit), (__bf16)((float)(signed char)(c >> 8) * unit)};
+            return __builtin_bit_cast(unsigned, v);
+        }
+        const unsigned c = raw[w >> 2];
+        pp_bf2 v;
+        if ((w & 3) == 0) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 0);
+        else if ((w & 3) == 1) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 1);
+        else if ((w & 3) == 2) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 2);
+        else v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 3);
+        return __builtin_bit_cast(unsigned, v) | nan;
+    }
+};
 
 template <int FMT, bool ALONG, int WI, int WO, int NI, int NO, class Y, bool SUMS>
 __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_inner x, pg_outer y, pr_out<Y> out, float *sums) {
     typedef PgTile<WI, WO, NI, NO> L;
-    constexpr int H = WO / 2, P = H ? H : WO;
     constexpr int CB = FMT == PP_PACK_INT8 ? 16 : 8;  // bytes of sixteen codes
     constexpr int PER_ROW = L::TI / 16, ROWS = PR_THREADS / PER_ROW, PIECES = 64 / ROWS;  // sixteen codes to a thread, PIECES times
     constexpr int RI = L::TI * 2, RO = L::TO * 2;     // bytes of a row of the sum
@@ -77,29 +81,33 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
     }
     pp_u4 raw[PIECES];
     unsigned char scale[PIECES];
-    auto load_inner = [&](int s) {
+    __amdgpu_buffer_rsrc_t xb, xsb;  // of the step whose codes are loaded next
+    auto aim_inner = [&](int s) {
         const long long c0 = (long long)((s0 + s) % per_plane) * 64;
-        const auto b = pr_resource(x.codes + c0 * xpitch, (x.rows - c0) * xpitch), sc = pr_resource(x.scales + c0 * spitch, (x.rows - c0) * spitch);
-#pragma unroll
-        for (int j = 0; j < PIECES; ++j) {
-            if constexpr (FMT == PP_PACK_INT8) {
-                raw[j] = __builtin_bit_cast(pp_u4, __builtin_amdgcn_raw_buffer_load_b128(b, vx[j], 0, 0));
-            } else {
-                const pp_u2 t = __builtin_bit_cast(pp_u2, __builtin_amdgcn_raw_buffer_load_b64(b, vx[j], 0, 0));
-                raw[j] = pp_u4{t[0], t[1], 0, 0};
-            }
-            scale[j] = __builtin_amdgcn_raw_buffer_load_b8(sc, vs[j], 0, 0);
+        xb = pr_resource(x.codes + c0 * xpitch, (x.rows - c0) * xpitch);
+        xsb = pr_resource(x.scales + c0 * spitch, (x.rows - c0) * spitch);
+    };
+    auto load_inner = [&](int j) {
+        if constexpr (FMT == PP_PACK_INT8) {
+            raw[j] = __builtin_bit_cast(pp_u4, __builtin_amdgcn_raw_buffer_load_b128(xb, vx[j], 0, 0));
+        } else {
+            const pp_u2 t = __builtin_bit_cast(pp_u2, __builtin_amdgcn_raw_buffer_load_b64(xb, vx[j], 0, 0));
+            raw[j][0] = t[0];
+            raw[j][1] = t[1];
         }
+        scale[j] = __builtin_amdgcn_raw_buffer_load_b8(xsb, vs[j], 0, 0);
     };
     int wx[PIECES];
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) wx[j] = (xr + j * ROWS) * RI + 32 * (xc ^ pg_turn(xr + j * ROWS));
-    auto store_inner = [&](int j, int s) {
-        pp_u4 v[2];
-        pg_convert<FMT>(raw[j], scale[j], v);
-        uint8_t *q = sm + (s & 1) * (L::SI + L::SO) + wx[j];
-        *(pp_u4 *)q = v[0];
-        *(pp_u4 *)(q + 16) = v[1];
+    PgUnit<FMT> unit;
+    pp_u4 half;
+    // Part t of turning step s's packed values into bf16: two of them, the eighth part of a piece.
+    auto turn_inner = [&](int t, int s) {
+        const int j = t >> 3, w = t & 7;
+        if (w == 0) unit.set(scale[j]);
+        half[w & 3] = unit.two(raw[j], w);
+        if ((w & 3) == 3) *(pp_u4 *)(sm + (s & 1) * (L::SI + L::SO) + wx[j] + 16 * (w >> 2)) = half;
     };
 
     // the gradients: 1024 bytes of a stage to a load of a wave
@@ -119,126 +127,139 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
             vo[j] = (unsigned)(row * y.ld * 2) + unit * 32 + (b & 16);
         }
     }
-    auto load_outer = [&](int s) {
+    pp_i4 ob;             // of the step whose gradients are loaded next
+    long long left = 1 << 30;  // columns of it that there are
+    auto aim_outer = [&](int s) {
         const int plane = (s0 + s) / per_plane;
         const long long c0 = (long long)(s0 + s - plane * per_plane) * 64;
         const uint8_t *q = y.p + plane * y.plane * 2;
-        pp_i4 b;
-        long long left = 1 << 30;
         if constexpr (ALONG) {
             const long long rows = y.rows - o0 < L::TO ? y.rows - o0 : L::TO;
             left = y.cols - c0;
-            b = pr_buffer(q + (o0 * y.ld + c0) * 2, s < steps ? ((rows - 1) * y.ld + left) * 2 : 0);
+            ob = pr_buffer(q + (o0 * y.ld + c0) * 2, ((rows - 1) * y.ld + left) * 2);
         } else {
             // up to the end of the last value's four bytes: less than four count as beyond the buffer
-            b = pr_buffer(q + (c0 * y.ld + o0) * 2, s < steps && c0 < y.rows ? (((y.rows - c0 - 1) * y.ld + y.cols - o0) * 2 + 3) & ~3ll : 0);
+            ob = pr_buffer(q + (c0 * y.ld + o0) * 2, c0 < y.rows ? (((y.rows - c0 - 1) * y.ld + y.cols - o0) * 2 + 3) & ~3ll : 0);
         }
-#pragma unroll
-        for (int j = 0; j < LO; ++j)
-            pr_to_lds(b, ALONG && col_o[j] >= left ? PR_BEYOND : vo[j], 0, base + (s & 1) * (L::SI + L::SO) + L::SI + lo[j]);
+    };
+    auto load_outer = [&](int j, int s) {
+        pr_to_lds(ob, ALONG && col_o[j] >= left ? PR_BEYOND : vo[j], 0, base + (s & 1) * (L::SI + L::SO) + L::SI + lo[j]);
     };
 
-    // fragments: inner ones transposed, outer ones where the sum runs across their rows
-    const int wi = wave % NI, wo = wave / NI, r = lane & 15, g = lane >> 4;
-    const int row_t = 8 * g + (r >> 2), turn = pg_turn(row_t);
-    int ai[WI / 2], ao[ALONG ? 1 : WO];
+    // fragments: inner ones transposed, outer ones where the sum runs across their rows.  A quarter of
+    // a step is 16 values of the sum, eight to a half of the lanes.
+    const int wi = wave % NI, wo = wave / NI, r = lane & 31, g = lane >> 5, h = (lane >> 4) & 1, u = lane & 15;
+    const int row_t = 8 * g + (u >> 2), turn = pg_turn(row_t);
+    int ai[WI], ao[ALONG ? 4 : WO];
 #pragma unroll
-    for (int j = 0; j < WI / 2; ++j) ai[j] = row_t * RI + 32 * ((wi * WI + 2 * j + ((r & 3) >> 1)) ^ turn) + 16 * (r & 1);
+    for (int j = 0; j < WI; ++j)  // chunk u % 4 of four columns, bits exchanged as by pr_inner_row
+        ai[j] = row_t * RI + 32 * ((2 * (wi * WI + j) + h) ^ turn) + 16 * (u & 1) + 4 * (u & 2);
     if constexpr (ALONG) {
-        ao[0] = L::SI + (wo * WO * 16 + r) * 128;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) ao[k] = L::SI + (wo * WO * 32 + r) * 128 + 16 * ((2 * k + g) ^ ((r >> 1) & 7));
     } else {
 #pragma unroll
-        for (int j = 0; j < WO; ++j) ao[j] = L::SI + row_t * RO + 32 * ((wo * WO + j) ^ (turn & TURN_O)) + 8 * (r & 3);
+        for (int j = 0; j < WO; ++j) ao[j] = L::SI + row_t * RO + 32 * ((2 * (wo * WO + j) + h) ^ (turn & TURN_O)) + 8 * (u & 3);
     }
-    pr_bf8 in[WI], first[P], late[H ? H : 1];
-    auto read_i = [&](int j, const uint8_t *b, int h) { in[j] = pg_read_t(b + ai[j >> 1] + 8 * (j & 1) + h * 32 * RI, 4 * RI); };
-    auto read_o = [&](pr_bf8 *f, int j0, int n, const uint8_t *b, int h) {
-#pragma unroll
-        for (int j = 0; j < n; ++j) {
-            if constexpr (ALONG) f[j] = *(const pr_bf8 *)(b + ao[0] + (j0 + j) * 2048 + 16 * ((4 * h + g) ^ (r >> 1)));
-            else f[j] = pg_read_t(b + ao[j0 + j] + h * 32 * RO, 4 * RO);
-        }
+    auto read_i = [&](const uint8_t *b, int k, int j) { return pg_read_t(b + ai[j] + k * 16 * RI, 4 * RI); };
+    auto read_o = [&](const uint8_t *b, int k, int j) {
+        if constexpr (ALONG) return *(const pr_bf8 *)(b + ao[k] + j * 4096);
+        else return pg_read_t(b + ao[j] + k * 16 * RO, 4 * RO);
     };
-    pp_f4 acc[WI][WO] = {}, acc_s[WO] = {};
+    pr_bf8 in[WI], outer[2][WO];  // the inner fragments are replaced as they have been used, the outer ones of odd quarters have places of their own
+    pr_f16 acc[WI][WO] = {}, acc_s[SUMS ? WO : 1] = {};
     const bool summing = SUMS && ti == 0 && wi == 0;
     const pr_bf8 ones = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
     // The columns' sums, a product with ones: in ordinary registers (the others are full), and waited
     // for at once, as what only some waves do may be moved about behind it.
-    auto add_up = [&](const pr_bf8 *f, int j0, int n) {
+    auto add_up = [&](const pr_bf8 *f) {
+        if constexpr (SUMS) {
 #pragma unroll
-        for (int j = 0; j < n; ++j)
-            asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc_s[j0 + j]) : "v"(ones), "v"(f[j]));
-        asm volatile("s_nop 15" : "+v"(acc_s[j0]));
+            for (int j = 0; j < WO; ++j) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc_s[j]) : "v"(ones), "v"(f[j]));
+            asm volatile("s_nop 15\n\ts_nop 3" : "+v"(acc_s[0]));
 #pragma unroll
-        for (int j = 1; j < n; ++j) asm volatile("" : "+v"(acc_s[j0 + j]));
+            for (int j = 1; j < WO; ++j) asm volatile("" : "+v"(acc_s[j]));
+        }
     };
 
-    load_outer(0);
-    load_inner(0);
+    constexpr int N = WI * WO, MEET = WO;  // products of a quarter step; those of the last one before the waves meet
+    constexpr int PARTS = 8 * PIECES;
+    aim_outer(0);
+    aim_inner(0);
 #pragma unroll
-    for (int j = 0; j < PIECES; ++j) store_inner(j, 0);
+    for (int j = 0; j < LO; ++j) load_outer(j, 0);
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) load_inner(j);
+#pragma unroll
+    for (int t = 0; t < PARTS; ++t) turn_inner(t, 0);
     PR_WAIT(0);
-    pr_barrier();
-    load_outer(1);
-    load_inner(1);
+    if (steps > 1) {
+        aim_outer(1);
+        aim_inner(1);
 #pragma unroll
-    for (int j = 0; j < WI; ++j) read_i(j, sm, 0);
-    read_o(first, 0, P, sm, 0);
+        for (int j = 0; j < LO; ++j) load_outer(j, 1);
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) load_inner(j);
+    }
+    pr_barrier();
+#pragma unroll
+    for (int j = 0; j < WI; ++j) in[j] = read_i(sm, 0, j);
+#pragma unroll
+    for (int j = 0; j < WO; ++j) outer[0][j] = read_o(sm, 0, j);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the compiler need not wait for these within the loop
     for (int s = 0; s < steps; ++s) {
         const uint8_t *now = sm + (s & 1) * (L::SI + L::SO), *next = sm + ((s + 1) & 1) * (L::SI + L::SO);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if constexpr (H > 0) {
-                read_o(late, H, H, now, h);
-                if (SUMS && summing) add_up(first, 0, H);
-            }
+        for (int k = 0; k < 4; ++k) {
+            const pr_bf8 *o = outer[k & 1];
+            const uint8_t *b = k < 3 ? now : next;  // after the last step: what lies there, for nothing
+            if (SUMS && summing) add_up(o);
+            if (k == 1) aim_inner(s + 2 < steps ? s + 2 : s);
 #pragma unroll
-            for (int i = 0; i < WI; ++i) {
-                if constexpr (H > 0) pr_multiply<H>(acc[i], in[i], first);
-                if (h == 1) {  // step s + 1's packed values, which were asked for a step ago
-#pragma unroll
-                    for (int j = i * PIECES / WI; j < (i + 1) * PIECES / WI; ++j) store_inner(j, s + 1);
+            for (int m = 0; m < N; ++m) {
+                const int i = m / WO, j = m % WO;
+                if (k == 3 && m == MEET) {  // step s + 1 is there, and every wave has read all of step s
+                    PR_WAIT(2 * PIECES);    // (but for the packed values of the step after it)
+                    pr_barrier();
+                    aim_outer(s + 2);
                 }
-            }
-            if (h == 1) {
-                PR_WAIT(0);  // and its gradients
-                pr_barrier();
-                load_outer(s + 2);
-                load_inner(s + 2);
-            }
-            const uint8_t *b = h == 0 ? now : next;  // after the last step: what lies there, for nothing
-            if constexpr (H > 0) read_o(first, 0, H, b, 1 - h);
+                pr_multiply(acc[i][j], in[i], o[j]);
+                if (k < 3) {
+                    if (i == 0) outer[(k + 1) & 1][j] = read_o(b, k + 1, j);
+                    if (j == WO - 1) in[i] = read_i(b, k + 1, i);
+                } else if (m >= MEET) {
+                    if (m - MEET < WO) outer[0][m - MEET] = read_o(b, 0, m - MEET);
+                    if (m == MEET) in[0] = read_i(b, 0, 0);
+                    if (j == WO - 1) in[i] = read_i(b, 0, i);
+                }
+                if (k == 1 || k == 2) {
+                    const int slot = (k - 1) * N + m;
 #pragma unroll
-            for (int i = 0; i < WI; ++i) {
-                if constexpr (H > 0) pr_multiply<H>(acc[i] + H, in[i], late);
-                else pr_multiply<WO>(acc[i], in[i], first);
-                read_i(i, b, 1 - h);
-            }
-            if constexpr (H > 0) {
-                if (SUMS && summing) add_up(late, H, H);
-            } else {
-                if (SUMS && summing) add_up(first, 0, WO);
-                read_o(first, 0, P, b, 1 - h);
+                    for (int t = slot * PARTS / (2 * N); t < (slot + 1) * PARTS / (2 * N); ++t) {
+                        turn_inner(t, s + 1);
+                        if ((t & 7) == 7) load_inner(t >> 3);  // step s + 2's: a whole step ahead
+                    }
+                }
+                if (k == 3 && m >= MEET && s + 2 < steps) {
+#pragma unroll
+                    for (int l = (m - MEET) * LO / (N - MEET); l < (m + 1 - MEET) * LO / (N - MEET); ++l) load_outer(l, s + 2);
+                }
+                PR_PIN;
             }
         }
         pr_settle(s + 1, steps);
     }
-    PR_WAIT(0);  // nothing is on its way to LDS when the workgroup ends
+    PR_WAIT(0);  // nothing is on its way to LDS any more
+    pr_barrier();
+    if constexpr (SUMS)
+        if (summing && g == 0) {
 #pragma unroll
-    for (int j = 0; j < WO; ++j) {
-        const long long o = o0 + (wo * WO + j) * 16 + r;
-#pragma unroll
-        for (int i = 0; i < WI; i += 2) {
-            float v[8];
-            *(pp_f4 *)v = acc[i][j];
-            *(pp_f4 *)(v + 4) = acc[i + 1][j];
-            pr_put8<Y>(p, out, o, i0 + wi * WI * 16 + 16 * i + 8 * g, piece, v);
+            for (int j = 0; j < WO; ++j) {
+                const long long o = o0 + (wo * WO + j) * 32 + r;
+                if (o < p.outer) sums[piece * p.outer + o] = acc_s[j][0];
+            }
         }
-        if constexpr (SUMS)
-            if (summing && g == 0 && o < p.outer) sums[piece * p.outer + o] = acc_s[j][0];
-        __builtin_amdgcn_sched_barrier(0);
-    }
+    pr_leave<Y, WI, WO>(p, out, acc, sm + wave * (32 * 32 * WI * 4), lane, i0 + wi * WI * 32, o0 + wo * WO * 32, piece);
 }
 
 template <int FMT, bool ALONG, int WI, int WO, int NI, int NO, class Y, bool SUMS>
@@ -265,12 +286,12 @@ static int launch_weight(const pr_plan &p, const pg_inner &x, const pg_outer &y,
 }
 
 int pg_launch_input(int shape, int type, const pr_plan &p, const pg_inner &w, const pg_outer &dy, void *dx, long long ld, hipStream_t st) {
-    if (shape == 0) return launch_input<8, 8, 2, 2>(type, p, w, dy, dx, ld, st);
-    if (shape == 1) return launch_input<4, 4, 2, 2>(type, p, w, dy, dx, ld, st);
-    return launch_input<4, 2, 4, 1>(type, p, w, dy, dx, ld, st);
+    if (shape == 0) return launch_input<4, 4, 2, 2>(type, p, w, dy, dx, ld, st);
+    if (shape == 1) return launch_input<2, 2, 2, 2>(type, p, w, dy, dx, ld, st);
+    return launch_input<2, 1, 4, 1>(type, p, w, dy, dx, ld, st);
 }
 
 int pg_launch_weight(int shape, const pr_plan &p, const pg_inner &x, const pg_outer &dy, float *dw, long long ld, const float *add, float *sums, hipStream_t st) {
-    if (shape == 0) return launch_weight<8, 8, 2, 2>(p, x, dy, dw, ld, add, sums, st);
-    return launch_weight<4, 4, 2, 2>(p, x, dy, dw, ld, add, sums, st);
+    if (shape == 0) return launch_weight<4, 4, 2, 2>(p, x, dy, dw, ld, add, sums, st);
+    return launch_weight<2, 2, 2, 2>(p, x, dy, dw, ld, add, sums, st);
 }
