@@ -165,6 +165,8 @@ static size_t planes_bytes(int type, int64_t rows, int64_t n_out) { return pp_al
 extern "C" size_t pp_linear_workspace_bytes(int call, int type, int64_t rows, int64_t n_in, int64_t n_out) {
     if (call < PP_LINEAR_FORWARD || call > PP_LINEAR_BACKWARD_WEIGHT || bad_layer(type, rows, n_in, n_out)) return 0;
     int shape;
+    if (call == PP_LINEAR_FORWARD && rows <= R4_ROWS)
+        return 256 + pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4) + pp_align256((size_t)rows * pp_groups(n_in) * 4);
     if (call == PP_LINEAR_FORWARD)
         return 256 + pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4) + pp_align256((size_t)rows * pp_groups(n_in) * 4) +
                pp_align256(partial_bytes(plan_forward(rows, n_in, n_out, &shape)));
@@ -190,9 +192,14 @@ extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n
     hipStream_t st = (hipStream_t)stream;
     const long long g = pp_groups(n_in);
     uint8_t *codes = (uint8_t *)workspace, *scales = codes + pp_align256((size_t)rows * g * PP_GROUP_CODES4);
+    const p4_operands all = {(const uint8_t *)w_codes, (const uint8_t *)w_scales, codes, scales};
+    if (rows == 1) ld_x = n_in;
+    if (rows <= R4_ROWS && r4_fuses(rows, n_in, n_out))
+        return r4_launch(type, rows, n_in, n_out, x, ld_x, (uint8_t *)x_codes, (uint8_t *)x_scales, all, y, ld_y, bias, st);
     if (x_codes)
         if (int rc = pp_launch_pack(PP_PACK_INT8, type, rows, n_in, x, ld_x, x_codes, x_scales, st)) return rc;
     if (int rc = pp_launch_pack(PP_PACK_FP4, type, rows, n_in, x, ld_x, codes, scales, st)) return rc;
+    if (rows <= R4_ROWS) return r4_launch(type, rows, n_in, n_out, x, ld_x, NULL, NULL, all, y, ld_y, bias, st);
     int shape;
     pr_plan p = plan_forward(rows, n_in, n_out, &shape);
     p.partial = (float *)(scales + pp_align256((size_t)rows * g * 4));

@@ -167,12 +167,153 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product4(pr_plan p, p4_operan
     pr_leave<Y, WI, WO>(p, out, acc, sm + wave * (32 * 32 * WI * 4), lane, i0 + wi * WI * 32, o0 + wo * WO * 32, piece);
 }
 
+// k_rows4: few rows of x (16 NB at most).  The weight is read once, straight into registers, by waves
+// that divide the sum among them: a wave takes 16 rows of W and up to eight groups at a time, and what
+// the waves of a workgroup have found is added in LDS.  With FUSED the workgroup also packs x itself
+// (rows of it are little beside 16 rows of W) and, for pp_linear_backward_weight, a part of x in 8 bits.
+#define R4_MAX_WAVES 16
+struct r4_x {  // FUSED: the matrix; else its codes and scales
+    const void *x;
+    long long ld, cols;
+    uint8_t *kept_codes, *kept_scales;  // or NULL
+    const uint8_t *codes, *scales;
+};
+
+template <int NB, bool FUSED, class Y>
+__global__ __launch_bounds__(64 * R4_MAX_WAVES) void k_rows4(int rows, long long inner, int groups, const uint8_t *__restrict__ w_codes,
+                                                             const uint8_t *__restrict__ w_scales, r4_x x, pr_out<Y> out) {
+    typedef typename Y::T T;
+    extern __shared__ uint8_t sm[];  // sums of the waves [NB][waves][64] of 16 bytes; FUSED: x's codes, then its scales
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
+    const int r = lane & 15, g = lane >> 4;
+    const long long n0 = (long long)blockIdx.x * 16;
+    const int per = (groups + waves - 1) / waves, k0 = wave * per, k1 = k0 + per < groups ? k0 + per : groups;
+    uint8_t *xc = sm + NB * waves * 1024, *xs = xc + rows * groups * PP_GROUP_CODES4;
+    const long long n = n0 + r < inner ? n0 + r : inner - 1;
+    const uint8_t *wc = w_codes + n * groups * PP_GROUP_CODES4 + 16 * g, *ws = w_scales + n * groups * 4;
+
+    pp_u4 w[8], s4[2];
+    auto load = [&](int k) {
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+            if (k + t < k1) w[t] = *(const pp_u4 *)(wc + (long long)(k + t) * PP_GROUP_CODES4);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {  // four groups' scales; one by one where fewer are left
+            if (k + 4 * h + 4 <= k1) s4[h] = ((const pp_any16<4> *)(ws + 4ll * (k + 4 * h)))->v;
+            else
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (k + 4 * h + t < k1) s4[h][t] = *(const unsigned *)(ws + 4ll * (k + 4 * h + t));
+        }
+    };
+    if constexpr (FUSED) {
+        const int row_chunks = groups * 16, chunks = rows * row_chunks, threads = blockDim.x;
+        const T *src = (const T *)x.x;
+        auto fetch = [&](int q) {
+            const int row = q / row_chunks, c = q - row * row_chunks;
+            return pp_load8<Y>(src + row * x.ld + 8 * c, q < chunks ? x.cols - 8ll * c : 0);
+        };
+        PpRaw<Y> raw = fetch(tid);  // before the weight's: what is waited for first is asked for first
+        load(k0);
+        for (int q = tid; q < chunks; q += threads) {
+            const PpRaw<Y> now = raw;
+            if (q + threads < chunks) raw = fetch(q + threads);
+            float v[8];
+            pp_values<Y>(now, v);
+            const unsigned m = pp_quad_max(pp_absmax<Y>(now, v));
+            unsigned c;
+            const unsigned byte = pp_codes4(v, m, c);
+            *(unsigned *)(xc + q * 4) = c;
+            if (!(q & 3)) xs[q >> 2] = (uint8_t)byte;
+            if (x.kept_codes && (unsigned)(q / threads) % gridDim.x == blockIdx.x) {
+                pp_u2 c8;
+                const unsigned byte8 = pp_codes8(v, m, c8);
+                *(pp_u2 *)(x.kept_codes + q * 8ll) = c8;
+                if (!(q & 3)) x.kept_scales[q >> 2] = (uint8_t)byte8;
+            }
+        }
+        __syncthreads();
+    } else {
+        load(k0);
+    }
+    pp_f4 acc[NB] = {};
+    for (int k = k0; k < k1; k += 8) {
+        if (k > k0) load(k);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+            if (k + t >= k1) break;
+            const pr_i8 a = {(int)w[t][0], (int)w[t][1], (int)w[t][2], (int)w[t][3]};
+            const int ca = s4[t >> 2][t & 3] >> (8 * g);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int m = 16 * b + r;
+                pp_u4 c = {0, 0, 0, 0};
+                int cb = 0;
+                if (m < rows) {
+                    const long long at = (long long)m * groups + k + t;
+                    c = *(const pp_u4 *)((FUSED ? xc : x.codes) + at * PP_GROUP_CODES4 + 16 * g);
+                    cb = (FUSED ? xs : x.scales)[at * 4 + g];
+                }
+                const pr_i8 d = {(int)c[0], (int)c[1], (int)c[2], (int)c[3]};
+                acc[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, d, acc[b], 4, 4, 0, ca, 0, cb);
+            }
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) ((pp_f4 *)sm)[(b * waves + wave) * 64 + lane] = acc[b];
+    __syncthreads();
+    if (wave < NB) {
+        pp_f4 v = {0, 0, 0, 0};
+        for (int t = 0; t < waves; ++t) v += ((const pp_f4 *)sm)[(wave * waves + t) * 64 + lane];
+        const int m = 16 * wave + r;
+        if (m < rows)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const long long i = n0 + 4 * g + j;
+                if (i < inner) out.p[m * out.ld + i] = Y::put(out.bias ? v[j] + out.bias[i] : v[j]);
+            }
+    }
+}
+
+// Waves to a workgroup: four where the rows of W alone fill the chip, more (down to two groups each)
+// where they do not.
+static int r4_waves(long long inner, long long groups) {
+    int n = 4;
+    while (n < R4_MAX_WAVES && (inner + 15) / 16 * n < 4096 && 2 * n * 2 <= groups) n *= 2;
+    return n;
+}
+static size_t r4_lds(int nb, int waves, int64_t rows, long long groups, bool fused) {
+    return (size_t)nb * waves * 1024 + (fused ? rows * groups * (PP_GROUP_CODES4 + 4) : 0);
+}
+
+// Whether a workgroup packs x itself: few rows, and few enough for LDS.
+bool r4_fuses(int64_t rows, int64_t n_in, int64_t n_out) {
+    return rows <= R4_FUSED_ROWS && r4_lds(1, r4_waves(n_out, pp_groups(n_in)), rows, pp_groups(n_in), true) <= 65536;
+}
+
+int r4_launch(int type, int64_t rows, int64_t n_in, int64_t n_out, const void *x, int64_t ld_x, uint8_t *kept_codes, uint8_t *kept_scales,
+              const p4_operands &q, void *y, int64_t ld_y, const float *bias, hipStream_t st) {
+    const long long groups = pp_groups(n_in);
+    const int waves = r4_waves(n_out, groups), nb = rows > 16 ? 2 : 1;
+    const bool fused = r4_fuses(rows, n_in, n_out);
+    const r4_x a = {x, ld_x, n_in, kept_codes, kept_scales, q.outer_codes, q.outer_scales};
+    const size_t lds = r4_lds(nb, waves, rows, groups, fused);
+    const unsigned grid = (unsigned)((n_out + 15) / 16);
+    return pp_by_type(type, [&](auto t) {
+        typedef decltype(t) Y;
+        const pr_out<Y> o = {(typename Y::T *)y, ld_y, bias, NULL, 0};
+        if (fused) k_rows4<1, true, Y><<<grid, 64 * waves, lds, st>>>((int)rows, n_out, (int)groups, q.inner_codes, q.inner_scales, a, o);
+        else if (nb == 1) k_rows4<1, false, Y><<<grid, 64 * waves, lds, st>>>((int)rows, n_out, (int)groups, q.inner_codes, q.inner_scales, a, o);
+        else k_rows4<2, false, Y><<<grid, 64 * waves, lds, st>>>((int)rows, n_out, (int)groups, q.inner_codes, q.inner_scales, a, o);
+        return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+    });
+}
+
 template <int WI, int WO, int NI, int NO> static int launch4(int type, pr_plan p, const p4_operands &q, void *y, long long ld, const float *bias, hipStream_t st) {
     typedef P4Tile<WI, WO, NI, NO> L;
     return pp_by_type(type, [&](auto t) {
         typedef decltype(t) Y;
         auto *k = k_product4<WI, WO, NI, NO, Y>;
-        if (hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, L::LDS) != hipSuccess) return PP_ERR_HIP;
         k<<<dim3(p.ni * p.no, p.splits), PR_THREADS, L::LDS, st>>>(p, q, pr_out<Y>{(typename Y::T *)y, ld, bias, NULL, 0});
         return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
     });

@@ -266,7 +266,6 @@ template <int FMT, bool ALONG, int WI, int WO, int NI, int NO, class Y, bool SUM
 static int launch_one(const pr_plan &p, const pg_inner &x, const pg_outer &y, const pr_out<Y> &out, float *sums, hipStream_t st) {
     typedef PgTile<WI, WO, NI, NO> L;
     auto *k = k_product_grad<FMT, ALONG, WI, WO, NI, NO, Y, SUMS>;
-    if (hipFuncSetAttribute((const void *)k, hipFuncAttributeMaxDynamicSharedMemorySize, L::LDS) != hipSuccess) return PP_ERR_HIP;
     k<<<dim3(p.ni * p.no, p.splits), PR_THREADS, L::LDS, st>>>(p, x, y, out, sums);
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
 }

@@ -11,7 +11,7 @@ import ctypes
 import torch
 
 from . import binding
-from .binding import PPError, _check, _stream  # noqa: F401
+from .binding import PP_OK, PPError  # noqa: F401
 
 PP_TYPE_F32, PP_TYPE_F16, PP_TYPE_BF16 = 0, 1, 2
 PP_PACK_INT8, PP_PACK_FP4 = 0, 1
@@ -62,22 +62,37 @@ def packed_bytes(fmt, rows, cols):
     return rows * -(-cols // GROUP) * (_CODES[fmt][1] + 4)
 
 
+_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+
+
+def _stream():
+    """The current HIP stream of the current device (torch.cuda.current_stream() without its object, which takes 3 us to make)."""
+    return _raw_stream(_device())
+
+
+def _check(rc):
+    if rc != PP_OK:
+        raise PPError(rc)
+
+
 def _matrix(t, dtype, rows, cols, name):
     """(data pointer, row stride) of a matrix."""
-    if not t.is_cuda or t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if not t.is_cuda or t.dtype is not dtype or t.shape != (rows, cols):
         raise ValueError("%s must be a %s matrix of %d x %d on the GPU" % (name, dtype, rows, cols))
     ld, step = t.stride()
     if step != 1 and cols > 1 or ld < cols and rows > 1:
         raise ValueError("%s must have rows of consecutive values that do not overlap" % name)
-    return t.data_ptr(), max(ld, cols)
+    return t.data_ptr(), ld if ld > cols else cols
 
 
 def _first(t, name):
     """(type code, rows, cols, data pointer, row stride) of the matrix that sets a call's type and sizes."""
-    if t.dim() != 2 or t.dtype not in TYPES:
+    code, shape = TYPES.get(t.dtype), t.shape
+    if code is None or len(shape) != 2:
         raise ValueError("%s must be a matrix of float32, float16 or bfloat16" % name)
-    rows, cols = t.shape
-    return (TYPES[t.dtype], rows, cols) + _matrix(t, t.dtype, rows, cols, name)
+    rows, cols = shape
+    ptr, ld = _matrix(t, t.dtype, rows, cols, name)
+    return code, rows, cols, ptr, ld
 
 
 def _packed(pair, fmt, rows, cols, name):
@@ -86,9 +101,9 @@ def _packed(pair, fmt, rows, cols, name):
         return None, None
     codes, scales = pair
     dtype, width = _CODES[fmt]
-    groups = -(-cols // GROUP)
-    if (not codes.is_cuda or codes.dtype != dtype or codes.shape != (rows, groups, width) or not codes.is_contiguous()
-            or not scales.is_cuda or scales.dtype != torch.uint8 or scales.shape != (rows, groups, 4) or not scales.is_contiguous()):
+    groups = (cols + GROUP - 1) // GROUP
+    if (not codes.is_cuda or codes.dtype is not dtype or codes.shape != (rows, groups, width) or not codes.is_contiguous()
+            or not scales.is_cuda or scales.dtype is not torch.uint8 or scales.shape != (rows, groups, 4) or not scales.is_contiguous()):
         raise ValueError("%s must be codes %s [%d][%d][%d] and scales uint8 [%d][%d][4], contiguous on the GPU"
                          % (name, dtype, rows, groups, width, rows, groups))
     return codes.data_ptr(), scales.data_ptr()
