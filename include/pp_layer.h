@@ -88,8 +88,8 @@ int pp_act_backward(int kind, int type, int64_t rows, int64_t cols, const void *
 /*
  * The linear layer y = x W^T + b with its weight W [n_out][n_in] packed with PP_PACK_FP4.
  * pp_linear_workspace_bytes: bytes of workspace that the call of this kind needs (host function;
- * 0 if a size or the type is out of range).  The workspace must be 256-byte aligned; its contents
- * need not be kept.
+ * 0 if a size or the type is out of range).  What a type needs serves the types of fewer bits too.
+ * The workspace must be 256-byte aligned; its contents need not be kept.
  */
 #define PP_LINEAR_FORWARD 0
 #define PP_LINEAR_BACKWARD_INPUT 1

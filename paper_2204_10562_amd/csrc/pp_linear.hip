@@ -3,7 +3,9 @@
 #include "pp_product_fp4.h"
 #include "pp_product_grad.h"
 
-int pp_launch_pack(int format, int type, int64_t rows, int64_t cols, const void *src, int64_t ld, void *codes, void *scales, hipStream_t st);
+// x in 4 bits, and in 8 where codes8 is given, in one pass (pp_pack.hip)
+int pp_launch_pack_both(int type, int64_t rows, int64_t cols, const void *src, int64_t ld, void *codes4, void *scales4, void *codes8, void *scales8,
+                        hipStream_t st);
 
 // ---- gradients as bf16 planes
 
@@ -54,7 +56,21 @@ __global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const fl
         const long long o = t / chunks, i = (t - o * chunks) * 8;
         const float *q = p.partial + o * p.partial_ld + i;
         pp_f4 a = {0, 0, 0, 0}, b = a;
-        for (int s = 0; s < p.splits; ++s, q += p.outer * p.partial_ld) {
+        int s = 0;
+        for (; s + 4 <= p.splits; s += 4) {  // four pieces' loads in flight, added in their order
+            pp_f4 u[4], w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k, q += p.outer * p.partial_ld) {
+                u[k] = *(const pp_f4 *)q;
+                w[k] = *(const pp_f4 *)(q + 4);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                a += u[k];
+                b += w[k];
+            }
+        }
+        for (; s < p.splits; ++s, q += p.outer * p.partial_ld) {
             a += *(const pp_f4 *)q;
             b += *(const pp_f4 *)(q + 4);
         }
@@ -90,30 +106,33 @@ static int launch_join(int type, const pr_plan &p, void *out, long long ld, cons
 
 // ---- how work is divided
 
-// A tile shape: results, workgroups of it that a compute unit holds, microseconds of a step and of
-// a workgroup's start and end.
+// A tile shape: results; microseconds of a step where a compute unit has one workgroup of it and where
+// it has as many as fit; how many fit; microseconds of a workgroup's start and end.  Measured: one step of
+// the sum is 128 values forward and 64 in the backward products.
 struct pr_shape {
     int ti, to, fit;
-    float step, once;
+    float alone, full, once;
 };
-static const pr_shape SHAPES_FP4[] = {{256, 256, 1, 0.9f, 4.0f}, {128, 128, 2, 0.55f, 2.5f}, {256, 32, 2, 0.4f, 2.0f}};
-static const pr_shape SHAPES_GRAD[] = {{256, 256, 1, 1.5f, 4.0f}, {128, 128, 2, 0.9f, 2.5f}, {256, 32, 2, 0.8f, 2.0f}};
+static const pr_shape FORWARD[] = {{256, 256, 1, 1.0f, 1.0f, 12.0f}, {128, 128, 2, 0.34f, 0.62f, 6.0f}, {256, 32, 2, 0.28f, 0.5f, 5.0f}};
+static const pr_shape INPUT[] = {{256, 256, 1, 1.7f, 1.7f, 12.0f}, {128, 128, 2, 0.68f, 1.14f, 6.0f}, {256, 32, 2, 0.78f, 1.1f, 5.0f}};
+static const pr_shape WEIGHT[] = {{256, 256, 1, 1.8f, 1.8f, 20.0f}, {128, 128, 2, 0.9f, 1.4f, 8.0f}};
 #define PR_CUS 256
 
-// The shape and the number of pieces with the least estimated time: rounds of workgroups over the
-// chip, and for more than one piece the pass that adds them.
+// The shape and the number of pieces with the least estimated time: rounds of workgroups over the chip, and
+// for more than one piece the pass that adds them (a launch, and each partial sum written and read).
 static pr_plan plan(const pr_shape *shapes, int n, long long inner, long long outer, long long steps, int *shape) {
     pr_plan best = {};
     float least = 0;
     for (int k = 0; k < n; ++k) {
         const pr_shape &s = shapes[k];
-        const long long ni = (inner + s.ti - 1) / s.ti, no = (outer + s.to - 1) / s.to, tiles = ni * no;
-        for (int pieces = 1; pieces <= 32; ++pieces) {
-            const long long per = (steps + pieces - 1) / pieces;
+        const long long tiles = ((inner + s.ti - 1) / s.ti) * ((outer + s.to - 1) / s.to);
+        for (int pieces = 1; pieces <= 32 && pieces <= steps; ++pieces) {
+            const long long per = (steps + pieces - 1) / pieces, work = tiles * pieces;
             if (pieces > 1 && ((steps + per - 1) / per != pieces || tiles > PR_CUS * s.fit)) continue;
-            const float rounds = (float)((tiles * pieces + PR_CUS * s.fit - 1) / (PR_CUS * s.fit));
-            float t = rounds * ((float)per * s.step + s.once);
-            if (pieces > 1) t += 4.0f + (float)(pieces + 1) * (float)(inner * outer) * 4.0f / 3.0e6f;
+            const long long rounds = work / (PR_CUS * s.fit), rest = work - rounds * PR_CUS * s.fit;
+            float t = (float)rounds * ((float)per * s.full + s.once);
+            if (rest) t += (float)per * (rest > PR_CUS ? s.full : s.alone) + s.once;
+            if (pieces > 1) t += 4.0f + (float)pieces * (0.25f + (float)(inner * outer) * 8.0f / 1.0e7f);
             if (!best.splits || t < least) {
                 least = t;
                 *shape = k;
@@ -145,12 +164,12 @@ template <class F> static int in_turns(const pr_plan &p, int to, F launch) {
     return PP_OK;
 }
 
-static pr_plan plan_forward(int64_t rows, int64_t n_in, int64_t n_out, int *shape) { return plan(SHAPES_FP4, 3, n_out, rows, pp_groups(n_in), shape); }
+static pr_plan plan_forward(int64_t rows, int64_t n_in, int64_t n_out, int *shape) { return plan(FORWARD, 3, n_out, rows, pp_groups(n_in), shape); }
 static pr_plan plan_input(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(SHAPES_GRAD, 3, n_in, rows, planes_of(type) * ((n_out + 63) / 64), shape);
+    return plan(INPUT, 3, n_in, rows, planes_of(type) * ((n_out + 63) / 64), shape);
 }
 static pr_plan plan_weight(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(SHAPES_GRAD, 2, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), shape);
+    return plan(WEIGHT, 2, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), shape);
 }
 
 // ---- entry points
@@ -162,23 +181,45 @@ static bool bad_layer(int type, int64_t rows, int64_t n_in, int64_t n_out) {
 static int64_t planes_ld(int64_t n_out) { return (n_out + 7) & ~(int64_t)7; }
 static size_t planes_bytes(int type, int64_t rows, int64_t n_out) { return pp_align256((size_t)planes_of(type) * rows * planes_ld(n_out) * 2); }
 
+// What a call keeps in its workspace: places of its parts, and the whole.
+struct pr_room {
+    size_t scales, partial, sums, total;
+};
+static pr_room room_forward(const pr_plan *p, int64_t rows, int64_t n_in) {
+    pr_room r = {};
+    r.scales = pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4);
+    r.partial = r.scales + pp_align256((size_t)rows * pp_groups(n_in) * 4);
+    r.total = 256 + r.partial + (p ? pp_align256(partial_bytes(*p)) : 0);
+    return r;
+}
+static pr_room room_backward(const pr_plan &p, int type, int64_t rows, int64_t n_out, bool sums) {
+    pr_room r = {};
+    r.partial = planes_bytes(type, rows, n_out);
+    r.sums = r.partial + pp_align256(partial_bytes(p));
+    r.total = 256 + r.sums + (sums ? pp_align256((size_t)p.splits * n_out * 4) : 0);
+    return r;
+}
+
 extern "C" size_t pp_linear_workspace_bytes(int call, int type, int64_t rows, int64_t n_in, int64_t n_out) {
     if (call < PP_LINEAR_FORWARD || call > PP_LINEAR_BACKWARD_WEIGHT || bad_layer(type, rows, n_in, n_out)) return 0;
     int shape;
-    if (call == PP_LINEAR_FORWARD && rows <= R4_ROWS)
-        return 256 + pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4) + pp_align256((size_t)rows * pp_groups(n_in) * 4);
-    if (call == PP_LINEAR_FORWARD)
-        return 256 + pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4) + pp_align256((size_t)rows * pp_groups(n_in) * 4) +
-               pp_align256(partial_bytes(plan_forward(rows, n_in, n_out, &shape)));
-    if (call == PP_LINEAR_BACKWARD_INPUT)
-        return 256 + planes_bytes(type, rows, n_out) + pp_align256(partial_bytes(plan_input(type, rows, n_in, n_out, &shape)));
-    const pr_plan p = plan_weight(type, rows, n_in, n_out, &shape);
-    return 256 + planes_bytes(type, rows, n_out) + pp_align256(partial_bytes(p)) + pp_align256((size_t)p.splits * n_out * 4);
+    if (call == PP_LINEAR_FORWARD) {
+        if (rows <= R4_ROWS) return room_forward(NULL, rows, n_in).total;
+        const pr_plan p = plan_forward(rows, n_in, n_out, &shape);
+        return room_forward(&p, rows, n_in).total;
+    }
+    // what the types of as many bits or fewer need: the work may be divided otherwise for them
+    size_t most = 0;
+    for (int t = type; t <= PP_TYPE_BF16; ++t) {
+        const bool weight = call == PP_LINEAR_BACKWARD_WEIGHT;
+        const pr_plan p = weight ? plan_weight(t, rows, n_in, n_out, &shape) : plan_input(t, rows, n_in, n_out, &shape);
+        const size_t n = room_backward(p, t, rows, n_out, weight).total;
+        most = n > most ? n : most;
+    }
+    return most;
 }
 
-static int bad_workspace(int call, int type, int64_t rows, int64_t n_in, int64_t n_out, const void *ws, size_t bytes) {
-    return !ws || ((uintptr_t)ws & 255) || bytes < pp_linear_workspace_bytes(call, type, rows, n_in, n_out) ? PP_ERR_WORKSPACE : PP_OK;
-}
+static bool bad_workspace(const void *ws, size_t bytes, const pr_room &r) { return !ws || ((uintptr_t)ws & 255) || bytes < r.total; }
 
 extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n_out, const void *x, int64_t ld_x, const void *w_codes,
                                  const void *w_scales, const float *bias, void *y, int64_t ld_y, void *x_codes, void *x_scales,
@@ -187,24 +228,25 @@ extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n
     if (pp_bad_matrix(x, type, rows, n_in, ld_x) || pp_bad_matrix(y, type, rows, n_out, ld_y)) return PP_ERR_INVALID_ARG;
     if (pp_bad_packed(w_codes, w_scales, n_out) || ((uintptr_t)bias & 3)) return PP_ERR_INVALID_ARG;
     if ((x_codes || x_scales) && pp_bad_packed(x_codes, x_scales, rows)) return PP_ERR_INVALID_ARG;
-    if (int rc = bad_workspace(PP_LINEAR_FORWARD, type, rows, n_in, n_out, workspace, workspace_bytes)) return rc;
-    if (!rows) return PP_OK;
     hipStream_t st = (hipStream_t)stream;
-    const long long g = pp_groups(n_in);
-    uint8_t *codes = (uint8_t *)workspace, *scales = codes + pp_align256((size_t)rows * g * PP_GROUP_CODES4);
-    const p4_operands all = {(const uint8_t *)w_codes, (const uint8_t *)w_scales, codes, scales};
-    if (rows == 1) ld_x = n_in;
-    if (rows <= R4_ROWS && r4_fuses(rows, n_in, n_out))
-        return r4_launch(type, rows, n_in, n_out, x, ld_x, (uint8_t *)x_codes, (uint8_t *)x_scales, all, y, ld_y, bias, st);
-    if (x_codes)
-        if (int rc = pp_launch_pack(PP_PACK_INT8, type, rows, n_in, x, ld_x, x_codes, x_scales, st)) return rc;
-    if (int rc = pp_launch_pack(PP_PACK_FP4, type, rows, n_in, x, ld_x, codes, scales, st)) return rc;
-    if (rows <= R4_ROWS) return r4_launch(type, rows, n_in, n_out, x, ld_x, NULL, NULL, all, y, ld_y, bias, st);
+    const bool few = rows <= R4_ROWS;
     int shape;
-    pr_plan p = plan_forward(rows, n_in, n_out, &shape);
-    p.partial = (float *)(scales + pp_align256((size_t)rows * g * 4));
-    const int rc = in_turns(p, SHAPES_FP4[shape].to, [&](const pr_plan &q, long long o) {
-        return p4_launch(shape, type, q, p4_operands{(const uint8_t *)w_codes, (const uint8_t *)w_scales, codes + o * g * PP_GROUP_CODES4, scales + o * g * 4},
+    pr_plan p = {};
+    if (!few) p = plan_forward(rows, n_in, n_out, &shape);
+    const pr_room room = room_forward(few ? NULL : &p, rows, n_in);
+    if (bad_workspace(workspace, workspace_bytes, room)) return PP_ERR_WORKSPACE;
+    if (!rows) return PP_OK;
+    if (rows == 1) ld_x = n_in;
+    const long long g = pp_groups(n_in);
+    uint8_t *codes = (uint8_t *)workspace, *scales = codes + room.scales;
+    const p4_operands all = {(const uint8_t *)w_codes, (const uint8_t *)w_scales, codes, scales};
+    if (few && r4_fuses(rows, n_in, n_out))
+        return r4_launch(type, rows, n_in, n_out, x, ld_x, (uint8_t *)x_codes, (uint8_t *)x_scales, all, y, ld_y, bias, st);
+    if (int rc = pp_launch_pack_both(type, rows, n_in, x, ld_x, codes, scales, x_codes, x_scales, st)) return rc;
+    if (few) return r4_launch(type, rows, n_in, n_out, x, ld_x, NULL, NULL, all, y, ld_y, bias, st);
+    p.partial = (float *)((uint8_t *)workspace + room.partial);
+    const int rc = in_turns(p, FORWARD[shape].to, [&](const pr_plan &q, long long o) {
+        return p4_launch(shape, type, q, p4_operands{all.inner_codes, all.inner_scales, codes + o * g * PP_GROUP_CODES4, scales + o * g * 4},
                          (uint8_t *)y + o * ld_y * pp_type_size(type), ld_y, bias, st);
     });
     if (rc || p.splits == 1) return rc;
@@ -229,16 +271,17 @@ extern "C" int pp_linear_backward_input(int type, int64_t rows, int64_t n_in, in
     if (bad_layer(type, rows, n_in, n_out)) return PP_ERR_INVALID_ARG;
     if (pp_bad_matrix(dy, type, rows, n_out, ld_dy) || pp_bad_matrix(dx, type, rows, n_in, ld_dx)) return PP_ERR_INVALID_ARG;
     if (pp_bad_packed(w_codes, w_scales, n_out)) return PP_ERR_INVALID_ARG;
-    if (int rc = bad_workspace(PP_LINEAR_BACKWARD_INPUT, type, rows, n_in, n_out, workspace, workspace_bytes)) return rc;
+    int shape;
+    pr_plan p = plan_input(type, rows, n_in, n_out, &shape);
+    const pr_room room = room_backward(p, type, rows, n_out, false);
+    if (bad_workspace(workspace, workspace_bytes, room)) return PP_ERR_WORKSPACE;
     if (!rows) return PP_OK;
     hipStream_t st = (hipStream_t)stream;
     pg_outer y;
     if (int rc = outer_of(type, true, rows, n_out, dy, ld_dy, workspace, &y, st)) return rc;
-    int shape;
-    pr_plan p = plan_input(type, rows, n_in, n_out, &shape);
-    p.partial = (float *)((uint8_t *)workspace + planes_bytes(type, rows, n_out));
+    p.partial = (float *)((uint8_t *)workspace + room.partial);
     const pg_inner w = {(const uint8_t *)w_codes, (const uint8_t *)w_scales, n_out, pp_groups(n_in)};
-    const int rc = in_turns(p, SHAPES_GRAD[shape].to, [&](const pr_plan &q, long long o) {
+    const int rc = in_turns(p, INPUT[shape].to, [&](const pr_plan &q, long long o) {
         pg_outer part = y;
         part.p += o * y.ld * 2;
         part.rows = q.outer;
@@ -254,18 +297,17 @@ extern "C" int pp_linear_backward_weight(int type, int64_t rows, int64_t n_in, i
     if (bad_layer(type, rows, n_in, n_out)) return PP_ERR_INVALID_ARG;
     if (pp_bad_matrix(dy, type, rows, n_out, ld_dy) || pp_bad_packed(x_codes, x_scales, rows)) return PP_ERR_INVALID_ARG;
     if (pp_bad_matrix(dw, PP_TYPE_F32, n_out, n_in, ld_dw) || ((uintptr_t)dw_in & 3) || ((uintptr_t)db & 3)) return PP_ERR_INVALID_ARG;
-    if (int rc = bad_workspace(PP_LINEAR_BACKWARD_WEIGHT, type, rows, n_in, n_out, workspace, workspace_bytes)) return rc;
+    int shape;
+    pr_plan p = plan_weight(type, rows, n_in, n_out, &shape);
+    const pr_room room = room_backward(p, type, rows, n_out, true);
+    if (bad_workspace(workspace, workspace_bytes, room)) return PP_ERR_WORKSPACE;
     hipStream_t st = (hipStream_t)stream;
     pg_outer y;
     if (int rc = outer_of(type, false, rows, n_out, dy, ld_dy, workspace, &y, st)) return rc;
-    int shape;
-    pr_plan p = plan_weight(type, rows, n_in, n_out, &shape);
-    p.steps = y.planes * (int)(rows ? (rows + 63) / 64 : 1);
-    uint8_t *room = (uint8_t *)workspace + planes_bytes(type, rows, n_out);
-    p.partial = (float *)room;
-    float *part_sums = (float *)(room + pp_align256(partial_bytes(p)));
+    p.partial = (float *)((uint8_t *)workspace + room.partial);
+    float *part_sums = (float *)((uint8_t *)workspace + room.sums);
     const pg_inner x = {(const uint8_t *)x_codes, (const uint8_t *)x_scales, rows, pp_groups(n_in)};
-    const int rc = in_turns(p, SHAPES_GRAD[shape].to, [&](const pr_plan &q, long long o) {
+    const int rc = in_turns(p, WEIGHT[shape].to, [&](const pr_plan &q, long long o) {
         pg_outer part = y;
         part.p += o * 2;
         part.cols -= o;

@@ -8,7 +8,7 @@
 
 #include "pp_layer_common.h"
 
-#define PR_THREADS 256
+#define PR_PIN __builtin_amdgcn_sched_barrier(0)  // instructions stay on their side
 #define PR_STEP 64  // bytes of an operand row to a step: 128 values of 4 bits, 32 of 16
 
 typedef int pr_i8 __attribute__((ext_vector_type(8)));
@@ -71,6 +71,13 @@ __device__ __forceinline__ void pr_to_lds(pp_i4 buf, unsigned voff, unsigned sof
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                  ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(voff), "s"(buf), "s"(__builtin_amdgcn_readfirstlane(soff)) : "memory");
 }
+// The same in two halves, for between products: where to, and (an instruction later) the load.
+__device__ __forceinline__ void pr_aim(unsigned lds, int offset) {
+    asm volatile("s_add_u32 m0, %0, %1" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "n"(offset) : "scc");
+}
+__device__ __forceinline__ void pr_fire(pp_i4 buf, unsigned voff, unsigned soff) {
+    asm volatile("buffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(voff), "s"(buf), "s"(__builtin_amdgcn_readfirstlane(soff)) : "memory");
+}
 #define PR_WAIT(n) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory")
 
 // A barrier that leaves loads in flight: what a wave has read from LDS has arrived.
@@ -103,35 +110,39 @@ template <class Y, int WI> struct PrRows {
 #pragma unroll
         for (int i = 0; i < PpRaw<Y>::W; ++i) *(pp_u4 *)(room + at(row, col / VALUES + i)) = r.w[i];
     }
-    // rows o0.. of the result, columns i0..; `add` in the same places, where Y is float
-    static __device__ __forceinline__ void store(const uint8_t *room, int lane, typename Y::T *p, long long ld, long long o0, long long outer,
-                                                 long long i0, long long inner, const float *add, long long add_ld) {
-        const long long i = i0 + lane % UNITS * VALUES;
-#pragma unroll 4
-        for (int t = 0; t < 32 / ROWS; ++t) {
-            const int row = t * ROWS + lane / UNITS;
-            const long long o = o0 + row;
-            pp_u4 w = *(const pp_u4 *)(room + at(row, lane % UNITS));
-            if (o >= outer || i >= inner) continue;
-            typename Y::T *q = p + o * ld + i;
-            if (i + VALUES <= inner) {
-                if constexpr (SIZE == 4)
-                    if (add) {
-                        const pp_u4 d = ((const pp_any16<4> *)(add + o * add_ld + i))->v;
+    static const int TURNS = 32 / ROWS / 2;  // of half the rows
+    // What is added to 16 rows from o0 on, where Y is float: asked for before those in front of them are written.
+    // (What a row's end leaves over is not used.)
+    static __device__ __forceinline__ void fetch(pp_u4 *d, int lane, long long o0, long long outer, long long i0, long long inner, const float *add,
+                                                 long long add_ld) {
+        const auto b = pr_resource(add + o0 * add_ld + i0, o0 < outer ? (((outer - o0 < 16 ? outer - o0 : 16) - 1) * add_ld + inner - i0) * 4 : 0);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) w[j] = pp_bits(pp_bits(w[j]) + pp_bits(d[j]));
-                    }
-                ((pp_any16<SIZE> *)q)->v = w;
-            } else {
+        for (int t = 0; t < TURNS; ++t)
+            d[t] = __builtin_bit_cast(pp_u4, __builtin_amdgcn_raw_buffer_load_b128(b, (unsigned)((t * ROWS + lane / UNITS) * add_ld + lane % UNITS * 4) * 4, 0, 0));
+    }
+    // half h of the 32 rows in `room`, the result's rows o0.., columns i0..
+    static __device__ __forceinline__ void store(const uint8_t *room, int h, int lane, typename Y::T *p, long long ld, long long o0, long long outer,
+                                                 long long i0, long long inner, const pp_u4 *d) {
+        const long long i = i0 + lane % UNITS * VALUES;
+        typename Y::T *q = p + (o0 + lane / UNITS) * ld + i;
+        const bool all = o0 + 16 <= outer && i0 + 32 * WI <= inner;
+#pragma unroll
+        for (int t = 0; t < TURNS; ++t) {
+            const int row = t * ROWS + lane / UNITS;
+            pp_u4 w = *(const pp_u4 *)(room + at(16 * h + row, lane % UNITS));
+            if constexpr (SIZE == 4)
+                if (d) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = pp_bits(pp_bits(w[j]) + pp_bits(d[t][j]));
+                }
+            if (all || (o0 + row < outer && i + VALUES <= inner)) {
+                ((pp_any16<SIZE> *)(q + t * ROWS * ld))->v = w;
+            } else if (o0 + row < outer) {
                 typename Y::T v[VALUES];
                 __builtin_memcpy(v, &w, 16);
 #pragma unroll
                 for (int j = 0; j < VALUES; ++j)
-                    if (i + j < inner) {
-                        if constexpr (SIZE == 4)
-                            if (add) v[j] += add[o * add_ld + i + j];
-                        q[j] = v[j];
-                    }
+                    if (i + j < inner) q[t * ROWS * ld + j] = v[j];
             }
         }
     }
@@ -142,34 +153,55 @@ template <class Y, int WI, int WO, class ACC>
 __device__ __forceinline__ void pr_leave(const pr_plan &p, const pr_out<Y> &out, ACC &acc, uint8_t *room, int lane, long long i0, long long o0, int piece) {
     const int r = lane & 31, g = lane >> 5;
     const bool whole = p.splits == 1;
+    typedef PrRows<Y, WI> Rows;
+    typedef PrRows<PpF32, WI> Part;
+    const bool adding = Rows::SIZE == 4 && whole && out.add;
+    pp_u4 d[2][Rows::SIZE == 4 ? Rows::TURNS : 1];
+    if (adding) Rows::fetch(d[0], lane, o0, p.outer, i0, p.inner, out.add, out.add_ld);
 #pragma unroll
-    for (int j = 0; j < WO; ++j) {
+    for (int q = 0; q < 2 * WO; ++q) {
+        const int j = q >> 1, h = q & 1;
+        if (h == 0)
 #pragma unroll
-        for (int i = 0; i < WI; ++i) {
-            float v[16];
-            *(pr_f16 *)v = acc[i][j];
+            for (int i = 0; i < WI; ++i) {
+                float v[16];
+                *(pr_f16 *)v = acc[i][j];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int col = 32 * i + 16 * h + 8 * g;
-                if (!whole) {
-                    PrRows<PpF32, WI>::put(room, r, col, v + 8 * h);
-                    continue;
+                for (int e = 0; e < 2; ++e) {
+                    const int col = 32 * i + 16 * e + 8 * g;
+                    if (!whole) {
+                        Part::put(room, r, col, v + 8 * e);
+                        continue;
+                    }
+                    if (out.bias) {
+                        const PpRaw<PpF32> b = pp_load8<PpF32>(out.bias + i0 + col, p.inner - i0 - col);
+                        float w[8];
+                        pp_values<PpF32>(b, w);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[8 * e + k] += w[k];
+                    }
+                    Rows::put(room, r, col, v + 8 * e);
                 }
-                if (out.bias) {
-                    const PpRaw<PpF32> b = pp_load8<PpF32>(out.bias + i0 + col, p.inner - i0 - col);
-                    float w[8];
-                    pp_values<PpF32>(b, w);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) v[8 * h + k] += w[k];
-                }
-                PrRows<Y, WI>::put(room, r, col, v + 8 * h);
+                PR_PIN;
             }
-        }
-        if (whole)
-            PrRows<Y, WI>::store(room, lane, out.p, out.ld, o0 + 32 * j, p.outer, i0, p.inner, out.add, out.add_ld);
-        else
-            PrRows<PpF32, WI>::store(room, lane, p.partial + (long long)piece * p.outer * p.partial_ld, p.partial_ld, o0 + 32 * j, p.outer, i0, p.inner, NULL, 0);
+        // (loads wait for the stores before them: what is added next is asked for first)
+        if (adding && q + 1 < 2 * WO) Rows::fetch(d[(q + 1) & 1], lane, o0 + 16 * (q + 1), p.outer, i0, p.inner, out.add, out.add_ld);
+        if (whole) Rows::store(room, h, lane, out.p, out.ld, o0 + 16 * q, p.outer, i0, p.inner, adding ? d[q & 1] : NULL);
+        else Part::store(room, h, lane, p.partial + (long long)piece * p.outer * p.partial_ld, p.partial_ld, o0 + 16 * q, p.outer, i0, p.inner, NULL);
+        PR_PIN;
     }
+}
+
+// Sums start at zero, in their registers and settled there before the first product.
+template <int WI, int WO> __device__ __forceinline__ void pr_clear(pr_f16 (&acc)[WI][WO]) {
+#pragma unroll
+    for (int i = 0; i < WI; ++i)
+#pragma unroll
+        for (int j = 0; j < WO; ++j) {
+            acc[i][j] = pr_f16{};
+            asm volatile("" : "+a"(acc[i][j]));
+        }
+    asm volatile("s_nop 7" ::: "memory");
 }
 
 // Products are written in assembly because their results have to stay in their registers: where the
@@ -177,13 +209,11 @@ __device__ __forceinline__ void pr_leave(const pr_plan &p, const pr_out<Y> &out,
 // what else there is to do between them: a wave has a matrix unit to itself and issues in order, so
 // a product's 32 cycles leave room for seven other instructions, and what comes in a heap leaves the
 // unit idle.  What the compiler does not see has to be right as it stands: operands come from loads
-// (which it waits for), never from an instruction less than two ahead, and sums are read behind
+// (which it waits for), never from an instruction less than three ahead, and sums are read behind
 // pr_settle.
 __device__ __forceinline__ void pr_multiply(pr_f16 &acc, pr_bf8 a, pr_bf8 b) {
     asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(acc) : "v"(a), "v"(b));
 }
-#define PR_PIN __builtin_amdgcn_sched_barrier(0)  // instructions stay on their side
-
 // Behind a loop's last products (where s == end): the matrix units have written their results.  The
 // branch around the waits is in here so that it stays within the loop, before any use of a sum.
 __device__ __forceinline__ void pr_settle(int s, int end) {

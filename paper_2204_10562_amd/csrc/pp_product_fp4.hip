@@ -6,11 +6,11 @@
 // work on this one.
 #include "pp_product_fp4.h"
 
-// Of the four scales of a row's step, the lane's own of either half become the bytes 0 and 2.  The two
-// wait states are those from here to a product's operand.
+// Of the four scales of a row's step, the lane's own of either half become the bytes 0 and 2.  Three
+// wait states have to lie between this and a product that takes it.
 __device__ __forceinline__ int p4_own(int scales, int shift) {
     int v;
-    asm volatile("v_lshrrev_b32 %0, %1, %2\n\ts_nop 1" : "=v"(v) : "v"(shift), "v"(scales));
+    asm volatile("v_lshrrev_b32 %0, %1, %2" : "=v"(v) : "v"(shift), "v"(scales));
     return v;
 }
 
@@ -27,15 +27,15 @@ __device__ __forceinline__ int p4_turn(int row) { return (row >> 2) & 3; }
 
 // WI x WO fragments of 32 x 32 to a wave, NI x NO waves
 template <int WI, int WO, int NI, int NO> struct P4Tile {
-    static const int TI = 32 * WI * NI, TO = 32 * WO * NO;
+    static const int TI = 32 * WI * NI, TO = 32 * WO * NO, WAVES = NI * NO;
     static const int SI = TI * PR_STEP, SO = TO * PR_STEP;           // bytes of a stage
     static const int CI = TI * 16, CO = (TO < 64 ? 64 : TO) * 16;    // bytes of four steps' scales
-    static const int LDS = 3 * (SI + SO) + 2 * (CI + CO);
-    static const int LI = TI / 64, LO = TO < 64 ? 1 : TO / 64, LL = LI + LO;  // loads of a wave to a step
+    static const int LDS = 3 * (SI + SO) + 2 * (CI + CO) > WAVES * 4096 * WI ? 3 * (SI + SO) + 2 * (CI + CO) : WAVES * 4096 * WI;
+    static const int LI = TI / 16 / WAVES, LO = TO / 16 < WAVES ? 1 : TO / 16 / WAVES, LL = LI + LO;  // loads of a wave to a step
 };
 
 template <int WI, int WO, int NI, int NO, class Y>
-__global__ __launch_bounds__(PR_THREADS, 1) void k_product4(pr_plan p, p4_operands q, pr_out<Y> out) {
+__global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_operands q, pr_out<Y> out) {
     typedef P4Tile<WI, WO, NI, NO> L;
     extern __shared__ uint8_t sm[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -50,36 +50,47 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product4(pr_plan p, p4_operan
     const pp_i4 ci = pr_buffer(q.inner_scales + i0 * spitch, ri * spitch), co = pr_buffer(q.outer_scales + o0 * spitch, ro * spitch);
     const unsigned base = pr_lds_of(sm), scales = base + 3 * (L::SI + L::SO);
 
-    // where this lane's pieces come from: 16 rows of four pieces to a load
+    // where this lane's pieces come from: 16 rows of four pieces to a load, a wave's loads 1024 bytes of LDS apart
     unsigned vi[L::LI], vo[L::LO];
-    int li[L::LI], lo[L::LO];
 #pragma unroll
     for (int j = 0; j < L::LI; ++j) {
-        const int chunk = wave * L::LI + j, row = 16 * chunk + (lane >> 2);
+        const int row = 16 * (wave * L::LI + j) + (lane >> 2);
         vi[j] = (unsigned)(row * pitch) + 16 * ((lane & 3) ^ p4_turn(row));
-        li[j] = chunk * 1024;
     }
+    const int ochunk = wave * L::LO % (L::TO / 16);
 #pragma unroll
     for (int j = 0; j < L::LO; ++j) {
-        const int chunk = (wave * L::LO + j) % (L::TO / 16), row = 16 * chunk + (lane >> 2);
+        const int row = 16 * (ochunk + j) + (lane >> 2);
         vo[j] = (unsigned)(row * pitch) + 16 * ((lane & 3) ^ p4_turn(row));
-        lo[j] = chunk * 1024;
     }
+    const unsigned to_i = base + wave * L::LI * 1024, to_o = base + L::SI + ochunk * 1024;
     const int wi64 = wave % (L::TI / 64), wo64 = wave % (L::TO < 64 ? 1 : L::TO / 64);
     const unsigned vci = (unsigned)((64 * wi64 + lane) * spitch);
     const unsigned vco = L::TO < 64 && lane >= L::TO ? PR_BEYOND : (unsigned)((64 * wo64 + lane) * spitch);
 
-    // Load k of step s of this piece into stage `buf`.  They go out one by one between the products: a
-    // wave whose loads come all at once waits for room in their queue.
-    auto load = [&](int k, int s, unsigned buf) {
-        if (k == 0 && !(s & 3)) {
+    // The loads of a step of this piece into stage `buf`, in their order: at every fourth step the scales
+    // of four, then load k of the codes.  Behind the last step they find nothing (buffers of no bytes), so
+    // that there are always as many.  They go out one by one between the products: a wave whose loads
+    // come all at once waits for room in their queue.
+    auto load_scales = [&](int s) {
+        if (!(s & 3) && s < steps) {
             const unsigned c = scales + ((s >> 2) & 1) * (L::CI + L::CO);
             pr_to_lds(ci, vci, (unsigned)(s0 + s) * 4, c + wi64 * 1024);
             pr_to_lds(co, vco, (unsigned)(s0 + s) * 4, c + L::CI + wo64 * 1024);
         }
-        const unsigned b = base + buf * (L::SI + L::SO), at = (unsigned)(s0 + s) * PR_STEP;
-        if (k < L::LI) pr_to_lds(bi, vi[k], at, b + li[k]);
-        else pr_to_lds(bo, vo[k - L::LI], at, b + L::SI + lo[k - L::LI]);
+    };
+    auto aim = [&](int k, unsigned at) {
+        if (k < L::LI) pr_aim(to_i + at, k * 1024);
+        else pr_aim(to_o + at, (k - L::LI) * 1024);
+    };
+    pp_i4 ni = bi, no = bo;
+    auto open = [&](int s) {
+        ni[2] = s < steps ? bi[2] : 0;
+        no[2] = s < steps ? bo[2] : 0;
+    };
+    auto fire = [&](int k, int s) {
+        if (k < L::LI) pr_fire(ni, vi[k], (unsigned)(s0 + s) * PR_STEP);
+        else pr_fire(no, vo[k - L::LI], (unsigned)(s0 + s) * PR_STEP);
     };
 
     const int wi = wave % NI, wo = wave / NI, r = lane & 31, g = lane >> 5;
@@ -101,14 +112,19 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product4(pr_plan p, p4_operan
 #pragma unroll
         for (int j = 0; j < WO; ++j) out_raw[j] = *(const int *)(c + so + j * 512);
     };
-    pr_f16 acc[WI][WO] = {};
+    pr_f16 acc[WI][WO];
 
 #pragma unroll
-    for (int t = 0; t < 3; ++t)
-        if (t < steps) {
+    for (int t = 0; t < 3; ++t) {
+        load_scales(t);
+        open(t);
 #pragma unroll
-            for (int k = 0; k < L::LL; ++k) load(k, t, t);
+        for (int k = 0; k < L::LL; ++k) {
+            aim(k, t * (L::SI + L::SO));
+            asm volatile("s_nop 0");
+            fire(k, t);
         }
+    }
     PR_WAIT(0);
     pr_barrier();
 #pragma unroll
@@ -116,33 +132,50 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product4(pr_plan p, p4_operan
 #pragma unroll
     for (int j = 0; j < WO; ++j) first[j] = read(codes_at(0), fo0, j);
     read_scales(scales_at(0));
+    pr_clear(acc);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the compiler need not wait for these within the loop
     constexpr int N = WI * WO, MEET = WO;  // products of a half step; those of the second one before the waves meet
-    int b0 = 0, b1 = 1, b2 = 2;                       // the stages of steps s, s + 1 and s + 2
+    constexpr int SLOTS = 2 * N - MEET;    // products from one meeting to the next: step s + 3's loads go out behind them, into step s's stage
+    int b0 = 0, b1 = 1, b2 = 2;            // the stages of steps s, s + 1 and s + 2
+    int sent = 2;                          // the last step whose loads went out or are going out
+    unsigned sent_at = 2 * (L::SI + L::SO);
     for (int s = 0; s < steps; ++s) {
         const uint8_t *now = codes_at(b0), *next = codes_at(b1);  // after the last step: what lies there, for nothing
+        // what follows product m, counted from the meeting of the step before
+        auto behind = [&](int m) {
+#pragma unroll
+            for (int k = m * L::LL / SLOTS; k < (m + 1) * L::LL / SLOTS; ++k) {
+                if (k > m * L::LL / SLOTS) asm volatile("s_nop 0");
+                fire(k, sent);
+                if (k + 1 < L::LL) aim(k + 1, sent_at);
+            }
+        };
         in_c[0] = p4_own(in_raw[0], shift);
+        out_c[0] = p4_own(out_raw[0], shift);
+        asm volatile("s_nop 3");
 #pragma unroll
         for (int m = 0; m < N; ++m) {
             const int i = m / WO, j = m % WO;
-            if (i == 0) out_c[j] = p4_own(out_raw[j], shift);
             p4_multiply<0>(acc[i][j], in[i], in_c[i], first[j], out_c[j]);
-            if (j == 0 && i + 1 < WI) in_c[i + 1] = p4_own(in_raw[i + 1], shift);
+            if (i == 0 && j + 1 < WO) out_c[j + 1] = p4_own(out_raw[j + 1], shift);
+            if (j == WO - 1 && i + 1 < WI) in_c[i + 1] = p4_own(in_raw[i + 1], shift);
             if (i == 0) late[j] = read(now, fo1, j);
             if (j == WO - 1) in[i] = read(now, fi1, i);
-            if (s + 2 < steps && s > 0) {  // the second half of step s + 2's loads
-#pragma unroll
-                for (int k = L::LL / 2 + m * (L::LL - L::LL / 2) / N; k < L::LL / 2 + (m + 1) * (L::LL - L::LL / 2) / N; ++k) load(k, s + 2, b2);
-            }
+            if (s > 0) behind(N - MEET + m);
+            if (i == 0 || j == WO - 1) asm volatile("s_nop 2");
             PR_PIN;
         }
 #pragma unroll
         for (int m = 0; m < N; ++m) {
             const int i = m / WO, j = m % WO;
             if (m == MEET) {  // step s + 1 has arrived for every wave, and every wave has read all of step s
-                if (s + 2 < steps) PR_WAIT(L::LL);
-                else PR_WAIT(0);
+                PR_WAIT(L::LL);
                 pr_barrier();
+                sent = s + 3;
+                sent_at = b0 * (L::SI + L::SO);
+                open(sent);
+                load_scales(sent);
+                aim(0, sent_at);
             }
             p4_multiply<1>(acc[i][j], in[i], in_c[i], late[j], out_c[j]);
             if (m >= MEET) {
@@ -150,10 +183,7 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product4(pr_plan p, p4_operan
                 if (m == MEET) in[0] = read(next, fi0, 0);
                 if (m == (MEET + N) / 2) read_scales(scales_at(s + 1));
                 if (j == WO - 1) in[i] = read(next, fi0, i);
-                if (s + 3 < steps) {
-#pragma unroll
-                    for (int k = (m - MEET) * (L::LL / 2) / (N - MEET); k < (m + 1 - MEET) * (L::LL / 2) / (N - MEET); ++k) load(k, s + 3, b0);
-                }
+                behind(m - MEET);
             }
             PR_PIN;
         }
@@ -163,6 +193,7 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product4(pr_plan p, p4_operan
         b2 = t;
         pr_settle(s + 1, steps);
     }
+    PR_WAIT(0);  // nothing is on its way to LDS any more
     pr_barrier();
     pr_leave<Y, WI, WO>(p, out, acc, sm + wave * (32 * 32 * WI * 4), lane, i0 + wi * WI * 32, o0 + wo * WO * 32, piece);
 }
@@ -314,7 +345,7 @@ template <int WI, int WO, int NI, int NO> static int launch4(int type, pr_plan p
     return pp_by_type(type, [&](auto t) {
         typedef decltype(t) Y;
         auto *k = k_product4<WI, WO, NI, NO, Y>;
-        k<<<dim3(p.ni * p.no, p.splits), PR_THREADS, L::LDS, st>>>(p, q, pr_out<Y>{(typename Y::T *)y, ld, bias, NULL, 0});
+        k<<<dim3(p.ni * p.no, p.splits), 64 * L::WAVES, L::LDS, st>>>(p, q, pr_out<Y>{(typename Y::T *)y, ld, bias, NULL, 0});
         return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
     });
 }

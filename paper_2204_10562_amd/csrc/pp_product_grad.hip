@@ -9,9 +9,9 @@
 
 // WI x WO fragments of 32 x 32 to a wave, NI x NO waves
 template <int WI, int WO, int NI, int NO> struct PgTile {
-    static const int TI = 32 * WI * NI, TO = 32 * WO * NO;
+    static const int TI = 32 * WI * NI, TO = 32 * WO * NO, WAVES = NI * NO;
     static const int SI = TI * 128, SO = TO * 128;  // bytes of a stage: 64 values of the sum
-    static const int LDS = 2 * (SI + SO);
+    static const int LDS = 2 * (SI + SO) > WAVES * 4096 * WI ? 2 * (SI + SO) : WAVES * 4096 * WI;
 };
 
 // 32-byte units of a row of the sum are swapped by this (an exclusive or), so that the 16 rows which
@@ -52,12 +52,12 @@ template <int FMT> struct PgUnit {  // of a block
 };
 
 template <int FMT, bool ALONG, int WI, int WO, int NI, int NO, class Y, bool SUMS>
-__global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_inner x, pg_outer y, pr_out<Y> out, float *sums) {
+__global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_inner x, pg_outer y, pr_out<Y> out, float *sums) {
     typedef PgTile<WI, WO, NI, NO> L;
     constexpr int CB = FMT == PP_PACK_INT8 ? 16 : 8;  // bytes of sixteen codes
-    constexpr int PER_ROW = L::TI / 16, ROWS = PR_THREADS / PER_ROW, PIECES = 64 / ROWS;  // sixteen codes to a thread, PIECES times
+    constexpr int PER_ROW = L::TI / 16, ROWS = 64 * L::WAVES / PER_ROW, PIECES = 64 / ROWS;  // sixteen codes to a thread, PIECES times
     constexpr int RI = L::TI * 2, RO = L::TO * 2;     // bytes of a row of the sum
-    constexpr int LO = L::SO / 4096 ? L::SO / 4096 : 1;  // loads of a wave for the outer operand
+    constexpr int LO = L::SO / 1024 / L::WAVES ? L::SO / 1024 / L::WAVES : 1;  // loads of a wave for the outer operand
     constexpr int TURN_O = L::TO / 16 < 8 ? L::TO / 16 - 1 : 7;
     extern __shared__ uint8_t sm[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -81,11 +81,17 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
     }
     pp_u4 raw[PIECES];
     unsigned char scale[PIECES];
-    __amdgpu_buffer_rsrc_t xb, xsb;  // of the step whose codes are loaded next
-    auto aim_inner = [&](int s) {
-        const long long c0 = (long long)((s0 + s) % per_plane) * 64;
-        xb = pr_resource(x.codes + c0 * xpitch, (x.rows - c0) * xpitch);
-        xsb = pr_resource(x.scales + c0 * spitch, (x.rows - c0) * spitch);
+    // The operand from the step on that is loaded next; behind the last step loads find nothing.
+    __amdgpu_buffer_rsrc_t xb, xsb;
+    int xi = s0 % per_plane;
+    long long xat = (long long)xi * 64, xleft = x.rows - xat;  // its first row, and the rows from there on
+    auto next_inner = [&](bool some) {
+        xb = pr_resource(x.codes + xat * xpitch, some ? xleft * xpitch : 0);
+        xsb = pr_resource(x.scales + xat * spitch, some ? xleft * spitch : 0);
+        const bool wrap = ++xi == per_plane;
+        xi = wrap ? 0 : xi;
+        xat = wrap ? 0 : xat + 64;
+        xleft = wrap ? x.rows : xleft - 64;
     };
     auto load_inner = [&](int j) {
         if constexpr (FMT == PP_PACK_INT8) {
@@ -112,11 +118,11 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
 
     // the gradients: 1024 bytes of a stage to a load of a wave
     unsigned vo[LO];
-    int lo[LO], col_o[LO];
+    int col_o[LO];
+    const int chunk = (wave * LO) % (L::SO / 1024);
 #pragma unroll
     for (int j = 0; j < LO; ++j) {
-        const int at = ((wave * LO + j) * 1024) % L::SO, b = at + lane * 16;  // byte of the stage
-        lo[j] = at;
+        const int b = (chunk + j) * 1024 + lane * 16;  // byte of the stage
         if constexpr (ALONG) {
             const int row = b >> 7, unit = ((b >> 4) & 7) ^ ((row >> 1) & 7);
             col_o[j] = unit * 8;
@@ -127,24 +133,30 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
             vo[j] = (unsigned)(row * y.ld * 2) + unit * 32 + (b & 16);
         }
     }
-    pp_i4 ob;             // of the step whose gradients are loaded next
-    long long left = 1 << 30;  // columns of it that there are
-    auto aim_outer = [&](int s) {
-        const int plane = (s0 + s) / per_plane;
-        const long long c0 = (long long)(s0 + s - plane * per_plane) * 64;
-        const uint8_t *q = y.p + plane * y.plane * 2;
-        if constexpr (ALONG) {
-            const long long rows = y.rows - o0 < L::TO ? y.rows - o0 : L::TO;
-            left = y.cols - c0;
-            ob = pr_buffer(q + (o0 * y.ld + c0) * 2, ((rows - 1) * y.ld + left) * 2);
-        } else {
-            // up to the end of the last value's four bytes: less than four count as beyond the buffer
-            ob = pr_buffer(q + (c0 * y.ld + o0) * 2, c0 < y.rows ? (((y.rows - c0 - 1) * y.ld + y.cols - o0) * 2 + 3) & ~3ll : 0);
-        }
+    const unsigned to_o = base + L::SI + chunk * 1024;
+    // From the step on that is loaded next: address, bytes to the operand's end, and columns.  (Across the
+    // rows up to the end of the last value's four bytes: less than four count as beyond the buffer.)
+    const int per_step = ALONG ? 128 : (int)(y.ld * 128);
+    const long long orows = y.rows - o0 < L::TO ? y.rows - o0 : L::TO;
+    const uint8_t *const ofirst = y.p + (ALONG ? o0 * y.ld : o0) * 2;
+    const long long obytes = ALONG ? ((orows - 1) * y.ld + y.cols) * 2 : (((y.rows - 1) * y.ld + y.cols - o0) * 2 + 3) & ~3ll;
+    int oi = s0 % per_plane;
+    const uint8_t *oplane = ofirst + (s0 / per_plane) * y.plane * 2, *oat = oplane + (long long)oi * per_step;
+    long long oleft = obytes - (long long)oi * per_step;
+    pp_i4 ob;
+    int ocols;
+    auto next_outer = [&](bool some) {
+        ob = pr_buffer(oat, some ? oleft : 0);
+        const long long c = y.cols - 64ll * oi;
+        ocols = c < 64 ? (int)c : 64;
+        const bool wrap = ++oi == per_plane;
+        oi = wrap ? 0 : oi;
+        oplane = wrap ? oplane + y.plane * 2 : oplane;
+        oat = wrap ? oplane : oat + per_step;
+        oleft = wrap ? obytes : oleft - per_step;
     };
-    auto load_outer = [&](int j, int s) {
-        pr_to_lds(ob, ALONG && col_o[j] >= left ? PR_BEYOND : vo[j], 0, base + (s & 1) * (L::SI + L::SO) + L::SI + lo[j]);
-    };
+    auto aim = [&](int j, int s) { pr_aim(to_o + (s & 1) * (L::SI + L::SO), j * 1024); };
+    auto fire = [&](int j) { pr_fire(ob, ALONG && col_o[j] >= ocols ? PR_BEYOND : vo[j], 0); };
 
     // fragments: inner ones transposed, outer ones where the sum runs across their rows.  A quarter of
     // a step is 16 values of the sum, eight to a half of the lanes.
@@ -167,7 +179,7 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
         else return pg_read_t(b + ao[j] + k * 16 * RO, 4 * RO);
     };
     pr_bf8 in[WI], outer[2][WO];  // the inner fragments are replaced as they have been used, the outer ones of odd quarters have places of their own
-    pr_f16 acc[WI][WO] = {}, acc_s[SUMS ? WO : 1] = {};
+    pr_f16 acc[WI][WO], acc_s[SUMS ? WO : 1] = {};
     const bool summing = SUMS && ti == 0 && wi == 0;
     const pr_bf8 ones = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
     // The columns' sums, a product with ones: in ordinary registers (the others are full), and waited
@@ -175,7 +187,7 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
     auto add_up = [&](const pr_bf8 *f) {
         if constexpr (SUMS) {
 #pragma unroll
-            for (int j = 0; j < WO; ++j) asm volatile("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc_s[j]) : "v"(ones), "v"(f[j]));
+            for (int j = 0; j < WO; ++j) asm volatile("s_nop 3\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc_s[j]) : "v"(ones), "v"(f[j]));
             asm volatile("s_nop 15\n\ts_nop 3" : "+v"(acc_s[0]));
 #pragma unroll
             for (int j = 1; j < WO; ++j) asm volatile("" : "+v"(acc_s[j]));
@@ -184,29 +196,46 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
 
     constexpr int N = WI * WO, MEET = WO;  // products of a quarter step; those of the last one before the waves meet
     constexpr int PARTS = 8 * PIECES;
-    aim_outer(0);
-    aim_inner(0);
-#pragma unroll
-    for (int j = 0; j < LO; ++j) load_outer(j, 0);
+    // Step s + 2's gradients are asked for in the SLOTS products behind a meeting; step s + 1's packed values
+    // turned from product TURN to TURN_END of a step on.  (Waiting for a packed value the compiler, which does
+    // not know of the gradients, waits for those of them that were asked for later too: they have to be old.)
+    // Turned in the second and third quarters instead, dx = dy W4 takes 830 us where this takes 764 (8192 rows,
+    // 16384 -> 4096, all zeros); the many instructions of 8 bits are better spread: 950, and 967 in the third alone.
+    constexpr int SLOTS = N - MEET, TURN = FMT == PP_PACK_INT8 ? 3 * N / 2 : 2 * N, TURN_END = 3 * N;
+    next_inner(true);
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) load_inner(j);
 #pragma unroll
-    for (int t = 0; t < PARTS; ++t) turn_inner(t, 0);
-    PR_WAIT(0);
-    if (steps > 1) {
-        aim_outer(1);
-        aim_inner(1);
+    for (int t = 0; t < 2; ++t) {
+        next_outer(t < steps);
 #pragma unroll
-        for (int j = 0; j < LO; ++j) load_outer(j, 1);
-#pragma unroll
-        for (int j = 0; j < PIECES; ++j) load_inner(j);
+        for (int j = 0; j < LO; ++j) {
+            aim(j, t);
+            asm volatile("s_nop 0");
+            fire(j);
+        }
     }
+#pragma unroll
+    for (int t = 0; t < PARTS; ++t) turn_inner(t, 0);
+    next_inner(steps > 1);
+#pragma unroll
+    for (int j = 0; j < PIECES; ++j) load_inner(j);
+    PR_WAIT(2 * PIECES);
     pr_barrier();
 #pragma unroll
     for (int j = 0; j < WI; ++j) in[j] = read_i(sm, 0, j);
 #pragma unroll
     for (int j = 0; j < WO; ++j) outer[0][j] = read_o(sm, 0, j);
+    pr_clear(acc);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the compiler need not wait for these within the loop
+    auto behind = [&](int m, int stage) {  // what goes out behind product m from a meeting on
+#pragma unroll
+        for (int j = m * LO / SLOTS; j < (m + 1) * LO / SLOTS; ++j) {
+            if (j > m * LO / SLOTS) asm volatile("s_nop 0");
+            fire(j);
+            if (j + 1 < LO) aim(j + 1, stage);
+        }
+    };
     for (int s = 0; s < steps; ++s) {
         const uint8_t *now = sm + (s & 1) * (L::SI + L::SO), *next = sm + ((s + 1) & 1) * (L::SI + L::SO);
 #pragma unroll
@@ -214,14 +243,15 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
             const pr_bf8 *o = outer[k & 1];
             const uint8_t *b = k < 3 ? now : next;  // after the last step: what lies there, for nothing
             if (SUMS && summing) add_up(o);
-            if (k == 1) aim_inner(s + 2 < steps ? s + 2 : s);
+            if (k == TURN / N) next_inner(s + 2 < steps);
 #pragma unroll
             for (int m = 0; m < N; ++m) {
                 const int i = m / WO, j = m % WO;
                 if (k == 3 && m == MEET) {  // step s + 1 is there, and every wave has read all of step s
                     PR_WAIT(2 * PIECES);    // (but for the packed values of the step after it)
                     pr_barrier();
-                    aim_outer(s + 2);
+                    next_outer(s + 2 < steps);
+                    aim(0, s);
                 }
                 pr_multiply(acc[i][j], in[i], o[j]);
                 if (k < 3) {
@@ -232,18 +262,15 @@ __global__ __launch_bounds__(PR_THREADS, 1) void k_product_grad(pr_plan p, pg_in
                     if (m == MEET) in[0] = read_i(b, 0, 0);
                     if (j == WO - 1) in[i] = read_i(b, 0, i);
                 }
-                if (k == 1 || k == 2) {
-                    const int slot = (k - 1) * N + m;
+                if (k * N + m >= TURN && k * N + m < TURN_END) {
+                    const int slot = k * N + m - TURN;
 #pragma unroll
-                    for (int t = slot * PARTS / (2 * N); t < (slot + 1) * PARTS / (2 * N); ++t) {
+                    for (int t = slot * PARTS / (TURN_END - TURN); t < (slot + 1) * PARTS / (TURN_END - TURN); ++t) {
                         turn_inner(t, s + 1);
                         if ((t & 7) == 7) load_inner(t >> 3);  // step s + 2's: a whole step ahead
                     }
                 }
-                if (k == 3 && m >= MEET && s + 2 < steps) {
-#pragma unroll
-                    for (int l = (m - MEET) * LO / (N - MEET); l < (m + 1 - MEET) * LO / (N - MEET); ++l) load_outer(l, s + 2);
-                }
+                if (k == 3 && m >= MEET) behind(m - MEET, s);
                 PR_PIN;
             }
         }
@@ -266,7 +293,7 @@ template <int FMT, bool ALONG, int WI, int WO, int NI, int NO, class Y, bool SUM
 static int launch_one(const pr_plan &p, const pg_inner &x, const pg_outer &y, const pr_out<Y> &out, float *sums, hipStream_t st) {
     typedef PgTile<WI, WO, NI, NO> L;
     auto *k = k_product_grad<FMT, ALONG, WI, WO, NI, NO, Y, SUMS>;
-    k<<<dim3(p.ni * p.no, p.splits), PR_THREADS, L::LDS, st>>>(p, x, y, out, sums);
+    k<<<dim3(p.ni * p.no, p.splits), 64 * L::WAVES, L::LDS, st>>>(p, x, y, out, sums);
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
 }
 
@@ -285,12 +312,12 @@ static int launch_weight(const pr_plan &p, const pg_inner &x, const pg_outer &y,
 }
 
 int pg_launch_input(int shape, int type, const pr_plan &p, const pg_inner &w, const pg_outer &dy, void *dx, long long ld, hipStream_t st) {
-    if (shape == 0) return launch_input<4, 4, 2, 2>(type, p, w, dy, dx, ld, st);
+    if (shape == 0) return launch_input<4, 2, 2, 4>(type, p, w, dy, dx, ld, st);
     if (shape == 1) return launch_input<2, 2, 2, 2>(type, p, w, dy, dx, ld, st);
     return launch_input<2, 1, 4, 1>(type, p, w, dy, dx, ld, st);
 }
 
 int pg_launch_weight(int shape, const pr_plan &p, const pg_inner &x, const pg_outer &dy, float *dw, long long ld, const float *add, float *sums, hipStream_t st) {
-    if (shape == 0) return launch_weight<4, 4, 2, 2>(p, x, dy, dw, ld, add, sums, st);
+    if (shape == 0) return launch_weight<4, 2, 2, 4>(p, x, dy, dw, ld, add, sums, st);
     return launch_weight<2, 2, 2, 2>(p, x, dy, dw, ld, add, sums, st);
 }
