@@ -24,16 +24,13 @@ __device__ __forceinline__ pr_bf8 pg_read_t(const uint8_t *p, int second) {  // 
     return __builtin_bit_cast(pr_bf8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Two packed values, the w-th of a piece of sixteen, as bf16: exact, NaN where the block is.
-template <int FMT> struct PgUnit {  // of a block
+// Two packed values, the w-th of a piece of sixteen, as bf16: exact, and NaN where the block is (products
+// with a unit that is NaN are, and so are conversions of 4 bits).
+template <int FMT> struct PgUnit {
     float unit;
-    unsigned nan;
     __device__ __forceinline__ void set(unsigned byte) {
-        if constexpr (FMT == PP_PACK_INT8) unit = pp_unit8(byte);
-        else {
-            unit = pp_unit4(byte == 255 ? 0 : byte);
-            nan = byte == 255 ? 0x7fc07fc0u : 0;
-        }
+        unit = __builtin_amdgcn_ldexpf(1.0f, (int)byte - (FMT == PP_PACK_INT8 ? 133 : 127));
+        unit = byte == 255 ? pp_bits(0x7fc00000u) : unit;
     }
     __device__ __forceinline__ unsigned two(pp_u4 raw, int w) const {
         if constexpr (FMT == PP_PACK_INT8) {
@@ -47,7 +44,7 @@ template <int FMT> struct PgUnit {  // of a block
         else if ((w & 3) == 1) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 1);
         else if ((w & 3) == 2) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 2);
         else v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, unit, 3);
-        return __builtin_bit_cast(unsigned, v) | nan;
+        return __builtin_bit_cast(unsigned, v);
     }
 };
 
@@ -81,17 +78,20 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     }
     pp_u4 raw[PIECES];
     unsigned char scale[PIECES];
-    // The operand from the step on that is loaded next; behind the last step loads find nothing.
+    // The rows of the step that is loaded next; behind the last step loads find nothing.  (64 rows are less
+    // than 2^29 bytes.)
     __amdgpu_buffer_rsrc_t xb, xsb;
-    int xi = s0 % per_plane;
-    long long xat = (long long)xi * 64, xleft = x.rows - xat;  // its first row, and the rows from there on
+    int xi = s0 % per_plane, xleft = (int)x.rows - xi * 64;  // its number in its plane, the rows from there on
+    const uint8_t *xat = x.codes + (long long)xi * 64 * xpitch, *xsat = x.scales + (long long)xi * 64 * spitch;
     auto next_inner = [&](bool some) {
-        xb = pr_resource(x.codes + xat * xpitch, some ? xleft * xpitch : 0);
-        xsb = pr_resource(x.scales + xat * spitch, some ? xleft * spitch : 0);
+        const int n = !some || xleft < 0 ? 0 : xleft < 64 ? xleft : 64;
+        xb = __builtin_amdgcn_make_buffer_rsrc((void *)xat, 0, n * (int)xpitch, 0x00027000);
+        xsb = __builtin_amdgcn_make_buffer_rsrc((void *)xsat, 0, n * (int)spitch, 0x00027000);
         const bool wrap = ++xi == per_plane;
         xi = wrap ? 0 : xi;
-        xat = wrap ? 0 : xat + 64;
-        xleft = wrap ? x.rows : xleft - 64;
+        xat = wrap ? x.codes : xat + 64 * xpitch;
+        xsat = wrap ? x.scales : xsat + 64 * spitch;
+        xleft = wrap ? (int)x.rows : xleft - 64;
     };
     auto load_inner = [&](int j) {
         if constexpr (FMT == PP_PACK_INT8) {
@@ -134,26 +134,33 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
         }
     }
     const unsigned to_o = base + L::SI + chunk * 1024;
-    // From the step on that is loaded next: address, bytes to the operand's end, and columns.  (Across the
-    // rows up to the end of the last value's four bytes: less than four count as beyond the buffer.)
+    // From the step on that is loaded next: address, and bytes that it may use (less than 2^32).  (Across
+    // the rows up to the end of the last value's four bytes: less than four count as beyond the buffer.)
     const int per_step = ALONG ? 128 : (int)(y.ld * 128);
-    const long long orows = y.rows - o0 < L::TO ? y.rows - o0 : L::TO;
-    const uint8_t *const ofirst = y.p + (ALONG ? o0 * y.ld : o0) * 2;
-    const long long obytes = ALONG ? ((orows - 1) * y.ld + y.cols) * 2 : (((y.rows - 1) * y.ld + y.cols - o0) * 2 + 3) & ~3ll;
+    const int orows = y.rows - o0 < L::TO ? (int)(y.rows - o0) : L::TO, row_bytes = (int)(y.cols - (ALONG ? 0 : o0)) * 2;
+    const uint8_t *oplane = y.p + (ALONG ? o0 * y.ld : o0) * 2 + (s0 / per_plane) * y.plane * 2;
     int oi = s0 % per_plane;
-    const uint8_t *oplane = ofirst + (s0 / per_plane) * y.plane * 2, *oat = oplane + (long long)oi * per_step;
-    long long oleft = obytes - (long long)oi * per_step;
+    const uint8_t *oat = oplane + (long long)oi * per_step;
     pp_i4 ob;
     int ocols;
     auto next_outer = [&](bool some) {
-        ob = pr_buffer(oat, some ? oleft : 0);
-        const long long c = y.cols - 64ll * oi;
-        ocols = c < 64 ? (int)c : 64;
+        unsigned bytes;
+        if constexpr (ALONG) {
+            ocols = (int)y.cols - 64 * oi;
+            bytes = (unsigned)((orows - 1) * (int)y.ld) * 2 + ocols * 2;
+        } else {
+            const int left = (int)y.rows - 64 * oi, n = left < 64 ? left : 64;
+            bytes = n <= 0 ? 0 : (((unsigned)(n - 1) * (unsigned)y.ld) * 2 + row_bytes + 3) & ~3u;
+        }
+        const unsigned long long at = (unsigned long long)oat;
+        ob[0] = __builtin_amdgcn_readfirstlane((int)at);
+        ob[1] = __builtin_amdgcn_readfirstlane((int)(at >> 32) & 0xffff);
+        ob[2] = __builtin_amdgcn_readfirstlane(some ? (int)bytes : 0);
+        ob[3] = 0x00027000;
         const bool wrap = ++oi == per_plane;
         oi = wrap ? 0 : oi;
         oplane = wrap ? oplane + y.plane * 2 : oplane;
         oat = wrap ? oplane : oat + per_step;
-        oleft = wrap ? obytes : oleft - per_step;
     };
     auto aim = [&](int j, int s) { pr_aim(to_o + (s & 1) * (L::SI + L::SO), j * 1024); };
     auto fire = [&](int j) { pr_fire(ob, ALONG && col_o[j] >= ocols ? PR_BEYOND : vo[j], 0); };
