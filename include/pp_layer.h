@@ -54,6 +54,7 @@ extern "C" {
 
 #define PP_LAYER_MAX_ROWS (1 << 30)
 #define PP_LAYER_MAX_COLS (1 << 22)
+#define PP_LAYER_MAX_LD_DW (1 << 24)
 
 /* src [rows][cols] -> packed. */
 int pp_pack(int format, int type, int64_t rows, int64_t cols, const void *src, int64_t ld_src, void *codes,
@@ -113,7 +114,7 @@ int pp_linear_backward_input(int type, int64_t rows, int64_t n_in, int64_t n_out
 /*
  * dw = dw_in + dy^T xk, db = sum over the rows of dy, with xk the kept x (PP_PACK_INT8).
  *   dy [rows][n_out] of `type`; dw_in, dw float [n_out][n_in] with rows ld_dw apart
- *   dw_in   NULL = zero; may be dw
+ *   dw_in   NULL = zero; may be dw (rows of both at most PP_LAYER_MAX_LD_DW apart)
  *   db      float [n_out], or NULL = not wanted
  * With rows = 0, dw = dw_in and db = 0.
  */

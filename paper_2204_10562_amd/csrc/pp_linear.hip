@@ -253,10 +253,11 @@ extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n
     return launch_join(type, p, y, ld_y, bias, NULL, NULL, NULL, st);
 }
 
-// dy as the products take it: as it is where it can be loaded so, else copied into `room`.
+// dy as the products take it: as it is where it can be loaded so, else copied into `room`.  (As it is: bf16,
+// rows at multiples of 16 bytes, and so near each other that 256 of them are within the reach of 32-bit offsets.)
 static int outer_of(int type, bool along_sum, int64_t rows, int64_t cols, const void *dy, int64_t ld, void *room, pg_outer *out, hipStream_t st) {
     if (rows < 2) ld = cols;
-    if (type == PP_TYPE_BF16 && !((uintptr_t)dy & 15) && (rows < 2 || !(ld & 7)) && (!along_sum || !(cols & 7))) {
+    if (type == PP_TYPE_BF16 && !((uintptr_t)dy & 15) && (rows < 2 || (!(ld & 7) && ld <= PP_LAYER_MAX_COLS)) && (!along_sum || !(cols & 7))) {
         *out = pg_outer{(const uint8_t *)dy, rows, cols, ld, 0, 1};
         return PP_OK;
     }
@@ -297,6 +298,8 @@ extern "C" int pp_linear_backward_weight(int type, int64_t rows, int64_t n_in, i
     if (bad_layer(type, rows, n_in, n_out)) return PP_ERR_INVALID_ARG;
     if (pp_bad_matrix(dy, type, rows, n_out, ld_dy) || pp_bad_packed(x_codes, x_scales, rows)) return PP_ERR_INVALID_ARG;
     if (pp_bad_matrix(dw, PP_TYPE_F32, n_out, n_in, ld_dw) || ((uintptr_t)dw_in & 3) || ((uintptr_t)db & 3)) return PP_ERR_INVALID_ARG;
+    if (dw_in && n_out > 1 && ld_dw > PP_LAYER_MAX_LD_DW) return PP_ERR_INVALID_ARG;
+    if (n_out == 1) ld_dw = n_in;
     int shape;
     pr_plan p = plan_weight(type, rows, n_in, n_out, &shape);
     const pr_room room = room_backward(p, type, rows, n_out, true);

@@ -112,7 +112,7 @@ template <class Y, int WI> struct PrRows {
     }
     static const int TURNS = 32 / ROWS / 2;  // of half the rows
     // What is added to 16 rows from o0 on, where Y is float: asked for before those in front of them are written.
-    // (What a row's end leaves over is not used.)
+    // (What a row's end leaves over is not used.  Offsets are within 32 bits: add_ld <= 2^24.)
     static __device__ __forceinline__ void fetch(pp_u4 *d, int lane, long long o0, long long outer, long long i0, long long inner, const float *add,
                                                  long long add_ld) {
         const auto b = pr_resource(add + o0 * add_ld + i0, o0 < outer ? (((outer - o0 < 16 ? outer - o0 : 16) - 1) * add_ld + inner - i0) * 4 : 0);

@@ -17,7 +17,7 @@ PP_TYPE_F32, PP_TYPE_F16, PP_TYPE_BF16 = 0, 1, 2
 PP_PACK_INT8, PP_PACK_FP4 = 0, 1
 PP_ACT_GELU, PP_ACT_GELU_TANH, PP_ACT_SILU = 0, 1, 2
 PP_LINEAR_FORWARD, PP_LINEAR_BACKWARD_INPUT, PP_LINEAR_BACKWARD_WEIGHT = 0, 1, 2
-PP_LAYER_MAX_ROWS, PP_LAYER_MAX_COLS = 1 << 30, 1 << 22
+PP_LAYER_MAX_ROWS, PP_LAYER_MAX_COLS, PP_LAYER_MAX_LD_DW = 1 << 30, 1 << 22, 1 << 24
 BLOCK, GROUP = 32, 128
 
 EXPORTS = ("pp_pack", "pp_unpack", "pp_act_forward", "pp_act_backward", "pp_linear_workspace_bytes",
