@@ -84,7 +84,8 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     int xi = s0 % per_plane, xleft = (int)x.rows - xi * 64;  // its number in its plane, the rows from there on
     const uint8_t *xat = x.codes + (long long)xi * 64 * xpitch, *xsat = x.scales + (long long)xi * 64 * spitch;
     auto next_inner = [&](bool some) {
-        const int n = !some || xleft < 0 ? 0 : xleft < 64 ? xleft : 64;
+        // (a scalar, which the compiler has to be told: it would load in a loop over the lanes' buffers)
+        const int n = __builtin_amdgcn_readfirstlane(!some || xleft < 0 ? 0 : xleft < 64 ? xleft : 64);
         xb = __builtin_amdgcn_make_buffer_rsrc((void *)xat, 0, n * (int)xpitch, 0x00027000);
         xsb = __builtin_amdgcn_make_buffer_rsrc((void *)xsat, 0, n * (int)spitch, 0x00027000);
         const bool wrap = ++xi == per_plane;
@@ -185,7 +186,11 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
         if constexpr (ALONG) return *(const pr_bf8 *)(b + ao[k] + j * 4096);
         else return pg_read_t(b + ao[j] + k * 16 * RO, 4 * RO);
     };
-    pr_bf8 in[WI], outer[2][WO];  // the inner fragments are replaced as they have been used, the outer ones of odd quarters have places of their own
+    // Fragments.  Of small ones there is room for a whole step's, read two quarters ahead; of large ones the inner
+    // are replaced as they have been used, and the outer of odd quarters have places of their own.
+    constexpr int N = WI * WO;  // products of a quarter step
+    constexpr bool DEEP = N <= 4;
+    pr_bf8 in[DEEP ? 4 : 1][WI], outer[DEEP ? 4 : 2][WO];
     pr_f16 acc[WI][WO], acc_s[SUMS ? WO : 1] = {};
     const bool summing = SUMS && ti == 0 && wi == 0;
     const pr_bf8 ones = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
@@ -201,14 +206,15 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
         }
     };
 
-    constexpr int N = WI * WO, MEET = WO;  // products of a quarter step; those of the last one before the waves meet
+    // The waves meet in front of product MEET: step s + 1 is there then, and every wave has read all of step s.
+    constexpr int MEET = DEEP ? 2 * N + N / 2 : 3 * N + WO;
     constexpr int PARTS = 8 * PIECES;
     // Step s + 2's gradients are asked for in the SLOTS products behind a meeting; step s + 1's packed values
     // turned from product TURN to TURN_END of a step on.  (Waiting for a packed value the compiler, which does
     // not know of the gradients, waits for those of them that were asked for later too: they have to be old.)
     // Turned in the second and third quarters instead, dx = dy W4 takes 830 us where this takes 764 (8192 rows,
     // 16384 -> 4096, all zeros); the many instructions of 8 bits are better spread: 950, and 967 in the third alone.
-    constexpr int SLOTS = N - MEET, TURN = FMT == PP_PACK_INT8 ? 3 * N / 2 : 2 * N, TURN_END = 3 * N;
+    constexpr int SLOTS = 4 * N - MEET, TURN = DEEP ? N : FMT == PP_PACK_INT8 ? 3 * N / 2 : 2 * N, TURN_END = DEEP ? MEET : 3 * N;
     next_inner(true);
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) load_inner(j);
@@ -230,9 +236,12 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     PR_WAIT(2 * PIECES);
     pr_barrier();
 #pragma unroll
-    for (int j = 0; j < WI; ++j) in[j] = read_i(sm, 0, j);
+    for (int k = 0; k < (DEEP ? 2 : 1); ++k) {
 #pragma unroll
-    for (int j = 0; j < WO; ++j) outer[0][j] = read_o(sm, 0, j);
+        for (int j = 0; j < WI; ++j) in[k][j] = read_i(sm, k, j);
+#pragma unroll
+        for (int j = 0; j < WO; ++j) outer[k][j] = read_o(sm, k, j);
+    }
     pr_clear(acc);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the compiler need not wait for these within the loop
     auto behind = [&](int m, int stage) {  // what goes out behind product m from a meeting on
@@ -247,37 +256,41 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
         const uint8_t *now = sm + (s & 1) * (L::SI + L::SO), *next = sm + ((s + 1) & 1) * (L::SI + L::SO);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const pr_bf8 *o = outer[k & 1];
-            const uint8_t *b = k < 3 ? now : next;  // after the last step: what lies there, for nothing
+            const pr_bf8 *f = in[DEEP ? k : 0], *o = outer[DEEP ? k : k & 1];
+            const int ahead = DEEP ? (k + 2) & 3 : (k + 1) & 3;  // the quarter read meanwhile
+            const uint8_t *b = k < (DEEP ? 2 : 3) ? now : next;  // after the last step: what lies there, for nothing
             if (SUMS && summing) add_up(o);
             if (k == TURN / N) next_inner(s + 2 < steps);
 #pragma unroll
             for (int m = 0; m < N; ++m) {
-                const int i = m / WO, j = m % WO;
-                if (k == 3 && m == MEET) {  // step s + 1 is there, and every wave has read all of step s
-                    PR_WAIT(2 * PIECES);    // (but for the packed values of the step after it)
+                const int i = m / WO, j = m % WO, at = k * N + m;
+                if (at == MEET) {
+                    PR_WAIT(2 * PIECES);  // (but for the packed values of the step after it)
                     pr_barrier();
                     next_outer(s + 2 < steps);
                     aim(0, s);
                 }
-                pr_multiply(acc[i][j], in[i], o[j]);
-                if (k < 3) {
-                    if (i == 0) outer[(k + 1) & 1][j] = read_o(b, k + 1, j);
-                    if (j == WO - 1) in[i] = read_i(b, k + 1, i);
-                } else if (m >= MEET) {
-                    if (m - MEET < WO) outer[0][m - MEET] = read_o(b, 0, m - MEET);
-                    if (m == MEET) in[0] = read_i(b, 0, 0);
-                    if (j == WO - 1) in[i] = read_i(b, 0, i);
+                pr_multiply(acc[i][j], f[i], o[j]);
+                const int from = k == MEET / N ? MEET % N : 0, n = m - from;  // the quarter's reads start here
+                if (n >= 0) {
+                    constexpr int TO = DEEP ? 4 : 2;
+                    pr_bf8 *fa = in[DEEP ? ahead : 0], *oa = outer[ahead % TO];
+                    if (n < WO) oa[n] = read_o(b, ahead, n);
+                    if (!DEEP && from && n == 0) fa[0] = read_i(b, ahead, 0);  // (used up before the meeting)
+                    if (!DEEP && j == WO - 1) fa[i] = read_i(b, ahead, i);
+                    if (DEEP)
+#pragma unroll
+                        for (int q = n * WI / (N - from); q < (n + 1) * WI / (N - from); ++q) fa[q] = read_i(b, ahead, q);
                 }
-                if (k * N + m >= TURN && k * N + m < TURN_END) {
-                    const int slot = k * N + m - TURN;
+                if (at >= TURN && at < TURN_END) {
+                    const int slot = at - TURN;
 #pragma unroll
                     for (int t = slot * PARTS / (TURN_END - TURN); t < (slot + 1) * PARTS / (TURN_END - TURN); ++t) {
                         turn_inner(t, s + 1);
                         if ((t & 7) == 7) load_inner(t >> 3);  // step s + 2's: a whole step ahead
                     }
                 }
-                if (k == 3 && m >= MEET) behind(m - MEET, s);
+                if (at >= MEET) behind(at - MEET, s);
                 PR_PIN;
             }
         }
