@@ -49,10 +49,20 @@ static int launch_planes(int type, int64_t rows, int64_t cols, const void *src, 
 
 // ---- pieces of a sum, added in their order
 
+// The first `sum_blocks` workgroups add the columns' sums.
 template <class Y>
-__global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const float *__restrict__ part_sums, float *__restrict__ sums) {
+__global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const float *__restrict__ part_sums, float *__restrict__ sums, unsigned sum_blocks) {
+    if (blockIdx.x < sum_blocks) {
+        const long long o = blockIdx.x * 256ll + threadIdx.x;
+        float v = 0;
+        if (o < p.outer) {
+            for (int s = 0; s < p.splits; ++s) v += part_sums[s * p.outer + o];
+            sums[o] = v;
+        }
+        return;
+    }
     const long long chunks = p.partial_ld / 8, n = p.outer * chunks;
-    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < n; t += (long long)gridDim.x * 256) {
+    for (long long t = (blockIdx.x - sum_blocks) * 256ll + threadIdx.x; t < n; t += (gridDim.x - sum_blocks) * 256ll) {
         const long long o = t / chunks, i = (t - o * chunks) * 8;
         const float *q = p.partial + o * p.partial_ld + i;
         pp_f4 a = {0, 0, 0, 0}, b = a;
@@ -86,20 +96,15 @@ __global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const fl
         }
         pp_store8<Y>(out.p + o * out.ld + i, p.inner - i, v);
     }
-    if (sums)
-        for (long long o = (long long)blockIdx.x * 256 + threadIdx.x; o < p.outer; o += (long long)gridDim.x * 256) {
-            float v = 0;
-            for (int s = 0; s < p.splits; ++s) v += part_sums[s * p.outer + o];
-            sums[o] = v;
-        }
 }
 
 static int launch_join(int type, const pr_plan &p, void *out, long long ld, const float *bias, const float *add, const float *part_sums, float *sums,
                        hipStream_t st) {
     const long long blocks = (p.outer * (p.partial_ld / 8) + 255) / 256;
+    const unsigned sum_blocks = sums ? (unsigned)((p.outer + 255) / 256) : 0;
     return pp_by_type(type, [&](auto t) {
         typedef decltype(t) Y;
-        k_join<Y><<<(unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(p, pr_out<Y>{(typename Y::T *)out, ld, bias, add, ld}, part_sums, sums);
+        k_join<Y><<<sum_blocks + (unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(p, pr_out<Y>{(typename Y::T *)out, ld, bias, add, ld}, part_sums, sums, sum_blocks);
         return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
     });
 }
@@ -120,7 +125,8 @@ static const pr_shape WEIGHT[] = {{256, 256, 1, 1.8f, 1.8f, 20.0f}, {128, 128, 2
 
 // The shape and the number of pieces with the least estimated time: rounds of workgroups over the chip, and
 // for more than one piece the pass that adds them (a launch, and each partial sum written and read).
-static pr_plan plan(const pr_shape *shapes, int n, long long inner, long long outer, long long steps, int *shape) {
+// bi, bo: bytes of a step of the operands to an inner and an outer index.
+static pr_plan plan(const pr_shape *shapes, int n, long long inner, long long outer, long long steps, int bi, int bo, int *shape) {
     pr_plan best = {};
     float least = 0;
     for (int k = 0; k < n; ++k) {
@@ -143,6 +149,10 @@ static pr_plan plan(const pr_shape *shapes, int n, long long inner, long long ou
         }
     }
     const pr_shape &s = shapes[*shape];
+    // A die whose run is of one piece's tiles reads only that piece's part of the operands.  Where these are larger
+    // than a few L2s (4 MiB each) that is worth it: dw of 32771 rows, 520 -> 1000 (87 MB), 71 us for 75, 8192 rows
+    // (21 MB) 30 for 31; of less, reads are better spread: 2048 rows, 1024 -> 1024 (6 MB), 21.4 us for 23.7.
+    best.by_piece = steps * (inner * bi + outer * bo) >= (1 << 24);
     best.inner = inner;
     best.outer = outer;
     best.ni = (unsigned)((inner + s.ti - 1) / s.ti);
@@ -164,12 +174,12 @@ template <class F> static int in_turns(const pr_plan &p, int to, F launch) {
     return PP_OK;
 }
 
-static pr_plan plan_forward(int64_t rows, int64_t n_in, int64_t n_out, int *shape) { return plan(FORWARD, 3, n_out, rows, pp_groups(n_in), shape); }
+static pr_plan plan_forward(int64_t rows, int64_t n_in, int64_t n_out, int *shape) { return plan(FORWARD, 3, n_out, rows, pp_groups(n_in), 68, 68, shape); }
 static pr_plan plan_input(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(INPUT, 3, n_in, rows, planes_of(type) * ((n_out + 63) / 64), shape);
+    return plan(INPUT, 3, n_in, rows, planes_of(type) * ((n_out + 63) / 64), 34, 128, shape);
 }
 static pr_plan plan_weight(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(WEIGHT, 2, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), shape);
+    return plan(WEIGHT, 2, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), 66, 128, shape);
 }
 
 // ---- entry points

@@ -23,6 +23,7 @@ struct pr_plan {
     int steps;   // of the whole sum
     int per;     // of a piece
     int splits;
+    int by_piece;  // see pr_tile
     unsigned ni, no;  // tiles
     float *partial;
     long long partial_ld;
@@ -36,14 +37,18 @@ template <class Y> struct pr_out {
     long long add_ld;
 };
 
-// Tile of a workgroup.  Workgroups go to the eight dies in turn, and each die has an L2 of its own:
-// a die gets a run of neighbouring tiles, and within it patches of eight outer tiles by as many inner
-// ones as fit, so that what is in flight shares operands.
-__device__ __forceinline__ void pr_tile(const pr_plan &p, unsigned b, unsigned &ti, unsigned &to) {
-    const unsigned n = p.ni * p.no, die = b & 7, at = b >> 3, per = n >> 3, more = n & 7;
-    const unsigned t = die * per + (die < more ? die : more) + at;
+// Tile and piece of a workgroup.  Workgroups go to the eight dies in turn, and each die has an L2 of its own:
+// a die gets a run of neighbouring tiles, and within it patches of eight outer tiles by as many inner ones as
+// fit, so that what is in flight shares operands.  Its run is of each piece's tiles, or of all the pieces' one
+// after the other (by_piece), where a die reads little beside its own part of the sum.
+__device__ __forceinline__ void pr_tile(const pr_plan &p, unsigned b, unsigned &ti, unsigned &to, int &piece) {
+    const unsigned tiles = p.ni * p.no, z = p.by_piece ? 0 : b / tiles, n = p.by_piece ? tiles * p.splits : tiles;
+    b -= z * tiles;
+    const unsigned die = b & 7, at = b >> 3, per = n >> 3, more = n & 7;
+    const unsigned all = die * per + (die < more ? die : more) + at, y = all / tiles, t = all - y * tiles;
     const unsigned strip = t / (8 * p.ni), in = t - strip * 8 * p.ni, o0 = strip * 8;
     const unsigned high = p.no - o0 < 8 ? p.no - o0 : 8;
+    piece = (int)(z + y);
     to = o0 + in % high;
     ti = in / high;
 }

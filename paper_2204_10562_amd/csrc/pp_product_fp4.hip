@@ -40,8 +40,9 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
     extern __shared__ uint8_t sm[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unsigned ti, to;
-    pr_tile(p, blockIdx.x, ti, to);
-    const int piece = blockIdx.y, s0 = piece * p.per;
+    int piece;
+    pr_tile(p, blockIdx.x, ti, to, piece);
+    const int s0 = piece * p.per;
     const int steps = p.steps - s0 < p.per ? p.steps - s0 : p.per;
     const long long i0 = (long long)ti * L::TI, o0 = (long long)to * L::TO;
     const long long pitch = (long long)p.steps * PP_GROUP_CODES4, spitch = (long long)p.steps * 4;
@@ -345,7 +346,7 @@ template <int WI, int WO, int NI, int NO> static int launch4(int type, pr_plan p
     return pp_by_type(type, [&](auto t) {
         typedef decltype(t) Y;
         auto *k = k_product4<WI, WO, NI, NO, Y>;
-        k<<<dim3(p.ni * p.no, p.splits), 64 * L::WAVES, L::LDS, st>>>(p, q, pr_out<Y>{(typename Y::T *)y, ld, bias, NULL, 0});
+        k<<<p.ni * p.no * p.splits, 64 * L::WAVES, L::LDS, st>>>(p, q, pr_out<Y>{(typename Y::T *)y, ld, bias, NULL, 0});
         return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
     });
 }

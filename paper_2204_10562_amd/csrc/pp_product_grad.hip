@@ -59,8 +59,9 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     extern __shared__ uint8_t sm[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unsigned ti, to;
-    pr_tile(p, blockIdx.x, ti, to);
-    const int piece = blockIdx.y, s0 = piece * p.per;
+    int piece;
+    pr_tile(p, blockIdx.x, ti, to, piece);
+    const int s0 = piece * p.per;
     const int steps = p.steps - s0 < p.per ? p.steps - s0 : p.per, per_plane = p.steps / y.planes;
     const long long i0 = (long long)ti * L::TI, o0 = (long long)to * L::TO;
     const unsigned base = pr_lds_of(sm);
@@ -191,18 +192,18 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     constexpr int N = WI * WO;  // products of a quarter step
     constexpr bool DEEP = N <= 4;
     pr_bf8 in[DEEP ? 4 : 1][WI], outer[DEEP ? 4 : 2][WO];
-    pr_f16 acc[WI][WO], acc_s[SUMS ? WO : 1] = {};
+    pr_f16 acc[WI][WO];
     const bool summing = SUMS && ti == 0 && wi == 0;
-    const pr_bf8 ones = {(__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f, (__bf16)1.0f};
-    // The columns' sums, a product with ones: in ordinary registers (the others are full), and waited
-    // for at once, as what only some waves do may be moved about behind it.
+    // The columns' sums, by the waves that have them all: a lane's eight rows by pairs, in 32 bits.
+    float total[SUMS ? WO : 1] = {};
     auto add_up = [&](const pr_bf8 *f) {
-        if constexpr (SUMS) {
 #pragma unroll
-            for (int j = 0; j < WO; ++j) asm volatile("s_nop 3\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(acc_s[j]) : "v"(ones), "v"(f[j]));
-            asm volatile("s_nop 15\n\ts_nop 3" : "+v"(acc_s[0]));
-#pragma unroll
-            for (int j = 1; j < WO; ++j) asm volatile("" : "+v"(acc_s[j]));
+        for (int j = 0; j < (SUMS ? WO : 0); ++j) {
+            const pp_bf2 one = {(__bf16)1.0f, (__bf16)1.0f};
+            float v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f[j], f[j], 0, 1), one, 0.0f, false);
+            v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f[j], f[j], 2, 3), one, v, false);
+            v = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f[j], f[j], 4, 5), one, v, false);
+            total[j] += __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(f[j], f[j], 6, 7), one, v, false);
         }
     };
 
@@ -299,11 +300,12 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     PR_WAIT(0);  // nothing is on its way to LDS any more
     pr_barrier();
     if constexpr (SUMS)
-        if (summing && g == 0) {
+        if (summing) {
 #pragma unroll
             for (int j = 0; j < WO; ++j) {
+                const float v = total[j] + __shfl_xor(total[j], 32);
                 const long long o = o0 + (wo * WO + j) * 32 + r;
-                if (o < p.outer) sums[piece * p.outer + o] = acc_s[j][0];
+                if (g == 0 && o < p.outer) sums[piece * p.outer + o] = v;
             }
         }
     pr_leave<Y, WI, WO>(p, out, acc, sm + wave * (32 * 32 * WI * 4), lane, i0 + wi * WI * 32, o0 + wo * WO * 32, piece);
@@ -313,7 +315,7 @@ template <int FMT, bool ALONG, int WI, int WO, int NI, int NO, class Y, bool SUM
 static int launch_one(const pr_plan &p, const pg_inner &x, const pg_outer &y, const pr_out<Y> &out, float *sums, hipStream_t st) {
     typedef PgTile<WI, WO, NI, NO> L;
     auto *k = k_product_grad<FMT, ALONG, WI, WO, NI, NO, Y, SUMS>;
-    k<<<dim3(p.ni * p.no, p.splits), 64 * L::WAVES, L::LDS, st>>>(p, x, y, out, sums);
+    k<<<p.ni * p.no * p.splits, 64 * L::WAVES, L::LDS, st>>>(p, x, y, out, sums);
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
 }
 
