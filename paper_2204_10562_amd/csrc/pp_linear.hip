@@ -118,7 +118,7 @@ struct pr_shape {
     int ti, to, fit;
     float alone, full, once;
 };
-static const pr_shape FORWARD[] = {{256, 256, 1, 1.0f, 1.0f, 12.0f}, {128, 128, 2, 0.34f, 0.62f, 6.0f}, {256, 32, 2, 0.28f, 0.5f, 5.0f}};
+static const pr_shape FORWARD[] = {{256, 256, 1, 1.0f, 1.0f, 12.0f}, {128, 128, 2, 0.32f, 0.62f, 6.0f}, {256, 32, 2, 0.36f, 0.5f, 5.0f}};
 static const pr_shape INPUT[] = {{256, 256, 1, 1.5f, 1.7f, 12.0f}, {128, 128, 2, 0.68f, 1.14f, 6.0f}, {256, 32, 2, 0.78f, 1.1f, 5.0f}};
 static const pr_shape WEIGHT[] = {{256, 256, 1, 1.5f, 1.8f, 20.0f}, {128, 128, 2, 1.0f, 1.22f, 8.0f}};
 #define PR_CUS 256

@@ -2,7 +2,7 @@
 // take 64 values of either operand and a power of two for every 32 at once.
 //
 // k_product4: both operands go from global memory straight to LDS, 64 bytes (128 values) of a row to
-// a step, three steps deep; a wave reads the fragments of the next half step while the matrix units
+// a step, three or four steps deep; a wave reads the fragments of the next half step while the matrix units
 // work on this one.
 #include "pp_product_fp4.h"
 
@@ -26,17 +26,19 @@ template <int HALF> __device__ __forceinline__ void p4_multiply(pr_f16 &acc, pp_
 __device__ __forceinline__ int p4_turn(int row) { return (row >> 2) & 3; }
 
 // WI x WO fragments of 32 x 32 to a wave, NI x NO waves
-template <int WI, int WO, int NI, int NO> struct P4Tile {
+// (AHEAD steps in LDS)
+template <int WI, int WO, int NI, int NO, int AHEAD> struct P4Tile {
     static const int TI = 32 * WI * NI, TO = 32 * WO * NO, WAVES = NI * NO;
     static const int SI = TI * PR_STEP, SO = TO * PR_STEP;           // bytes of a stage
     static const int CI = TI * 16, CO = (TO < 64 ? 64 : TO) * 16;    // bytes of four steps' scales
-    static const int LDS = 3 * (SI + SO) + 2 * (CI + CO) > WAVES * 4096 * WI ? 3 * (SI + SO) + 2 * (CI + CO) : WAVES * 4096 * WI;
+    static const int SCALES = AHEAD * (SI + SO), ALL = SCALES + 2 * (CI + CO);
+    static const int LDS = ALL > WAVES * 4096 * WI ? ALL : WAVES * 4096 * WI;
     static const int LI = TI / 16 / WAVES, LO = TO / 16 < WAVES ? 1 : TO / 16 / WAVES, LL = LI + LO;  // loads of a wave to a step
 };
 
-template <int WI, int WO, int NI, int NO, class Y>
+template <int WI, int WO, int NI, int NO, int AHEAD, class Y>
 __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_operands q, pr_out<Y> out) {
-    typedef P4Tile<WI, WO, NI, NO> L;
+    typedef P4Tile<WI, WO, NI, NO, AHEAD> L;
     extern __shared__ uint8_t sm[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     unsigned ti, to;
@@ -49,7 +51,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
     const long long ri = p.inner - i0 < L::TI ? p.inner - i0 : L::TI, ro = p.outer - o0 < L::TO ? p.outer - o0 : L::TO;
     const pp_i4 bi = pr_buffer(q.inner_codes + i0 * pitch, ri * pitch), bo = pr_buffer(q.outer_codes + o0 * pitch, ro * pitch);
     const pp_i4 ci = pr_buffer(q.inner_scales + i0 * spitch, ri * spitch), co = pr_buffer(q.outer_scales + o0 * spitch, ro * spitch);
-    const unsigned base = pr_lds_of(sm), scales = base + 3 * (L::SI + L::SO);
+    const unsigned base = pr_lds_of(sm), scales = base + L::SCALES;
 
     // where this lane's pieces come from: 16 rows of four pieces to a load, a wave's loads 1024 bytes of LDS apart
     unsigned vi[L::LI], vo[L::LO];
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
     pp_i4 in[WI], first[WO], late[WO];
     int in_raw[WI], out_raw[WO], in_c[WI], out_c[WO];
     auto codes_at = [&](int buf) { return sm + buf * (L::SI + L::SO); };
-    auto scales_at = [&](int s) { return sm + 3 * (L::SI + L::SO) + ((s >> 2) & 1) * (L::CI + L::CO) + (s & 3) * 4; };
+    auto scales_at = [&](int s) { return sm + L::SCALES + ((s >> 2) & 1) * (L::CI + L::CO) + (s & 3) * 4; };
     auto read = [&](const uint8_t *b, int at, int j) { return *(const pp_i4 *)(b + at + j * 32 * PR_STEP); };
     auto read_scales = [&](const uint8_t *c) {
 #pragma unroll
@@ -116,7 +118,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
     pr_f16 acc[WI][WO];
 
 #pragma unroll
-    for (int t = 0; t < 3; ++t) {
+    for (int t = 0; t < AHEAD; ++t) {
         load_scales(t);
         open(t);
 #pragma unroll
@@ -136,10 +138,10 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
     pr_clear(acc);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the compiler need not wait for these within the loop
     constexpr int N = WI * WO, MEET = WO;  // products of a half step; those of the second one before the waves meet
-    constexpr int SLOTS = 2 * N - MEET;    // products from one meeting to the next: step s + 3's loads go out behind them, into step s's stage
-    int b0 = 0, b1 = 1, b2 = 2;            // the stages of steps s, s + 1 and s + 2
-    int sent = 2;                          // the last step whose loads went out or are going out
-    unsigned sent_at = 2 * (L::SI + L::SO);
+    constexpr int SLOTS = 2 * N - MEET;    // products from one meeting to the next: step s + AHEAD's loads go out behind them, into step s's stage
+    int b0 = 0, b1 = 1;                    // the stages of steps s and s + 1
+    int sent = AHEAD - 1;                  // the last step whose loads went out or are going out
+    unsigned sent_at = sent * (L::SI + L::SO);
     for (int s = 0; s < steps; ++s) {
         const uint8_t *now = codes_at(b0), *next = codes_at(b1);  // after the last step: what lies there, for nothing
         // what follows product m, counted from the meeting of the step before
@@ -170,9 +172,9 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
         for (int m = 0; m < N; ++m) {
             const int i = m / WO, j = m % WO;
             if (m == MEET) {  // step s + 1 has arrived for every wave, and every wave has read all of step s
-                PR_WAIT(L::LL);
+                PR_WAIT((AHEAD - 2) * L::LL);
                 pr_barrier();
-                sent = s + 3;
+                sent = s + AHEAD;
                 sent_at = b0 * (L::SI + L::SO);
                 open(sent);
                 load_scales(sent);
@@ -188,10 +190,8 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
             }
             PR_PIN;
         }
-        const int t = b0;
         b0 = b1;
-        b1 = b2;
-        b2 = t;
+        b1 = b1 == AHEAD - 1 ? 0 : b1 + 1;
         pr_settle(s + 1, steps);
     }
     PR_WAIT(0);  // nothing is on its way to LDS any more
@@ -341,18 +341,18 @@ int r4_launch(int type, int64_t rows, int64_t n_in, int64_t n_out, const void *x
     });
 }
 
-template <int WI, int WO, int NI, int NO> static int launch4(int type, pr_plan p, const p4_operands &q, void *y, long long ld, const float *bias, hipStream_t st) {
-    typedef P4Tile<WI, WO, NI, NO> L;
+template <int WI, int WO, int NI, int NO, int AHEAD> static int launch4(int type, pr_plan p, const p4_operands &q, void *y, long long ld, const float *bias, hipStream_t st) {
+    typedef P4Tile<WI, WO, NI, NO, AHEAD> L;
     return pp_by_type(type, [&](auto t) {
         typedef decltype(t) Y;
-        auto *k = k_product4<WI, WO, NI, NO, Y>;
+        auto *k = k_product4<WI, WO, NI, NO, AHEAD, Y>;
         k<<<p.ni * p.no * p.splits, 64 * L::WAVES, L::LDS, st>>>(p, q, pr_out<Y>{(typename Y::T *)y, ld, bias, NULL, 0});
         return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
     });
 }
 
 int p4_launch(int shape, int type, const pr_plan &p, const p4_operands &q, void *y, long long ld, const float *bias, hipStream_t st) {
-    if (shape == 0) return launch4<4, 4, 2, 2>(type, p, q, y, ld, bias, st);
-    if (shape == 1) return launch4<2, 2, 2, 2>(type, p, q, y, ld, bias, st);
-    return launch4<2, 1, 4, 1>(type, p, q, y, ld, bias, st);
+    if (shape == 0) return launch4<4, 4, 2, 2, 3>(type, p, q, y, ld, bias, st);
+    if (shape == 1) return launch4<2, 2, 2, 2, 4>(type, p, q, y, ld, bias, st);
+    return launch4<2, 1, 4, 1, 3>(type, p, q, y, ld, bias, st);
 }
