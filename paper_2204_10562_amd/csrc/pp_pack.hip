@@ -8,118 +8,87 @@
 
 #define PK_THREADS 256
 
-// What a launch covers: rows of `chunks` chunks of eight columns (those of whole groups), a thread to a
-// chunk and U rows: where there is enough for it, four rows under each other, whose loads are in flight
-// together; where there is little, one, and four times as many threads.
+// What a launch covers: rows of `chunks` chunks of eight columns (those of whole groups), a thread to each.
 struct pk_shape {
-    long long rows, cols;
+    long long cols;
     unsigned chunks, magic;  // t / chunks = t * magic >> 32 + shift
-    int shift, u;
-    unsigned runs, items;  // runs of u rows in the launch; threads = runs * chunks
+    int shift;
+    unsigned items;  // chunks of all rows
 };
 
-// From 2^20 chunks on (1024 to a SIMD) there is enough for four rows to a thread.
 static pk_shape pk_plan(int64_t rows, int64_t cols) {
     pk_shape s;
-    s.rows = rows;
     s.cols = cols;
     s.chunks = (unsigned)(pp_groups(cols) * (PP_GROUP / 8));
     s.shift = 0;
     while ((2ull << s.shift) < s.chunks) ++s.shift;  // (t < 2^31: 32 bits of the reciprocal are enough)
     s.magic = (unsigned)(((1ull << (32 + s.shift)) + s.chunks - 1) / s.chunks);
-    s.u = rows * s.chunks >= (1 << 20) ? 4 : 1;
-    const int64_t runs = (rows + s.u - 1) / s.u, most = (((int64_t)1 << 31) - 1) / s.chunks;
-    s.runs = (unsigned)(runs < most ? runs : most);
-    s.items = s.runs * s.chunks;
+    const int64_t most = (((int64_t)1 << 31) - 1) / s.chunks;
+    s.items = (unsigned)(rows < most ? rows : most) * s.chunks;
     return s;
 }
 
-// In a kernel of shape `s`: q the thread's chunk, its U rows from row0 on.  The lanes of a
-// quad have one row and four neighbouring chunks (chunks is a multiple of 16), and go together.
+// In a kernel of shape `s`: `at` the thread's chunk of all, q that of its row r.  The lanes of a quad have
+// one row and four neighbouring chunks (chunks is a multiple of 16), and go together.
 #define PK_THREAD(s)                                                              \
-    const unsigned item = blockIdx.x * PK_THREADS + threadIdx.x;                  \
-    if (item >= (s).items) return;                                                \
-    const unsigned run = __umulhi(item, (s).magic) >> (s).shift;                  \
-    const unsigned q = item - run * (s).chunks;                                   \
-    const long long row0 = (long long)run * U;                                    \
+    const unsigned at = blockIdx.x * PK_THREADS + threadIdx.x;                    \
+    if (at >= (s).items) return;                                                  \
+    const unsigned run = __umulhi(at, (s).magic) >> (s).shift;                    \
+    const unsigned q = at - run * (s).chunks;                                     \
+    const long long r = run;                                                      \
     const long long left = (s).cols - 8ll * q; /* columns from the chunk's first on, maybe <= 0 */
 
-// Runs launch(part, first row) for as many launches as the rows take.
+// Runs launch(part, grid, first row) for as many launches as the rows take.
 template <class F> static int pk_launch(int64_t rows, int64_t cols, F launch) {
     for (int64_t r = 0; r < rows;) {
         const pk_shape s = pk_plan(rows - r, cols);
         launch(s, (s.items + PK_THREADS - 1) / PK_THREADS, r);
         if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
-        r += (int64_t)s.runs * s.u;
+        r += s.items / s.chunks;
     }
     return PP_OK;
 }
 
-__device__ __forceinline__ void put_codes8(long long at, unsigned m, const float *v, uint8_t *codes, uint8_t *scales) {
+__device__ __forceinline__ void put_codes8(unsigned at, unsigned m, const float *v, uint8_t *codes, uint8_t *scales) {
     pp_u2 c;
     const unsigned byte = pp_codes8(v, m, c);
-    *(pp_u2 *)(codes + at * 8) = c;
+    *(pp_u2 *)(codes + at * 8ll) = c;
     if (!(at & 3)) scales[at >> 2] = (uint8_t)byte;
 }
-__device__ __forceinline__ void put_codes4(long long at, unsigned m, const float *v, uint8_t *codes, uint8_t *scales) {
+__device__ __forceinline__ void put_codes4(unsigned at, unsigned m, const float *v, uint8_t *codes, uint8_t *scales) {
     unsigned c;
     const unsigned byte = pp_codes4(v, m, c);
-    *(unsigned *)(codes + at * 4) = c;
+    *(unsigned *)(codes + at * 4ll) = c;
     if (!(at & 3)) scales[at >> 2] = (uint8_t)byte;
 }
 
 // FMT, or both formats at once (PK_BOTH)
 #define PK_BOTH 2
-template <int FMT, int U, class Y>
+template <int FMT, class Y>
 __global__ __launch_bounds__(PK_THREADS) void k_pack(pk_shape s, const typename Y::T *__restrict__ src, long long ld, uint8_t *__restrict__ codes,
                                                      uint8_t *__restrict__ scales, uint8_t *__restrict__ codes8, uint8_t *__restrict__ scales8) {
     PK_THREAD(s)
-    PpRaw<Y> raw[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const long long r = row0 + i;
-        raw[i] = pp_load8<Y>(src + r * ld + 8 * q, r < s.rows ? left : 0);
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const long long r = row0 + i, at = r * s.chunks + q;
-        if (r >= s.rows) break;
-        float v[8];
-        pp_values<Y>(raw[i], v);
-        const unsigned m = pp_quad_max(pp_absmax<Y>(raw[i], v));
-        if constexpr (FMT == PP_PACK_INT8) {
-            put_codes8(at, m, v, codes, scales);
-        } else {
-            put_codes4(at, m, v, codes, scales);
-            if constexpr (FMT == PK_BOTH) put_codes8(at, m, v, codes8, scales8);
-        }
+    const PpRaw<Y> raw = pp_load8<Y>(src + r * ld + 8 * q, left);
+    float v[8];
+    pp_values<Y>(raw, v);
+    const unsigned m = pp_quad_max(pp_absmax<Y>(raw, v));
+    if constexpr (FMT == PP_PACK_INT8) {
+        put_codes8(at, m, v, codes, scales);
+    } else {
+        put_codes4(at, m, v, codes, scales);
+        if constexpr (FMT == PK_BOTH) put_codes8(at, m, v, codes8, scales8);
     }
 }
 
-template <int FMT, int U, class Y>
+template <int FMT, class Y>
 __global__ __launch_bounds__(PK_THREADS) void k_unpack(pk_shape s, const uint8_t *__restrict__ codes, const uint8_t *__restrict__ scales,
                                                        typename Y::T *__restrict__ dst, long long ld) {
     PK_THREAD(s)
     if (left <= 0) return;
-    pp_u2 c[U];
-    unsigned byte[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const long long r = row0 + i, at = r * s.chunks + q;
-        if (r >= s.rows) break;
-        if constexpr (FMT == PP_PACK_INT8) c[i] = *(const pp_u2 *)(codes + at * 8);
-        else c[i][0] = *(const unsigned *)(codes + at * 4);
-        byte[i] = scales[at >> 2];
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const long long r = row0 + i;
-        if (r >= s.rows) break;
-        float v[8];
-        if constexpr (FMT == PP_PACK_INT8) pp_values8(c[i], pp_unit8(byte[i]), v);
-        else pp_values4(c[i][0], byte[i], v);
-        pp_store8<Y>(dst + r * ld + 8 * q, left, v);
-    }
+    float v[8];
+    if constexpr (FMT == PP_PACK_INT8) pp_values8(*(const pp_u2 *)(codes + at * 8ll), pp_unit8(scales[at >> 2]), v);
+    else pp_values4(*(const unsigned *)(codes + at * 4ll), scales[at >> 2], v);
+    pp_store8<Y>(dst + r * ld + 8 * q, left, v);
 }
 
 // f and f'.  exp2 and the reciprocal are the hardware's (a unit or two of the last place), which
@@ -155,87 +124,54 @@ template <int KIND> __device__ __forceinline__ void act_both(float x, float &f, 
     }
 }
 
-template <int KIND, int U, class Y, bool GATED>
+template <int KIND, class Y, bool GATED>
 __global__ __launch_bounds__(PK_THREADS) void k_act_forward(pk_shape s, const typename Y::T *__restrict__ x, long long ld_x,
                                                             const typename Y::T *__restrict__ u, long long ld_u,
                                                             typename Y::T *__restrict__ y, long long ld_y, uint8_t *__restrict__ xc,
                                                             uint8_t *__restrict__ xs, uint8_t *__restrict__ uc, uint8_t *__restrict__ us) {
     PK_THREAD(s)
-    PpRaw<Y> rx[U], ru[U];
+    const PpRaw<Y> rx = pp_load8<Y>(x + r * ld_x + 8 * q, left);
+    PpRaw<Y> ru;
+    if constexpr (GATED) ru = pp_load8<Y>(u + r * ld_u + 8 * q, left);
+    float v[8], w[8], t[8];
+    pp_values<Y>(rx, v);
+    if (xc) put_codes8(at, pp_quad_max(pp_absmax<Y>(rx, v)), v, xc, xs);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const long long r = row0 + i, n = r < s.rows ? left : 0;
-        rx[i] = pp_load8<Y>(x + r * ld_x + 8 * q, n);
-        if constexpr (GATED) ru[i] = pp_load8<Y>(u + r * ld_u + 8 * q, n);
+    for (int j = 0; j < 8; ++j) t[j] = act<KIND>(v[j]);
+    if constexpr (GATED) {
+        pp_values<Y>(ru, w);
+        if (uc) put_codes8(at, pp_quad_max(pp_absmax<Y>(ru, w)), w, uc, us);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] *= w[j];
     }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const long long r = row0 + i, at = r * s.chunks + q;
-        if (r >= s.rows) break;
-        float v[8], w[8], t[8];
-        pp_values<Y>(rx[i], v);
-        if (xc) put_codes8(at, pp_quad_max(pp_absmax<Y>(rx[i], v)), v, xc, xs);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) t[j] = act<KIND>(v[j]);
-        if constexpr (GATED) {
-            pp_values<Y>(ru[i], w);
-            if (uc) put_codes8(at, pp_quad_max(pp_absmax<Y>(ru[i], w)), w, uc, us);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) t[j] *= w[j];
-        }
-        if (left > 0) pp_store8<Y>(y + r * ld_y + 8 * q, left, t);
-    }
+    if (left > 0) pp_store8<Y>(y + r * ld_y + 8 * q, left, t);
 }
 
 // dy and dx may be one matrix: a thread reads its values before it writes them
-template <int KIND, int U, class Y, bool GATED>
+template <int KIND, class Y, bool GATED>
 __global__ __launch_bounds__(PK_THREADS) void k_act_backward(pk_shape s, const typename Y::T *dy, long long ld_dy,
                                                              const uint8_t *__restrict__ xc, const uint8_t *__restrict__ xs,
                                                              const uint8_t *__restrict__ uc, const uint8_t *__restrict__ us,
                                                              typename Y::T *dx, long long ld_dx, typename Y::T *__restrict__ du, long long ld_du) {
     PK_THREAD(s)
     if (left <= 0) return;
-    PpRaw<Y> rd[U];
-    pp_u2 cx[U], cu[U];
-    unsigned bx[U], bu[U];
+    const PpRaw<Y> rd = pp_load8<Y>(dy + r * ld_dy + 8 * q, left);
+    float g[8], v[8], w[8], a[8];
+    pp_values8(*(const pp_u2 *)(xc + at * 8ll), pp_unit8(xs[at >> 2]), v);
+    if constexpr (GATED) pp_values8(*(const pp_u2 *)(uc + at * 8ll), pp_unit8(us[at >> 2]), w);
+    pp_values<Y>(rd, g);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const long long r = row0 + i, at = r * s.chunks + q;
-        if (r >= s.rows) break;
-        rd[i] = pp_load8<Y>(dy + r * ld_dy + 8 * q, left);
-        cx[i] = *(const pp_u2 *)(xc + at * 8);
-        bx[i] = xs[at >> 2];
-        if constexpr (GATED) {
-            cu[i] = *(const pp_u2 *)(uc + at * 8);
-            bu[i] = us[at >> 2];
-        }
+    for (int j = 0; j < 8; ++j) {
+        float f, d;
+        act_both<KIND>(v[j], f, d);
+        a[j] = g[j] * f;
+        v[j] = g[j] * d;
+        if constexpr (GATED) v[j] *= w[j];
     }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-        const long long r = row0 + i;
-        if (r >= s.rows) break;
-        float g[8], v[8], w[8], a[8];
-        pp_values<Y>(rd[i], g);
-        pp_values8(cx[i], pp_unit8(bx[i]), v);
-        if constexpr (GATED) pp_values8(cu[i], pp_unit8(bu[i]), w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            float f, d;
-            act_both<KIND>(v[j], f, d);
-            a[j] = g[j] * f;
-            v[j] = g[j] * d;
-            if constexpr (GATED) v[j] *= w[j];
-        }
-        pp_store8<Y>(dx + r * ld_dx + 8 * q, left, v);
-        if constexpr (GATED) pp_store8<Y>(du + r * ld_du + 8 * q, left, a);
-    }
+    pp_store8<Y>(dx + r * ld_dx + 8 * q, left, v);
+    if constexpr (GATED) pp_store8<Y>(du + r * ld_du + 8 * q, left, a);
 }
 
-// Calls f with U as a constant.
-template <class F> static void by_u(int u, F f) {
-    if (u == 1) f(std::integral_constant<int, 1>());
-    else f(std::integral_constant<int, 4>());
-}
 // `p` moved on by so many bytes; NULL stays.
 static uint8_t *on(void *p, int64_t bytes) { return p ? (uint8_t *)p + bytes : NULL; }
 static const uint8_t *on(const void *p, int64_t bytes) { return p ? (const uint8_t *)p + bytes : NULL; }
@@ -247,10 +183,8 @@ template <int FMT> static int launch_pack(int type, int64_t rows, int64_t cols, 
         typedef decltype(y) Y;
         typedef typename Y::T T;
         return pk_launch(rows, cols, [&](const pk_shape &s, unsigned grid, int64_t r) {
-            by_u(s.u, [&](auto u) {
-                k_pack<FMT, decltype(u)::value, Y><<<grid, PK_THREADS, 0, st>>>(s, (const T *)src + r * ld, ld, on(codes, r * g * width), on(scales, r * g * 4),
-                                                                                on(codes8, r * g * PP_GROUP_CODES8), on(scales8, r * g * 4));
-            });
+            k_pack<FMT, Y><<<grid, PK_THREADS, 0, st>>>(s, (const T *)src + r * ld, ld, on(codes, r * g * width), on(scales, r * g * 4),
+                                                                            on(codes8, r * g * PP_GROUP_CODES8), on(scales8, r * g * 4));
         });
     });
 }
@@ -279,13 +213,10 @@ extern "C" int pp_unpack(int format, int type, int64_t rows, int64_t cols, const
         typedef decltype(y) Y;
         typedef typename Y::T T;
         return pk_launch(rows, cols, [&](const pk_shape &s, unsigned grid, int64_t r) {
-            by_u(s.u, [&](auto u) {
-                constexpr int U = decltype(u)::value;
-                if (format == PP_PACK_INT8)
-                    k_unpack<PP_PACK_INT8, U, Y><<<grid, PK_THREADS, 0, st>>>(s, on(codes, r * g * PP_GROUP_CODES8), on(scales, r * g * 4), (T *)dst + r * ld_dst, ld_dst);
-                else
-                    k_unpack<PP_PACK_FP4, U, Y><<<grid, PK_THREADS, 0, st>>>(s, on(codes, r * g * PP_GROUP_CODES4), on(scales, r * g * 4), (T *)dst + r * ld_dst, ld_dst);
-            });
+            if (format == PP_PACK_INT8)
+                k_unpack<PP_PACK_INT8, Y><<<grid, PK_THREADS, 0, st>>>(s, on(codes, r * g * PP_GROUP_CODES8), on(scales, r * g * 4), (T *)dst + r * ld_dst, ld_dst);
+            else
+                k_unpack<PP_PACK_FP4, Y><<<grid, PK_THREADS, 0, st>>>(s, on(codes, r * g * PP_GROUP_CODES4), on(scales, r * g * 4), (T *)dst + r * ld_dst, ld_dst);
         });
     });
 }
@@ -314,15 +245,12 @@ extern "C" int pp_act_forward(int kind, int type, int64_t rows, int64_t cols, co
             return pk_launch(rows, cols, [&](const pk_shape &s, unsigned grid, int64_t r) {
                 uint8_t *xc = on(x_codes, r * g * PP_GROUP_CODES8), *xs = on(x_scales, r * g * 4);
                 uint8_t *uc = on(u_codes, r * g * PP_GROUP_CODES8), *us = on(u_scales, r * g * 4);
-                by_u(s.u, [&](auto n) {
-                    constexpr int U = decltype(n)::value;
-                    if (u)
-                        k_act_forward<K, U, Y, true><<<grid, PK_THREADS, 0, st>>>(s, (const T *)x + r * ld_x, ld_x, (const T *)u + r * ld_u, ld_u, (T *)y + r * ld_y,
-                                                                                  ld_y, xc, xs, uc, us);
-                    else
-                        k_act_forward<K, U, Y, false><<<grid, PK_THREADS, 0, st>>>(s, (const T *)x + r * ld_x, ld_x, (const T *)NULL, 0, (T *)y + r * ld_y, ld_y, xc, xs,
-                                                                                   (uint8_t *)NULL, (uint8_t *)NULL);
-                });
+                if (u)
+                    k_act_forward<K, Y, true><<<grid, PK_THREADS, 0, st>>>(s, (const T *)x + r * ld_x, ld_x, (const T *)u + r * ld_u, ld_u, (T *)y + r * ld_y,
+                                                                              ld_y, xc, xs, uc, us);
+                else
+                    k_act_forward<K, Y, false><<<grid, PK_THREADS, 0, st>>>(s, (const T *)x + r * ld_x, ld_x, (const T *)NULL, 0, (T *)y + r * ld_y, ld_y, xc, xs,
+                                                                               (uint8_t *)NULL, (uint8_t *)NULL);
             });
         });
     });
@@ -346,15 +274,12 @@ extern "C" int pp_act_backward(int kind, int type, int64_t rows, int64_t cols, c
             return pk_launch(rows, cols, [&](const pk_shape &s, unsigned grid, int64_t r) {
                 const uint8_t *xc = on(x_codes, r * g * PP_GROUP_CODES8), *xs = on(x_scales, r * g * 4);
                 const uint8_t *uc = on(u_codes, r * g * PP_GROUP_CODES8), *us = on(u_scales, r * g * 4);
-                by_u(s.u, [&](auto n) {
-                    constexpr int U = decltype(n)::value;
-                    if (gated)
-                        k_act_backward<K, U, Y, true><<<grid, PK_THREADS, 0, st>>>(s, (const T *)dy + r * ld_dy, ld_dy, xc, xs, uc, us, (T *)dx + r * ld_dx, ld_dx,
-                                                                                   (T *)du + r * ld_du, ld_du);
-                    else
-                        k_act_backward<K, U, Y, false><<<grid, PK_THREADS, 0, st>>>(s, (const T *)dy + r * ld_dy, ld_dy, xc, xs, uc, us, (T *)dx + r * ld_dx, ld_dx,
-                                                                                    (T *)NULL, 0);
-                });
+                if (gated)
+                    k_act_backward<K, Y, true><<<grid, PK_THREADS, 0, st>>>(s, (const T *)dy + r * ld_dy, ld_dy, xc, xs, uc, us, (T *)dx + r * ld_dx, ld_dx,
+                                                                               (T *)du + r * ld_du, ld_du);
+                else
+                    k_act_backward<K, Y, false><<<grid, PK_THREADS, 0, st>>>(s, (const T *)dy + r * ld_dy, ld_dy, xc, xs, uc, us, (T *)dx + r * ld_dx, ld_dx,
+                                                                                (T *)NULL, 0);
             });
         });
     });

@@ -190,7 +190,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     // Fragments.  Of small ones there is room for a whole step's, read two quarters ahead; of large ones the inner
     // are replaced as they have been used, and the outer of odd quarters have places of their own.
     constexpr int N = WI * WO;  // products of a quarter step
-    constexpr bool DEEP = N <= 4;
+    constexpr bool DEEP = N == 4;
     pr_bf8 in[DEEP ? 4 : 1][WI], outer[DEEP ? 4 : 2][WO];
     pr_f16 acc[WI][WO];
     const bool summing = SUMS && ti == 0 && wi == 0;
@@ -213,9 +213,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     // Step s + 2's gradients are asked for in the SLOTS products behind a meeting; step s + 1's packed values
     // turned from product TURN to TURN_END of a step on.  (Waiting for a packed value the compiler, which does
     // not know of the gradients, waits for those of them that were asked for later too: they have to be old.)
-    // Turned in the second and third quarters instead, dx = dy W4 takes 830 us where this takes 764 (8192 rows,
-    // 16384 -> 4096, all zeros); the many instructions of 8 bits are better spread: 950, and 967 in the third alone.
-    constexpr int SLOTS = 4 * N - MEET, TURN = DEEP ? N : FMT == PP_PACK_INT8 ? 3 * N / 2 : 2 * N, TURN_END = DEEP ? MEET : 3 * N;
+    constexpr int SLOTS = 4 * N - MEET, TURN = DEEP ? N : 2 * N, TURN_END = DEEP ? MEET : 3 * N;
     next_inner(true);
 #pragma unroll
     for (int j = 0; j < PIECES; ++j) load_inner(j);
