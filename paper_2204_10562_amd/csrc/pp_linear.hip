@@ -214,7 +214,7 @@ extern "C" size_t pp_linear_workspace_bytes(int call, int type, int64_t rows, in
     if (call < PP_LINEAR_FORWARD || call > PP_LINEAR_BACKWARD_WEIGHT || bad_layer(type, rows, n_in, n_out)) return 0;
     int shape;
     if (call == PP_LINEAR_FORWARD) {
-        if (rows <= R4_ROWS) return room_forward(NULL, rows, n_in).total;
+        if (r4_takes(rows, n_in, n_out)) return room_forward(NULL, rows, n_in).total;
         const pr_plan p = plan_forward(rows, n_in, n_out, &shape);
         return room_forward(&p, rows, n_in).total;
     }
@@ -239,7 +239,7 @@ extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n
     if (pp_bad_packed(w_codes, w_scales, n_out) || ((uintptr_t)bias & 3)) return PP_ERR_INVALID_ARG;
     if ((x_codes || x_scales) && pp_bad_packed(x_codes, x_scales, rows)) return PP_ERR_INVALID_ARG;
     hipStream_t st = (hipStream_t)stream;
-    const bool few = rows <= R4_ROWS;
+    const bool few = r4_takes(rows, n_in, n_out);
     int shape;
     pr_plan p = {};
     if (!few) p = plan_forward(rows, n_in, n_out, &shape);
@@ -250,7 +250,7 @@ extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n
     const long long g = pp_groups(n_in);
     uint8_t *codes = (uint8_t *)workspace, *scales = codes + room.scales;
     const p4_operands all = {(const uint8_t *)w_codes, (const uint8_t *)w_scales, codes, scales};
-    if (few && r4_fuses(rows, n_in, n_out))
+    if (few && r4_fuses(rows, n_in))
         return r4_launch(type, rows, n_in, n_out, x, ld_x, (uint8_t *)x_codes, (uint8_t *)x_scales, all, y, ld_y, bias, st);
     if (int rc = pp_launch_pack_both(type, rows, n_in, x, ld_x, codes, scales, x_codes, x_scales, st)) return rc;
     if (few) return r4_launch(type, rows, n_in, n_out, x, ld_x, NULL, NULL, all, y, ld_y, bias, st);

@@ -203,7 +203,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
 // that divide the sum among them: a wave takes 16 rows of W and up to eight groups at a time, and what
 // the waves of a workgroup have found is added in LDS.  With FUSED the workgroup also packs x itself
 // (rows of it are little beside 16 rows of W) and, for pp_linear_backward_weight, a part of x in 8 bits.
-#define R4_MAX_WAVES 16
+#define R4_MAX_WAVES(NB) ((NB) == 1 ? 16 : 8)  // 128 registers to a thread, or 256
 struct r4_x {  // FUSED: the matrix; else its codes and scales
     const void *x;
     long long ld, cols;
@@ -212,7 +212,7 @@ struct r4_x {  // FUSED: the matrix; else its codes and scales
 };
 
 template <int NB, bool FUSED, class Y>
-__global__ __launch_bounds__(64 * R4_MAX_WAVES) void k_rows4(int rows, long long inner, int groups, const uint8_t *__restrict__ w_codes,
+__global__ __launch_bounds__(64 * R4_MAX_WAVES(NB)) void k_rows4(int rows, long long inner, int groups, const uint8_t *__restrict__ w_codes,
                                                              const uint8_t *__restrict__ w_scales, r4_x x, pr_out<Y> out) {
     typedef typename Y::T T;
     extern __shared__ uint8_t sm[];  // sums of the waves [NB][waves][64] of 16 bytes; FUSED: x's codes, then its scales
@@ -224,20 +224,21 @@ __global__ __launch_bounds__(64 * R4_MAX_WAVES) void k_rows4(int rows, long long
     const long long n = n0 + r < inner ? n0 + r : inner - 1;
     const uint8_t *wc = w_codes + n * groups * PP_GROUP_CODES4 + 16 * g, *ws = w_scales + n * groups * 4;
 
-    pp_u4 w[8], s4[2];
-    auto load = [&](int k) {
+    // Up to eight groups of a row from p (16 bytes of each) and their scales from q on, none beyond k1.
+    auto load = [&](int k, const uint8_t *p, const uint8_t *q, pp_u4 *c, pp_u4 *s4) {
 #pragma unroll
         for (int t = 0; t < 8; ++t)
-            if (k + t < k1) w[t] = *(const pp_u4 *)(wc + (long long)(k + t) * PP_GROUP_CODES4);
+            if (k + t < k1) c[t] = *(const pp_u4 *)(p + (long long)(k + t) * PP_GROUP_CODES4);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // four groups' scales; one by one where fewer are left
-            if (k + 4 * h + 4 <= k1) s4[h] = ((const pp_any16<4> *)(ws + 4ll * (k + 4 * h)))->v;
+            if (k + 4 * h + 4 <= k1) s4[h] = ((const pp_any16<4> *)(q + 4ll * (k + 4 * h)))->v;
             else
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
-                    if (k + 4 * h + t < k1) s4[h][t] = *(const unsigned *)(ws + 4ll * (k + 4 * h + t));
+                    if (k + 4 * h + t < k1) s4[h][t] = *(const unsigned *)(q + 4ll * (k + 4 * h + t));
         }
     };
+    pp_u4 w[8], w4[2];
     if constexpr (FUSED) {
         const int row_chunks = groups * 16, chunks = rows * row_chunks, threads = blockDim.x;
         const T *src = (const T *)x.x;
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(64 * R4_MAX_WAVES) void k_rows4(int rows, long long
             return pp_load8<Y>(src + row * x.ld + 8 * c, q < chunks ? x.cols - 8ll * c : 0);
         };
         PpRaw<Y> raw = fetch(tid);  // before the weight's: what is waited for first is asked for first
-        load(k0);
+        load(k0, wc, ws, w, w4);
         for (int q = tid; q < chunks; q += threads) {
             const PpRaw<Y> now = raw;
             if (q + threads < chunks) raw = fetch(q + threads);
@@ -266,27 +267,35 @@ __global__ __launch_bounds__(64 * R4_MAX_WAVES) void k_rows4(int rows, long long
         }
         __syncthreads();
     } else {
-        load(k0);
+        load(k0, wc, ws, w, w4);
     }
     pp_f4 acc[NB] = {};
     for (int k = k0; k < k1; k += 8) {
-        if (k > k0) load(k);
+        if (k > k0) load(k, wc, ws, w, w4);
+        // x's, from memory all at once; from LDS as they are needed.  Lanes beyond the last row take it again, for
+        // results that are not written.
+        pp_u4 c[NB][8], c4[NB][2];
+        long long m[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            m[b] = (long long)(16 * b + r < rows ? 16 * b + r : rows - 1) * groups;
+            if constexpr (!FUSED) load(k, x.codes + m[b] * PP_GROUP_CODES4 + 16 * g, x.scales + m[b] * 4, c[b], c4[b]);
+        }
 #pragma unroll
         for (int t = 0; t < 8; ++t) {
             if (k + t >= k1) break;
             const pr_i8 a = {(int)w[t][0], (int)w[t][1], (int)w[t][2], (int)w[t][3]};
-            const int ca = s4[t >> 2][t & 3] >> (8 * g);
+            const int ca = w4[t >> 2][t & 3] >> (8 * g);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const int m = 16 * b + r;
-                pp_u4 c = {0, 0, 0, 0};
-                int cb = 0;
-                if (m < rows) {
-                    const long long at = (long long)m * groups + k + t;
-                    c = *(const pp_u4 *)((FUSED ? xc : x.codes) + at * PP_GROUP_CODES4 + 16 * g);
-                    cb = (FUSED ? xs : x.scales)[at * 4 + g];
+                int cb;
+                if constexpr (FUSED) {
+                    c[b][t] = *(const pp_u4 *)(xc + (m[b] + k + t) * PP_GROUP_CODES4 + 16 * g);
+                    cb = xs[(m[b] + k + t) * 4 + g];
+                } else {
+                    cb = c4[b][t >> 2][t & 3] >> (8 * g);
                 }
-                const pr_i8 d = {(int)c[0], (int)c[1], (int)c[2], (int)c[3]};
+                const pr_i8 d = {(int)c[b][t][0], (int)c[b][t][1], (int)c[b][t][2], (int)c[b][t][3]};
                 acc[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, d, acc[b], 4, 4, 0, ca, 0, cb);
             }
         }
@@ -309,25 +318,28 @@ __global__ __launch_bounds__(64 * R4_MAX_WAVES) void k_rows4(int rows, long long
 
 // Waves to a workgroup: four where the rows of W alone fill the chip, more (down to two groups each)
 // where they do not.
-static int r4_waves(long long inner, long long groups) {
+static int r4_waves(int nb, long long inner, long long groups) {
     int n = 4;
-    while (n < R4_MAX_WAVES && (inner + 15) / 16 * n < 4096 && 2 * n * 2 <= groups) n *= 2;
+    while (n < R4_MAX_WAVES(nb) && (inner + 15) / 16 * n < 4096 && 2 * n * 2 <= groups) n *= 2;
     return n;
 }
 static size_t r4_lds(int nb, int waves, int64_t rows, long long groups, bool fused) {
     return (size_t)nb * waves * 1024 + (fused ? rows * groups * (PP_GROUP_CODES4 + 4) : 0);
 }
 
-// Whether a workgroup packs x itself: few rows, and few enough for LDS.
-bool r4_fuses(int64_t rows, int64_t n_in, int64_t n_out) {
-    return rows <= R4_FUSED_ROWS && r4_lds(1, r4_waves(n_out, pp_groups(n_in)), rows, pp_groups(n_in), true) <= 65536;
-}
+// Whether few rows go this way.  Up to 16 they do; up to 32 where the weight is small: 4096 -> 4096 takes 8 us (12 in
+// tiles of 256 x 32), 4096 -> 16384 19 us (17).  (16 rows: 15 us, and 15.)
+bool r4_takes(int64_t rows, int64_t n_in, int64_t n_out) { return rows <= 16 || (rows <= 32 && n_in * n_out <= 1 << 25); }
+
+// Whether a workgroup packs x itself, which saves a launch and costs every workgroup the same work: up to 64 groups
+// of 128 values.  4096 -> 16384: a row 9.1 us (10.7 in two launches), four rows 13.4 us (11.7).
+bool r4_fuses(int64_t rows, int64_t n_in) { return rows <= 16 && rows * pp_groups(n_in) <= 64; }
 
 int r4_launch(int type, int64_t rows, int64_t n_in, int64_t n_out, const void *x, int64_t ld_x, uint8_t *kept_codes, uint8_t *kept_scales,
               const p4_operands &q, void *y, int64_t ld_y, const float *bias, hipStream_t st) {
     const long long groups = pp_groups(n_in);
-    const int waves = r4_waves(n_out, groups), nb = rows > 16 ? 2 : 1;
-    const bool fused = r4_fuses(rows, n_in, n_out);
+    const int nb = rows > 16 ? 2 : 1, waves = r4_waves(nb, n_out, groups);
+    const bool fused = r4_fuses(rows, n_in);
     const r4_x a = {x, ld_x, n_in, kept_codes, kept_scales, q.outer_codes, q.outer_scales};
     const size_t lds = r4_lds(nb, waves, rows, groups, fused);
     const unsigned grid = (unsigned)((n_out + 15) / 16);
