@@ -15,36 +15,39 @@ int pp_launch_pack_both(int type, int64_t rows, int64_t cols, const void *src, i
 static int planes_of(int type) { return type == PP_TYPE_BF16 ? 1 : type == PP_TYPE_F16 ? 2 : 3; }
 
 template <class Y, int PLANES>
-__global__ __launch_bounds__(256) void k_planes(long long rows, long long cols, const typename Y::T *__restrict__ src, long long ld,
+__global__ __launch_bounds__(256) void k_planes(long long row0, long long rows, long long cols, const typename Y::T *__restrict__ src, long long ld,
                                                 uint16_t *__restrict__ dst, long long ld_dst) {
-    const long long chunks = ld_dst / 8, n = rows * chunks;
-    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < n; t += (long long)gridDim.x * 256) {
-        const long long r = t / chunks, c = (t - r * chunks) * 8;
-        const PpRaw<Y> raw = pp_load8<Y>(src + r * ld + c, cols - c);
-        float v[8];
-        pp_values<Y>(raw, v);
+    const unsigned chunks = (unsigned)(ld_dst / 8), t = blockIdx.x * 256 + threadIdx.x, r_ = t / chunks;
+    const long long r = row0 + r_, c = (t - r_ * chunks) * 8ll;
+    if (r >= rows) return;
+    const PpRaw<Y> raw = pp_load8<Y>(src + r * ld + c, cols - c);
+    float v[8];
+    pp_values<Y>(raw, v);
 #pragma unroll
-        for (int k = 0; k < PLANES; ++k) {
-            unsigned h[8];
+    for (int k = 0; k < PLANES; ++k) {
+        unsigned h[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned b = pp_bits(v[j]);
-                const bool finite = (b & 0x7f800000u) != 0x7f800000u;
-                h[j] = (b >> 16) | ((b & 0x7fffffffu) > 0x7f800000u ? 0x40u : 0u);  // a NaN stays one
-                v[j] = finite ? v[j] - pp_bits(b & 0xffff0000u) : 0.0f;
-            }
-            *(pp_u4 *)(dst + (k * rows + r) * ld_dst + c) = pp_u4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+        for (int j = 0; j < 8; ++j) {
+            const unsigned b = pp_bits(v[j]);
+            const bool finite = (b & 0x7f800000u) != 0x7f800000u;
+            h[j] = (b >> 16) | ((b & 0x7fffffffu) > 0x7f800000u ? 0x40u : 0u);  // a NaN stays one
+            v[j] = finite ? v[j] - pp_bits(b & 0xffff0000u) : 0.0f;
         }
+        *(pp_u4 *)(dst + (k * rows + r) * ld_dst + c) = pp_u4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
     }
 }
 
 static int launch_planes(int type, int64_t rows, int64_t cols, const void *src, int64_t ld, void *dst, int64_t ld_dst, hipStream_t st) {
-    const int64_t blocks = (rows * (ld_dst / 8) + 255) / 256;
-    const unsigned grid = (unsigned)(blocks < 8192 ? blocks : 8192);
-    if (type == PP_TYPE_BF16) k_planes<PpBF16, 1><<<grid, 256, 0, st>>>(rows, cols, (const __bf16 *)src, ld, (uint16_t *)dst, ld_dst);
-    else if (type == PP_TYPE_F16) k_planes<PpF16, 2><<<grid, 256, 0, st>>>(rows, cols, (const _Float16 *)src, ld, (uint16_t *)dst, ld_dst);
-    else k_planes<PpF32, 3><<<grid, 256, 0, st>>>(rows, cols, (const float *)src, ld, (uint16_t *)dst, ld_dst);
-    return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+    const int64_t chunks = ld_dst / 8, most = ((int64_t)1 << 31) / chunks;  // rows of a launch
+    for (int64_t r = 0; r < rows; r += most) {
+        const int64_t n = rows - r < most ? rows - r : most;
+        const unsigned grid = (unsigned)((n * chunks + 255) / 256);
+        if (type == PP_TYPE_BF16) k_planes<PpBF16, 1><<<grid, 256, 0, st>>>(r, rows, cols, (const __bf16 *)src, ld, (uint16_t *)dst, ld_dst);
+        else if (type == PP_TYPE_F16) k_planes<PpF16, 2><<<grid, 256, 0, st>>>(r, rows, cols, (const _Float16 *)src, ld, (uint16_t *)dst, ld_dst);
+        else k_planes<PpF32, 3><<<grid, 256, 0, st>>>(r, rows, cols, (const float *)src, ld, (uint16_t *)dst, ld_dst);
+        if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
+    }
+    return PP_OK;
 }
 
 // ---- pieces of a sum, added in their order
@@ -61,9 +64,11 @@ __global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const fl
         }
         return;
     }
-    const long long chunks = p.partial_ld / 8, n = p.outer * chunks;
-    for (long long t = (blockIdx.x - sum_blocks) * 256ll + threadIdx.x; t < n; t += (gridDim.x - sum_blocks) * 256ll) {
-        const long long o = t / chunks, i = (t - o * chunks) * 8;
+    // (Results of a divided sum are few: 512 tiles at most.)
+    const unsigned chunks = (unsigned)(p.partial_ld / 8), n = (unsigned)p.outer * chunks;
+    for (unsigned t = (blockIdx.x - sum_blocks) * 256 + threadIdx.x; t < n; t += (gridDim.x - sum_blocks) * 256) {
+        const unsigned row = t / chunks;
+        const long long o = row, i = (t - row * chunks) * 8ll;
         const float *q = p.partial + o * p.partial_ld + i;
         pp_f4 a = {0, 0, 0, 0}, b = a;
         int s = 0;
