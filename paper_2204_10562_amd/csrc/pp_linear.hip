@@ -130,8 +130,8 @@ struct pr_shape {
     float alone, full, once;
 };
 static const pr_shape FORWARD[] = {{256, 256, 1, 1.0f, 1.0f, 12.0f}, {128, 128, 2, 0.32f, 0.62f, 6.0f}, {256, 32, 2, 0.36f, 0.5f, 5.0f}};
-static const pr_shape INPUT[] = {{256, 256, 1, 1.5f, 1.7f, 12.0f}, {128, 128, 2, 0.68f, 1.14f, 6.0f}, {256, 32, 2, 0.78f, 1.1f, 5.0f}};
-static const pr_shape WEIGHT[] = {{256, 256, 1, 1.5f, 1.8f, 20.0f}, {128, 128, 2, 1.0f, 1.22f, 8.0f}};
+static const pr_shape INPUT[] = {{256, 256, 1, 1.5f, 1.7f, 12.0f}, {128, 128, 2, 0.68f, 1.14f, 7.0f}, {256, 32, 2, 0.78f, 1.1f, 5.0f}, {256, 128, 1, 0.82f, 0.9f, 8.0f}};
+static const pr_shape WEIGHT[] = {{256, 256, 1, 1.5f, 1.8f, 20.0f}, {128, 128, 2, 1.0f, 1.22f, 8.0f}, {128, 256, 1, 0.95f, 1.03f, 12.0f}};
 #define PR_CUS 256
 
 // The shape and the number of pieces with the least estimated time: rounds of workgroups over the chip, and
@@ -187,10 +187,10 @@ template <class F> static int in_turns(const pr_plan &p, int to, F launch) {
 
 static pr_plan plan_forward(int64_t rows, int64_t n_in, int64_t n_out, int *shape) { return plan(FORWARD, 3, n_out, rows, pp_groups(n_in), 68, 68, shape); }
 static pr_plan plan_input(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(INPUT, 3, n_in, rows, planes_of(type) * ((n_out + 63) / 64), 34, 128, shape);
+    return plan(INPUT, 4, n_in, rows, planes_of(type) * ((n_out + 63) / 64), 34, 128, shape);
 }
 static pr_plan plan_weight(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(WEIGHT, 2, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), 66, 128, shape);
+    return plan(WEIGHT, 3, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), 66, 128, shape);
 }
 
 // ---- entry points

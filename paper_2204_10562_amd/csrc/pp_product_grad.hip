@@ -346,10 +346,12 @@ static int launch_weight(const pr_plan &p, const pg_inner &x, const pg_outer &y,
 int pg_launch_input(int shape, int type, const pr_plan &p, const pg_inner &w, const pg_outer &dy, void *dx, long long ld, hipStream_t st) {
     if (shape == 0) return launch_input<4, 2, 2, 4>(type, p, w, dy, dx, ld, st);
     if (shape == 1) return launch_input<2, 2, 2, 2>(type, p, w, dy, dx, ld, st);
-    return launch_input<2, 1, 4, 1>(type, p, w, dy, dx, ld, st);
+    if (shape == 2) return launch_input<2, 1, 4, 1>(type, p, w, dy, dx, ld, st);
+    return launch_input<2, 2, 4, 2>(type, p, w, dy, dx, ld, st);
 }
 
 int pg_launch_weight(int shape, const pr_plan &p, const pg_inner &x, const pg_outer &dy, float *dw, long long ld, const float *add, float *sums, hipStream_t st) {
     if (shape == 0) return launch_weight<4, 2, 2, 4>(p, x, dy, dw, ld, add, sums, st);
-    return launch_weight<2, 2, 2, 2>(p, x, dy, dw, ld, add, sums, st);
+    if (shape == 1) return launch_weight<2, 2, 2, 2>(p, x, dy, dw, ld, add, sums, st);
+    return launch_weight<2, 2, 2, 4>(p, x, dy, dw, ld, add, sums, st);
 }
