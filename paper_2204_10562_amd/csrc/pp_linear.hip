@@ -58,11 +58,18 @@ static int launch_planes(int type, int64_t rows, int64_t cols, const void *src, 
 // The first `sum_blocks` workgroups add the columns' sums.
 template <class Y>
 __global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const float *__restrict__ part_sums, float *__restrict__ sums, unsigned sum_blocks) {
-    if (blockIdx.x < sum_blocks) {
-        const long long o = blockIdx.x * 256ll + threadIdx.x;
+    if (blockIdx.x < sum_blocks) {  // 32 sums, their parts by eight threads each
+        __shared__ float found[8][32];
+        const int lane = threadIdx.x & 31, eighth = threadIdx.x >> 5, parts = p.splits * (int)p.ni;
+        const long long o = blockIdx.x * 32ll + lane;
         float v = 0;
-        if (o < p.outer) {
-            for (int s = 0; s < p.splits; ++s) v += part_sums[s * p.outer + o];
+        if (o < p.outer)
+#pragma unroll 4
+            for (int s = eighth; s < parts; s += 8) v += part_sums[s * p.outer + o];
+        found[eighth][lane] = v;
+        __syncthreads();
+        if (eighth == 0 && o < p.outer) {
+            for (int k = 1; k < 8; ++k) v += found[k][lane];
             sums[o] = v;
         }
         return;
@@ -109,7 +116,7 @@ __global__ __launch_bounds__(256) void k_join(pr_plan p, pr_out<Y> out, const fl
 static int launch_join(int type, const pr_plan &p, void *out, long long ld, const float *bias, const float *add, const float *part_sums, float *sums,
                        hipStream_t st) {
     const long long blocks = (p.outer * (p.partial_ld / 8) + 255) / 256;
-    const unsigned sum_blocks = sums ? (unsigned)((p.outer + 255) / 256) : 0;
+    const unsigned sum_blocks = sums ? (unsigned)((p.outer + 31) / 32) : 0;
     return pp_by_type(type, [&](auto t) {
         typedef decltype(t) Y;
         k_join<Y><<<sum_blocks + (unsigned)(blocks < 4096 ? blocks : 4096), 256, 0, st>>>(p, pr_out<Y>{(typename Y::T *)out, ld, bias, add, ld}, part_sums, sums, sum_blocks);
@@ -122,9 +129,10 @@ static int launch_join(int type, const pr_plan &p, void *out, long long ld, cons
 // A tile shape: results; microseconds of a step where a compute unit has one workgroup of it and where
 // it has as many as fit; how many fit; microseconds of a workgroup's start and end.  Measured: one step of
 // the sum is 128 values forward and 64 in the backward products.  The estimates below choose what is within
-// 7 % of the best of all shapes and numbers of pieces on 24 sizes from 16 to 32771 rows, within 4 % on 18.  The flat shapes are for few rows: 50 rows, 4096 -> 4096 forward 12.8 us (14.1 in tiles of
-// 128 x 128, 25.5 of 256 x 256, each with its best number of pieces); the large ones from a few hundred
-// tiles on: dx of 4000 rows, 500 -> 4000 33.7 us (36.0 in the middle one).
+// 9 % of the best of all shapes and numbers of pieces on 31 sizes from 16 to 32771 rows, within 4 % on 22.
+// The flat shapes are for few rows: 50 rows, 4096 -> 4096 forward 12.8 us (14.1 in tiles of 128 x 128, 25.5 of
+// 256 x 256, each with its best number of pieces); the large ones for many: dx of 4000 rows, 500 -> 4000 33 us (36
+// in 128 x 128); for those between see the kernels.
 struct pr_shape {
     int ti, to, fit;
     float alone, full, once;
@@ -217,7 +225,7 @@ static pr_room room_backward(const pr_plan &p, int type, int64_t rows, int64_t n
     pr_room r = {};
     r.partial = planes_bytes(type, rows, n_out);
     r.sums = r.partial + pp_align256(partial_bytes(p));
-    r.total = 256 + r.sums + (sums ? pp_align256((size_t)p.splits * n_out * 4) : 0);
+    r.total = 256 + r.sums + (sums ? pp_align256((size_t)p.splits * p.ni * n_out * 4) : 0);
     return r;
 }
 

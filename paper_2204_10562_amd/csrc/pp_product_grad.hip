@@ -12,10 +12,11 @@
 // (1.1 TFLOP) take 860 us for dx, 1.28 PFLOP/s (the library's product of two bf16 matrices of 8192 reaches
 // 1.2 to 1.4), and 1080 us for dw, whose 0.8 GB of results and of what they are added to come on top; 727 and
 // 952 us of zeros: power first.  (Four waves with sixteen fragments each have no registers left for
-// what is on its way.)  Tiles of 128 x 128, two workgroups to a compute unit, are bound by instruction issue:
-// 16 products to about 190 other instructions (250 of 8 bits) a step.  333 rows, 5000 -> 4100 from fp16, two
-// planes, in five pieces: 44 us; dw of 32771 rows, 520 -> 1000, in twelve: 65 us, 0.5 PFLOP/s.  256 x 32 is for
-// few rows of dy: 16 rows, 16384 -> 4096 takes 16 us.
+// what is on its way.)  Smaller tiles are bound by instruction issue: 16 products to 170 or 190 other instructions
+// (200 or 250 of 8 bits) a step and wave.  256 x 128 for dx and 128 x 256 for dw, eight waves, turn a packed value for
+// twice as many products as 128 x 128 with two workgroups to a compute unit, which wastes less where there are few.
+// 333 rows, 5000 -> 4100 from fp16, two planes, in four pieces: 40 us (44 in 128 x 128); dw and db of 32771 rows,
+// 520 -> 1000, in twelve: 61 us, 0.56 PFLOP/s (65).  256 x 32 is for few rows of dy: 16 rows, 16384 -> 4096 takes 16 us.
 #include "pp_product_grad.h"
 
 // WI x WO fragments of 32 x 32 to a wave, NI x NO waves
@@ -205,8 +206,11 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     constexpr bool DEEP = N == 4;
     pr_bf8 in[DEEP ? 4 : 1][WI], outer[DEEP ? 4 : 2][WO];
     pr_f16 acc[WI][WO];
-    const bool summing = SUMS && ti == 0 && wi == 0;
-    // The columns' sums, by the waves that have them all: a lane's eight rows by pairs, in 32 bits.
+    // The columns' sums: a lane's eight rows by pairs, in 32 bits.  In one piece the first tile of a row of tiles adds
+    // them all up, in several pieces its tiles take the steps in turn (what one of them adds keeps the others waiting:
+    // dw of 32771 rows, 520 -> 1000, 65 us with the first alone, 61 in turn), and k_join adds what they found.
+    const bool in_turn = p.splits > 1;
+    int until = wi ? 0x7fffffff : in_turn || ti == 0 ? (int)ti : 0x7fffffff;  // steps until this wave's next
     float total[SUMS ? WO : 1] = {};
     auto add_up = [&](const pr_bf8 *f) {
 #pragma unroll
@@ -270,7 +274,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
             const pr_bf8 *f = in[DEEP ? k : 0], *o = outer[DEEP ? k : k & 1];
             const int ahead = DEEP ? (k + 2) & 3 : (k + 1) & 3;  // the quarter read meanwhile
             const uint8_t *b = k < (DEEP ? 2 : 3) ? now : next;  // after the last step: what lies there, for nothing
-            if (SUMS && summing) add_up(o);
+            if (SUMS && until == 0) add_up(o);
             if (k == TURN / N) next_inner(s + 2 < steps);
 #pragma unroll
             for (int m = 0; m < N; ++m) {
@@ -305,17 +309,19 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
                 PR_PIN;
             }
         }
+        if (SUMS) until = until ? until - 1 : in_turn ? (int)p.ni - 1 : 0;
         pr_settle(s + 1, steps);
     }
     PR_WAIT(0);  // nothing is on its way to LDS any more
     pr_barrier();
     if constexpr (SUMS)
-        if (summing) {
+        if (wi == 0 && (in_turn || ti == 0)) {
+            float *part = sums + (in_turn ? ((long long)piece * p.ni + ti) * p.outer : 0);
 #pragma unroll
             for (int j = 0; j < WO; ++j) {
                 const float v = total[j] + __shfl_xor(total[j], 32);
                 const long long o = o0 + (wo * WO + j) * 32 + r;
-                if (g == 0 && o < p.outer) sums[piece * p.outer + o] = v;
+                if (g == 0 && o < p.outer) part[o] = v;
             }
         }
     pr_leave<Y, WI, WO>(p, out, acc, sm + wave * (32 * 32 * WI * 4), lane, i0 + wi * WI * 32, o0 + wo * WO * 32, piece);
