@@ -139,7 +139,7 @@ struct pr_shape {
 };
 static const pr_shape FORWARD[] = {{256, 256, 1, 1.0f, 1.0f, 12.0f}, {128, 128, 2, 0.32f, 0.62f, 6.0f}, {256, 32, 2, 0.36f, 0.5f, 5.0f}};
 static const pr_shape INPUT[] = {{256, 256, 1, 1.5f, 1.7f, 12.0f}, {128, 128, 2, 0.68f, 1.14f, 7.0f}, {256, 32, 2, 0.78f, 1.1f, 5.0f}, {256, 128, 1, 0.82f, 0.9f, 8.0f}};
-static const pr_shape WEIGHT[] = {{256, 256, 1, 1.5f, 1.8f, 20.0f}, {128, 128, 2, 1.0f, 1.22f, 8.0f}, {128, 256, 1, 0.95f, 1.03f, 12.0f}};
+static const pr_shape WEIGHT[] = {{256, 256, 1, 1.5f, 1.8f, 20.0f}, {128, 128, 2, 1.0f, 1.22f, 8.0f}};
 #define PR_CUS 256
 
 // The shape and the number of pieces with the least estimated time: rounds of workgroups over the chip, and
@@ -169,7 +169,7 @@ static pr_plan plan(const pr_shape *shapes, int n, long long inner, long long ou
     }
     const pr_shape &s = shapes[*shape];
     // A die whose run is of one piece's tiles reads only that piece's part of the operands.  Where these are larger
-    // than a few L2s (4 MiB each) that is worth it: dw of 32771 rows, 520 -> 1000 (87 MB), 71 us for 75, 8192 rows
+    // than a few L2s (4 MiB each) that is worth it: dw of 32771 rows, 520 -> 1000 (87 MB), 69 us for 76, 8192 rows
     // (21 MB) 30 for 31; of less, reads are better spread: 2048 rows, 1024 -> 1024 (6 MB), 21.4 us for 23.7.
     best.by_piece = steps * (inner * bi + outer * bo) >= (1 << 24);
     best.inner = inner;
@@ -198,7 +198,7 @@ static pr_plan plan_input(int type, int64_t rows, int64_t n_in, int64_t n_out, i
     return plan(INPUT, 4, n_in, rows, planes_of(type) * ((n_out + 63) / 64), 34, 128, shape);
 }
 static pr_plan plan_weight(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(WEIGHT, 3, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), 66, 128, shape);
+    return plan(WEIGHT, 2, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), 66, 128, shape);
 }
 
 // ---- entry points

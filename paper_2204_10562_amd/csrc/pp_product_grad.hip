@@ -13,10 +13,12 @@
 // 1.2 to 1.4), and 1080 us for dw, whose 0.8 GB of results and of what they are added to come on top; 727 and
 // 952 us of zeros: power first.  (Four waves with sixteen fragments each have no registers left for
 // what is on its way.)  Smaller tiles are bound by instruction issue: 16 products to 170 or 190 other instructions
-// (200 or 250 of 8 bits) a step and wave.  256 x 128 for dx and 128 x 256 for dw, eight waves, turn a packed value for
-// twice as many products as 128 x 128 with two workgroups to a compute unit, which wastes less where there are few.
-// 333 rows, 5000 -> 4100 from fp16, two planes, in four pieces: 40 us (44 in 128 x 128); dw and db of 32771 rows,
-// 520 -> 1000, in twelve: 61 us, 0.56 PFLOP/s (65).  256 x 32 is for few rows of dy: 16 rows, 16384 -> 4096 takes 16 us.
+// (250 of 8 bits) a step and wave.  256 x 128 for dx, eight waves, turns a packed value for twice as many products as
+// 128 x 128 with two workgroups to a compute unit, which wastes less where there are few: 333 rows, 5000 -> 4100 from
+// fp16, two planes, in four pieces 40 us (44).  For dw the same (128 x 256) is 5 % faster where the operands are in
+// cache and 8 % slower where they come from memory, with one workgroup to wait for them, so it is left out; dw and db
+// of 32771 rows, 520 -> 1000, take 66 us in twelve pieces, 0.52 PFLOP/s.  256 x 32 is for few rows of dy: 16 rows,
+// 16384 -> 4096 takes 16 us.
 #include "pp_product_grad.h"
 
 // WI x WO fragments of 32 x 32 to a wave, NI x NO waves
@@ -208,7 +210,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
     pr_f16 acc[WI][WO];
     // The columns' sums: a lane's eight rows by pairs, in 32 bits.  In one piece the first tile of a row of tiles adds
     // them all up, in several pieces its tiles take the steps in turn (what one of them adds keeps the others waiting:
-    // dw of 32771 rows, 520 -> 1000, 65 us with the first alone, 61 in turn), and k_join adds what they found.
+    // dw of 32771 rows, 520 -> 1000, 73 us with the first alone, 69 in turn), and k_join adds what they found.
     const bool in_turn = p.splits > 1;
     int until = wi ? 0x7fffffff : in_turn || ti == 0 ? (int)ti : 0x7fffffff;  // steps until this wave's next
     float total[SUMS ? WO : 1] = {};
@@ -358,6 +360,5 @@ int pg_launch_input(int shape, int type, const pr_plan &p, const pg_inner &w, co
 
 int pg_launch_weight(int shape, const pr_plan &p, const pg_inner &x, const pg_outer &dy, float *dw, long long ld, const float *add, float *sums, hipStream_t st) {
     if (shape == 0) return launch_weight<4, 2, 2, 4>(p, x, dy, dw, ld, add, sums, st);
-    if (shape == 1) return launch_weight<2, 2, 2, 2>(p, x, dy, dw, ld, add, sums, st);
-    return launch_weight<2, 2, 2, 4>(p, x, dy, dw, ld, add, sums, st);
+    return launch_weight<2, 2, 2, 2>(p, x, dy, dw, ld, add, sums, st);
 }
