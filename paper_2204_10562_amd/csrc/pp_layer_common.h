@@ -26,7 +26,6 @@ static inline bool pp_bad_sizes(int type, int64_t rows, int64_t cols) {
 }
 
 typedef __bf16 pp_bf2 __attribute__((ext_vector_type(2)));
-typedef _Float16 pp_h2 __attribute__((ext_vector_type(2)));
 typedef float pp_f2 __attribute__((ext_vector_type(2)));
 typedef float pp_f4 __attribute__((ext_vector_type(4)));
 typedef int pp_i4 __attribute__((ext_vector_type(4)));
