@@ -10,7 +10,8 @@ int pp_launch_pack_both(int type, int64_t rows, int64_t cols, const void *src, i
 // ---- gradients as bf16 planes
 
 // dy in a form the product can load as it is: rows at multiples of 16 bytes, in bf16.  A type with
-// more bits becomes two (f16) or three (float) planes that add up to it exactly, each the leading
+// more bits becomes two (f16) or three (float) planes that add up to it (but for what a float has below 2^-133,
+// bf16's smallest value), each the leading
 // eight bits of what the ones before leave; products with all of them are summed.  Bound by its bytes and the
 // launch: 333 x 5000 fp16 (10 MB) 4.5 us.  (fp16 products would need the packed values in fp16, which does not
 // hold all of their scales.)
