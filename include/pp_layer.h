@@ -89,8 +89,11 @@ int pp_act_backward(int kind, int type, int64_t rows, int64_t cols, const void *
 /*
  * The linear layer y = x W^T + b with its weight W [n_out][n_in] packed with PP_PACK_FP4.
  * pp_linear_workspace_bytes: bytes of workspace that the call of this kind needs (host function;
- * 0 if a size or the type is out of range).  What a type needs serves the types of fewer bits too.
- * The workspace must be 256-byte aligned; its contents need not be kept.
+ * 0 if a size or the type is out of range).  What a type needs serves the types of fewer bits too, and
+ * what so many rows need serves fewer.  (Fewer rows may want more bytes, for the partial sums of a sum
+ * that is divided into more pieces: a call divides its sum as its workspace allows, so with less than
+ * it asks for its results may be rounded otherwise, and it may take longer.  From these bytes on, more
+ * change nothing.)  The workspace must be 256-byte aligned; its contents need not be kept.
  */
 #define PP_LINEAR_FORWARD 0
 #define PP_LINEAR_BACKWARD_INPUT 1

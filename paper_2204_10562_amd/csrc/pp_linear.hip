@@ -15,8 +15,6 @@ int pp_launch_pack_both(int type, int64_t rows, int64_t cols, const void *src, i
 // eight bits of what the ones before leave; products with all of them are summed.  Bound by its bytes and the
 // launch: 333 x 5000 fp16 (10 MB) 4.5 us.  (fp16 products would need the packed values in fp16, which does not
 // hold all of their scales.)
-static int planes_of(int type) { return type == PP_TYPE_BF16 ? 1 : type == PP_TYPE_F16 ? 2 : 3; }
-
 template <class Y, int PLANES>
 __global__ __launch_bounds__(256) void k_planes(long long row0, long long rows, long long cols, const typename Y::T *__restrict__ src, long long ld,
                                                 uint16_t *__restrict__ dst, long long ld_dst) {
@@ -125,62 +123,7 @@ static int launch_join(int type, const pr_plan &p, void *out, long long ld, cons
     });
 }
 
-// ---- how work is divided
-
-// A tile shape: results; microseconds of a step where a compute unit has one workgroup of it and where
-// it has as many as fit; how many fit; microseconds of a workgroup's start and end.  Measured: one step of
-// the sum is 128 values forward and 64 in the backward products.  The estimates below choose what is within
-// 9 % of the best of all shapes and numbers of pieces on 31 sizes from 16 to 32771 rows, within 4 % on 22.
-// The flat shapes are for few rows: 50 rows, 4096 -> 4096 forward 12.8 us (14.1 in tiles of 128 x 128, 25.5 of
-// 256 x 256, each with its best number of pieces); the large ones for many: dx of 4000 rows, 500 -> 4000 33 us (36
-// in 128 x 128); for those between see the kernels.
-struct pr_shape {
-    int ti, to, fit;
-    float alone, full, once;
-};
-static const pr_shape FORWARD[] = {{256, 256, 1, 1.0f, 1.0f, 12.0f}, {128, 128, 2, 0.32f, 0.62f, 6.0f}, {256, 32, 2, 0.36f, 0.5f, 5.0f}};
-static const pr_shape INPUT[] = {{256, 256, 1, 1.5f, 1.7f, 12.0f}, {128, 128, 2, 0.68f, 1.14f, 7.0f}, {256, 32, 2, 0.78f, 1.1f, 5.0f}, {256, 128, 1, 0.82f, 0.9f, 8.0f}};
-static const pr_shape WEIGHT[] = {{256, 256, 1, 1.5f, 1.8f, 20.0f}, {128, 128, 2, 1.0f, 1.22f, 8.0f}};
-#define PR_CUS 256
-
-// The shape and the number of pieces with the least estimated time: rounds of workgroups over the chip, and
-// for more than one piece the pass that adds them (a launch, and each partial sum written and read).
-// bi, bo: bytes of a step of the operands to an inner and an outer index.
-static pr_plan plan(const pr_shape *shapes, int n, long long inner, long long outer, long long steps, int bi, int bo, int *shape) {
-    pr_plan best = {};
-    float least = 0;
-    for (int k = 0; k < n; ++k) {
-        const pr_shape &s = shapes[k];
-        const long long tiles = ((inner + s.ti - 1) / s.ti) * ((outer + s.to - 1) / s.to);
-        for (int pieces = 1; pieces <= 32 && pieces <= steps; ++pieces) {
-            const long long per = (steps + pieces - 1) / pieces, work = tiles * pieces;
-            if (pieces > 1 && ((steps + per - 1) / per != pieces || tiles > PR_CUS * s.fit)) continue;
-            const long long rounds = work / (PR_CUS * s.fit), rest = work - rounds * PR_CUS * s.fit;
-            float t = (float)rounds * ((float)per * s.full + s.once);
-            if (rest) t += (float)per * (rest > PR_CUS ? s.full : s.alone) + s.once;
-            if (pieces > 1) t += 4.0f + (float)pieces * (0.25f + (float)(inner * outer) * 8.0f / 1.0e7f);
-            if (!best.splits || t < least) {
-                least = t;
-                *shape = k;
-                best.steps = (int)steps;
-                best.per = (int)per;
-                best.splits = pieces;
-            }
-        }
-    }
-    const pr_shape &s = shapes[*shape];
-    // A die whose run is of one piece's tiles reads only that piece's part of the operands.  Where these are larger
-    // than a few L2s (4 MiB each) that is worth it: dw of 32771 rows, 520 -> 1000 (87 MB), 69 us for 76, 8192 rows
-    // (21 MB) 30 for 31; of less, reads are better spread: 2048 rows, 1024 -> 1024 (6 MB), 21.4 us for 23.7.
-    best.by_piece = steps * (inner * bi + outer * bo) >= (1 << 24);
-    best.inner = inner;
-    best.outer = outer;
-    best.ni = (unsigned)((inner + s.ti - 1) / s.ti);
-    best.no = (unsigned)((outer + s.to - 1) / s.to);
-    best.partial_ld = (inner + 7) & ~7ll;
-    return best;
-}
-static size_t partial_bytes(const pr_plan &p) { return p.splits > 1 ? (size_t)p.splits * p.outer * p.partial_ld * 4 : 0; }
+// ---- launches and workspaces
 
 // Runs launch(part, first outer index) over the outer index in launches of at most 2^20 tiles.
 template <class F> static int in_turns(const pr_plan &p, int to, F launch) {
@@ -194,14 +137,6 @@ template <class F> static int in_turns(const pr_plan &p, int to, F launch) {
     return PP_OK;
 }
 
-static pr_plan plan_forward(int64_t rows, int64_t n_in, int64_t n_out, int *shape) { return plan(FORWARD, 3, n_out, rows, pp_groups(n_in), 68, 68, shape); }
-static pr_plan plan_input(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(INPUT, 4, n_in, rows, planes_of(type) * ((n_out + 63) / 64), 34, 128, shape);
-}
-static pr_plan plan_weight(int type, int64_t rows, int64_t n_in, int64_t n_out, int *shape) {
-    return plan(WEIGHT, 2, n_in, n_out, planes_of(type) * (rows ? (rows + 63) / 64 : 1), 66, 128, shape);
-}
-
 // ---- entry points
 
 static bool bad_layer(int type, int64_t rows, int64_t n_in, int64_t n_out) {
@@ -211,45 +146,33 @@ static bool bad_layer(int type, int64_t rows, int64_t n_in, int64_t n_out) {
 static int64_t planes_ld(int64_t n_out) { return (n_out + 7) & ~(int64_t)7; }
 static size_t planes_bytes(int type, int64_t rows, int64_t n_out) { return pp_align256((size_t)planes_of(type) * rows * planes_ld(n_out) * 2); }
 
-// What a call keeps in its workspace: places of its parts, and the whole.
-struct pr_room {
-    size_t scales, partial, sums, total;
-};
-static pr_room room_forward(const pr_plan *p, int64_t rows, int64_t n_in) {
-    pr_room r = {};
-    r.scales = pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4);
-    r.partial = r.scales + pp_align256((size_t)rows * pp_groups(n_in) * 4);
-    r.total = 256 + r.partial + (p ? pp_align256(partial_bytes(*p)) : 0);
-    return r;
-}
-static pr_room room_backward(const pr_plan &p, int type, int64_t rows, int64_t n_out, bool sums) {
-    pr_room r = {};
-    r.partial = planes_bytes(type, rows, n_out);
-    r.sums = r.partial + pp_align256(partial_bytes(p));
-    r.total = 256 + r.sums + (sums ? pp_align256((size_t)p.splits * p.ni * n_out * 4) : 0);
-    return r;
+// What a call keeps in its workspace: first x packed in 4 bits, or dy's planes, whose bytes grow with the rows; behind
+// them, where the sum is divided, the partial sums and the columns'.
+static size_t codes_bytes(int64_t rows, int64_t n_in) { return pp_align256((size_t)rows * pp_groups(n_in) * PP_GROUP_CODES4); }
+static size_t packed_bytes(int64_t rows, int64_t n_in) { return codes_bytes(rows, n_in) + pp_align256((size_t)rows * pp_groups(n_in) * 4); }
+static size_t total_bytes(size_t first, const pr_plan &p, bool sums) {
+    return 256 + first + partial_bytes(p.splits, p.inner, p.outer) + (sums ? sums_bytes(p.splits, p.ni, p.outer) : 0);
 }
 
 extern "C" size_t pp_linear_workspace_bytes(int call, int type, int64_t rows, int64_t n_in, int64_t n_out) {
     if (call < PP_LINEAR_FORWARD || call > PP_LINEAR_BACKWARD_WEIGHT || bad_layer(type, rows, n_in, n_out)) return 0;
     int shape;
     if (call == PP_LINEAR_FORWARD) {
-        if (r4_takes(rows, n_in, n_out)) return room_forward(NULL, rows, n_in).total;
-        const pr_plan p = plan_forward(rows, n_in, n_out, &shape);
-        return room_forward(&p, rows, n_in).total;
+        if (r4_takes(rows, n_in, n_out)) return 256 + packed_bytes(rows, n_in);
+        return total_bytes(packed_bytes(rows, n_in), plan_forward(rows, n_in, n_out, PR_ANY_ROOM, &shape), false);
     }
     // what the types of as many bits or fewer need: the work may be divided otherwise for them
     size_t most = 0;
     for (int t = type; t <= PP_TYPE_BF16; ++t) {
         const bool weight = call == PP_LINEAR_BACKWARD_WEIGHT;
-        const pr_plan p = weight ? plan_weight(t, rows, n_in, n_out, &shape) : plan_input(t, rows, n_in, n_out, &shape);
-        const size_t n = room_backward(p, t, rows, n_out, weight).total;
+        const pr_plan p = weight ? plan_weight(t, rows, n_in, n_out, PR_ANY_ROOM, &shape) : plan_input(t, rows, n_in, n_out, PR_ANY_ROOM, &shape);
+        const size_t n = total_bytes(planes_bytes(t, rows, n_out), p, weight);
         most = n > most ? n : most;
     }
     return most;
 }
 
-static bool bad_workspace(const void *ws, size_t bytes, const pr_room &r) { return !ws || ((uintptr_t)ws & 255) || bytes < r.total; }
+static bool bad_workspace(const void *ws, size_t bytes, size_t first) { return !ws || ((uintptr_t)ws & 255) || bytes < 256 + first; }
 
 extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n_out, const void *x, int64_t ld_x, const void *w_codes,
                                  const void *w_scales, const float *bias, void *y, int64_t ld_y, void *x_codes, void *x_scales,
@@ -260,21 +183,21 @@ extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n
     if ((x_codes || x_scales) && pp_bad_packed(x_codes, x_scales, rows)) return PP_ERR_INVALID_ARG;
     hipStream_t st = (hipStream_t)stream;
     const bool few = r4_takes(rows, n_in, n_out);
-    int shape;
-    pr_plan p = {};
-    if (!few) p = plan_forward(rows, n_in, n_out, &shape);
-    const pr_room room = room_forward(few ? NULL : &p, rows, n_in);
-    if (bad_workspace(workspace, workspace_bytes, room)) return PP_ERR_WORKSPACE;
+    const size_t packed = packed_bytes(rows, n_in);
+    if (bad_workspace(workspace, workspace_bytes, packed)) return PP_ERR_WORKSPACE;
     if (!rows) return PP_OK;
     if (rows == 1) ld_x = n_in;
+    int shape;
+    pr_plan p = {};
+    if (!few) p = plan_forward(rows, n_in, n_out, workspace_bytes - 256 - packed, &shape);
     const long long g = pp_groups(n_in);
-    uint8_t *codes = (uint8_t *)workspace, *scales = codes + room.scales;
+    uint8_t *codes = (uint8_t *)workspace, *scales = codes + codes_bytes(rows, n_in);
     const p4_operands all = {(const uint8_t *)w_codes, (const uint8_t *)w_scales, codes, scales};
     if (few && r4_fuses(rows, n_in))
         return r4_launch(type, rows, n_in, n_out, x, ld_x, (uint8_t *)x_codes, (uint8_t *)x_scales, all, y, ld_y, bias, st);
     if (int rc = pp_launch_pack_both(type, rows, n_in, x, ld_x, codes, scales, x_codes, x_scales, st)) return rc;
     if (few) return r4_launch(type, rows, n_in, n_out, x, ld_x, NULL, NULL, all, y, ld_y, bias, st);
-    p.partial = (float *)((uint8_t *)workspace + room.partial);
+    p.partial = (float *)((uint8_t *)workspace + packed);
     const int rc = in_turns(p, FORWARD[shape].to, [&](const pr_plan &q, long long o) {
         return p4_launch(shape, type, q, p4_operands{all.inner_codes, all.inner_scales, codes + o * g * PP_GROUP_CODES4, scales + o * g * 4},
                          (uint8_t *)y + o * ld_y * pp_type_size(type), ld_y, bias, st);
@@ -302,15 +225,15 @@ extern "C" int pp_linear_backward_input(int type, int64_t rows, int64_t n_in, in
     if (bad_layer(type, rows, n_in, n_out)) return PP_ERR_INVALID_ARG;
     if (pp_bad_matrix(dy, type, rows, n_out, ld_dy) || pp_bad_matrix(dx, type, rows, n_in, ld_dx)) return PP_ERR_INVALID_ARG;
     if (pp_bad_packed(w_codes, w_scales, n_out)) return PP_ERR_INVALID_ARG;
-    int shape;
-    pr_plan p = plan_input(type, rows, n_in, n_out, &shape);
-    const pr_room room = room_backward(p, type, rows, n_out, false);
-    if (bad_workspace(workspace, workspace_bytes, room)) return PP_ERR_WORKSPACE;
+    const size_t planes = planes_bytes(type, rows, n_out);
+    if (bad_workspace(workspace, workspace_bytes, planes)) return PP_ERR_WORKSPACE;
     if (!rows) return PP_OK;
+    int shape;
+    pr_plan p = plan_input(type, rows, n_in, n_out, workspace_bytes - 256 - planes, &shape);
     hipStream_t st = (hipStream_t)stream;
     pg_outer y;
     if (int rc = outer_of(type, true, rows, n_out, dy, ld_dy, workspace, &y, st)) return rc;
-    p.partial = (float *)((uint8_t *)workspace + room.partial);
+    p.partial = (float *)((uint8_t *)workspace + planes);
     const pg_inner w = {(const uint8_t *)w_codes, (const uint8_t *)w_scales, n_out, pp_groups(n_in)};
     const int rc = in_turns(p, INPUT[shape].to, [&](const pr_plan &q, long long o) {
         pg_outer part = y;
@@ -330,15 +253,15 @@ extern "C" int pp_linear_backward_weight(int type, int64_t rows, int64_t n_in, i
     if (pp_bad_matrix(dw, PP_TYPE_F32, n_out, n_in, ld_dw) || ((uintptr_t)dw_in & 3) || ((uintptr_t)db & 3)) return PP_ERR_INVALID_ARG;
     if (dw_in && n_out > 1 && ld_dw > PP_LAYER_MAX_LD_DW) return PP_ERR_INVALID_ARG;
     if (n_out == 1) ld_dw = n_in;
+    const size_t planes = planes_bytes(type, rows, n_out);
+    if (bad_workspace(workspace, workspace_bytes, planes)) return PP_ERR_WORKSPACE;
     int shape;
-    pr_plan p = plan_weight(type, rows, n_in, n_out, &shape);
-    const pr_room room = room_backward(p, type, rows, n_out, true);
-    if (bad_workspace(workspace, workspace_bytes, room)) return PP_ERR_WORKSPACE;
+    pr_plan p = plan_weight(type, rows, n_in, n_out, workspace_bytes - 256 - planes, &shape);
     hipStream_t st = (hipStream_t)stream;
     pg_outer y;
     if (int rc = outer_of(type, false, rows, n_out, dy, ld_dy, workspace, &y, st)) return rc;
-    p.partial = (float *)((uint8_t *)workspace + room.partial);
-    float *part_sums = (float *)((uint8_t *)workspace + room.sums);
+    p.partial = (float *)((uint8_t *)workspace + planes);
+    float *part_sums = (float *)((uint8_t *)p.partial + partial_bytes(p.splits, p.inner, p.outer));
     const pg_inner x = {(const uint8_t *)x_codes, (const uint8_t *)x_scales, rows, pp_groups(n_in)};
     const int rc = in_turns(p, WEIGHT[shape].to, [&](const pr_plan &q, long long o) {
         pg_outer part = y;

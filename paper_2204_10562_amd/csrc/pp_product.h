@@ -7,6 +7,7 @@
 #pragma once
 
 #include "pp_layer_common.h"
+#include "pp_linear_plan.h"
 
 #define PR_PIN __builtin_amdgcn_sched_barrier(0)  // instructions stay on their side
 #define PR_STEP 64  // bytes of a row of 4-bit values to a step: 128 of them
@@ -15,19 +16,6 @@ typedef int pr_i8 __attribute__((ext_vector_type(8)));
 typedef __bf16 pr_bf8 __attribute__((ext_vector_type(8)));
 typedef short pr_s4 __attribute__((ext_vector_type(4)));
 #define PR_LDS __attribute__((address_space(3)))
-
-// How a launch divides its results: ti x to tiles by `splits` pieces of the sum.  Pieces beyond one
-// leave floats in `partial` [splits][outer][inner padded to 8], which k_join adds in their order.
-struct pr_plan {
-    long long inner, outer;
-    int steps;   // of the whole sum
-    int per;     // of a piece
-    int splits;
-    int by_piece;  // see pr_tile
-    unsigned ni, no;  // tiles
-    float *partial;
-    long long partial_ld;
-};
 
 // Where results go: rows of `type`, a row added to all (bias) or a matrix (add).
 template <class Y> struct pr_out {
