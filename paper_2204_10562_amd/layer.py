@@ -1,8 +1,8 @@
 """Python binding of the layer operators of libpp (include/pp_layer.h): argument marshalling only.
 
-As in `binding`, every function takes torch tensors that already live on the GPU, checks dtype,
-device, shape and strides, and passes raw pointers plus the current HIP stream to the C entry
-point of the same name; outputs and workspaces are the caller's.  A matrix is a tensor of two
+As in `binding`, every function takes torch tensors that already live on the GPU (all of a call on
+the current device), checks dtype, device, shape and strides, and passes raw pointers plus the
+current HIP stream to the C entry point of the same name; outputs and workspaces are the caller's.  A matrix is a tensor of two
 dimensions whose rows are consecutive values (stride(1) == 1); a packed matrix is the pair
 (codes, scales) that `empty_packed` makes.
 """
@@ -65,9 +65,12 @@ def packed_bytes(fmt, rows, cols):
 _device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
 
 
-def _stream():
-    """The current HIP stream of the current device (torch.cuda.current_stream() without its object, which takes 3 us to make)."""
-    return _raw_stream(_device())
+def _stream(dev):
+    """The current HIP stream of device `dev`, which has to be the current one (torch.cuda.current_stream() without its object, which
+    takes 3 us to make)."""
+    if dev != _device():
+        raise ValueError("operands must be on the current device (they are on cuda:%d)" % dev)
+    return _raw_stream(dev)
 
 
 def _check(rc):
@@ -75,10 +78,10 @@ def _check(rc):
         raise PPError(rc)
 
 
-def _matrix(t, dtype, rows, cols, name):
-    """(data pointer, row stride) of a matrix."""
-    if not t.is_cuda or t.dtype is not dtype or t.shape != (rows, cols):
-        raise ValueError("%s must be a %s matrix of %d x %d on the GPU" % (name, dtype, rows, cols))
+def _matrix(t, dtype, rows, cols, name, dev):
+    """(data pointer, row stride) of a matrix on device `dev`."""
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != (rows, cols):
+        raise ValueError("%s must be a %s matrix of %d x %d on the GPU of the other operands" % (name, dtype, rows, cols))
     ld, step = t.stride()
     if step != 1 and cols > 1 or ld < cols and rows > 1:
         raise ValueError("%s must have rows of consecutive values that do not overlap" % name)
@@ -86,75 +89,75 @@ def _matrix(t, dtype, rows, cols, name):
 
 
 def _first(t, name):
-    """(type code, rows, cols, data pointer, row stride) of the matrix that sets a call's type and sizes."""
-    code, shape = TYPES.get(t.dtype), t.shape
-    if code is None or len(shape) != 2:
-        raise ValueError("%s must be a matrix of float32, float16 or bfloat16" % name)
+    """(type code, rows, cols, data pointer, row stride, device) of the matrix that sets a call's type, sizes and device."""
+    code, shape, dev = TYPES.get(t.dtype), t.shape, t.get_device()
+    if code is None or len(shape) != 2 or dev < 0:
+        raise ValueError("%s must be a matrix of float32, float16 or bfloat16 on the GPU" % name)
     rows, cols = shape
-    ptr, ld = _matrix(t, t.dtype, rows, cols, name)
-    return code, rows, cols, ptr, ld
+    ptr, ld = _matrix(t, t.dtype, rows, cols, name, dev)
+    return code, rows, cols, ptr, ld, dev
 
 
-def _packed(pair, fmt, rows, cols, name):
-    """Pointers of a packed matrix of these sizes; None: no such matrix."""
+def _packed(pair, fmt, rows, cols, name, dev):
+    """Pointers of a packed matrix of these sizes on device `dev`; None: no such matrix."""
     if pair is None:
         return None, None
     codes, scales = pair
     dtype, width = _CODES[fmt]
     groups = (cols + GROUP - 1) // GROUP
-    if (not codes.is_cuda or codes.dtype is not dtype or codes.shape != (rows, groups, width) or not codes.is_contiguous()
-            or not scales.is_cuda or scales.dtype is not torch.uint8 or scales.shape != (rows, groups, 4) or not scales.is_contiguous()):
-        raise ValueError("%s must be codes %s [%d][%d][%d] and scales uint8 [%d][%d][4], contiguous on the GPU"
+    if (codes.get_device() != dev or codes.dtype is not dtype or codes.shape != (rows, groups, width) or not codes.is_contiguous()
+            or scales.get_device() != dev or scales.dtype is not torch.uint8 or scales.shape != (rows, groups, 4) or not scales.is_contiguous()):
+        raise ValueError("%s must be codes %s [%d][%d][%d] and scales uint8 [%d][%d][4], contiguous on the GPU of the other operands"
                          % (name, dtype, rows, groups, width, rows, groups))
     return codes.data_ptr(), scales.data_ptr()
 
 
-def _vector(t, n, name):
+def _vector(t, n, name, dev):
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError("%s must be %d contiguous float32 values on the GPU" % (name, n))
+    if t.get_device() != dev or t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
+        raise ValueError("%s must be %d contiguous float32 values on the GPU of the other operands" % (name, n))
     return t.data_ptr()
 
 
-def _workspace(t):
+def _workspace(t, dev):
     if t is None:
         return None, 0
-    if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous():
-        raise ValueError("workspace must be a contiguous uint8 tensor on the GPU")
+    if t.get_device() != dev or t.dtype != torch.uint8 or not t.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the GPU of the other operands")
     return t.data_ptr(), t.numel()
 
 
 def pp_pack(fmt, x, packed):
-    type_, rows, cols, px, ld = _first(x, "x")
-    codes, scales = _packed(packed, fmt, rows, cols, "packed")
-    _check(lib().pp_pack(fmt, type_, rows, cols, px, ld, codes, scales, _stream()))
+    type_, rows, cols, px, ld, dev = _first(x, "x")
+    codes, scales = _packed(packed, fmt, rows, cols, "packed", dev)
+    _check(lib().pp_pack(fmt, type_, rows, cols, px, ld, codes, scales, _stream(dev)))
 
 
 def pp_unpack(fmt, packed, out):
-    type_, rows, cols, po, ld = _first(out, "out")
-    codes, scales = _packed(packed, fmt, rows, cols, "packed")
-    _check(lib().pp_unpack(fmt, type_, rows, cols, codes, scales, po, ld, _stream()))
+    type_, rows, cols, po, ld, dev = _first(out, "out")
+    codes, scales = _packed(packed, fmt, rows, cols, "packed", dev)
+    _check(lib().pp_unpack(fmt, type_, rows, cols, codes, scales, po, ld, _stream(dev)))
 
 
 def pp_act_forward(kind, x, u, y, x_kept=None, u_kept=None):
     """u: the gate's other factor, or None."""
-    type_, rows, cols, px, ldx = _first(x, "x")
-    pu, ldu = (None, 0) if u is None else _matrix(u, x.dtype, rows, cols, "u")
-    py, ldy = _matrix(y, x.dtype, rows, cols, "y")
-    xc, xs = _packed(x_kept, PP_PACK_INT8, rows, cols, "x_kept")
-    uc, us = _packed(u_kept, PP_PACK_INT8, rows, cols, "u_kept")
-    _check(lib().pp_act_forward(kind, type_, rows, cols, px, ldx, pu, ldu, py, ldy, xc, xs, uc, us, _stream()))
+    type_, rows, cols, px, ldx, dev = _first(x, "x")
+    pu, ldu = (None, 0) if u is None else _matrix(u, x.dtype, rows, cols, "u", dev)
+    py, ldy = _matrix(y, x.dtype, rows, cols, "y", dev)
+    xc, xs = _packed(x_kept, PP_PACK_INT8, rows, cols, "x_kept", dev)
+    uc, us = _packed(u_kept, PP_PACK_INT8, rows, cols, "u_kept", dev)
+    _check(lib().pp_act_forward(kind, type_, rows, cols, px, ldx, pu, ldu, py, ldy, xc, xs, uc, us, _stream(dev)))
 
 
 def pp_act_backward(kind, dy, x_kept, u_kept, dx, du=None):
     """u_kept and du: both for a gated layer, else None."""
-    type_, rows, cols, pdy, lddy = _first(dy, "dy")
-    xc, xs = _packed(x_kept, PP_PACK_INT8, rows, cols, "x_kept")
-    uc, us = _packed(u_kept, PP_PACK_INT8, rows, cols, "u_kept")
-    pdx, lddx = _matrix(dx, dy.dtype, rows, cols, "dx")
-    pdu, lddu = (None, 0) if du is None else _matrix(du, dy.dtype, rows, cols, "du")
-    _check(lib().pp_act_backward(kind, type_, rows, cols, pdy, lddy, xc, xs, uc, us, pdx, lddx, pdu, lddu, _stream()))
+    type_, rows, cols, pdy, lddy, dev = _first(dy, "dy")
+    xc, xs = _packed(x_kept, PP_PACK_INT8, rows, cols, "x_kept", dev)
+    uc, us = _packed(u_kept, PP_PACK_INT8, rows, cols, "u_kept", dev)
+    pdx, lddx = _matrix(dx, dy.dtype, rows, cols, "dx", dev)
+    pdu, lddu = (None, 0) if du is None else _matrix(du, dy.dtype, rows, cols, "du", dev)
+    _check(lib().pp_act_backward(kind, type_, rows, cols, pdy, lddy, xc, xs, uc, us, pdx, lddx, pdu, lddu, _stream(dev)))
 
 
 def pp_linear_workspace_bytes(call, dtype, rows, n_in, n_out):
@@ -164,36 +167,36 @@ def pp_linear_workspace_bytes(call, dtype, rows, n_in, n_out):
 
 def pp_linear_forward(x, w, bias, y, x_kept, workspace):
     """w: the packed weight (PP_PACK_FP4); x_kept: room for the packed x (PP_PACK_INT8), or None."""
-    type_, rows, n_in, px, ldx = _first(x, "x")
+    type_, rows, n_in, px, ldx, dev = _first(x, "x")
     n_out = w[0].shape[0]
-    wc, wsc = _packed(w, PP_PACK_FP4, n_out, n_in, "w")
-    py, ldy = _matrix(y, x.dtype, rows, n_out, "y")
-    xc, xs = _packed(x_kept, PP_PACK_INT8, rows, n_in, "x_kept")
-    ws, nbytes = _workspace(workspace)
-    _check(lib().pp_linear_forward(type_, rows, n_in, n_out, px, ldx, wc, wsc, _vector(bias, n_out, "bias"), py, ldy,
-                                   xc, xs, ws, nbytes, _stream()))
+    wc, wsc = _packed(w, PP_PACK_FP4, n_out, n_in, "w", dev)
+    py, ldy = _matrix(y, x.dtype, rows, n_out, "y", dev)
+    xc, xs = _packed(x_kept, PP_PACK_INT8, rows, n_in, "x_kept", dev)
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().pp_linear_forward(type_, rows, n_in, n_out, px, ldx, wc, wsc, _vector(bias, n_out, "bias", dev), py, ldy,
+                                   xc, xs, ws, nbytes, _stream(dev)))
 
 
 def pp_linear_backward_input(dy, w, dx, workspace):
-    type_, rows, n_out, pdy, lddy = _first(dy, "dy")
+    type_, rows, n_out, pdy, lddy, dev = _first(dy, "dy")
     n_in = dx.shape[-1]
-    wc, wsc = _packed(w, PP_PACK_FP4, n_out, n_in, "w")
-    pdx, lddx = _matrix(dx, dy.dtype, rows, n_in, "dx")
-    ws, nbytes = _workspace(workspace)
-    _check(lib().pp_linear_backward_input(type_, rows, n_in, n_out, pdy, lddy, wc, wsc, pdx, lddx, ws, nbytes, _stream()))
+    wc, wsc = _packed(w, PP_PACK_FP4, n_out, n_in, "w", dev)
+    pdx, lddx = _matrix(dx, dy.dtype, rows, n_in, "dx", dev)
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().pp_linear_backward_input(type_, rows, n_in, n_out, pdy, lddy, wc, wsc, pdx, lddx, ws, nbytes, _stream(dev)))
 
 
 def pp_linear_backward_weight(dy, x_kept, dw_in, dw, db, workspace):
     """dw_in: what is added to (None = nothing; may be dw); db: the bias's gradient, or None."""
-    type_, rows, n_out, pdy, lddy = _first(dy, "dy")
+    type_, rows, n_out, pdy, lddy, dev = _first(dy, "dy")
     n_in = dw.shape[-1]
-    xc, xs = _packed(x_kept, PP_PACK_INT8, rows, n_in, "x_kept")
-    pdw, lddw = _matrix(dw, torch.float32, n_out, n_in, "dw")
+    xc, xs = _packed(x_kept, PP_PACK_INT8, rows, n_in, "x_kept", dev)
+    pdw, lddw = _matrix(dw, torch.float32, n_out, n_in, "dw", dev)
     pin = None
     if dw_in is not None:
-        pin, ldin = _matrix(dw_in, torch.float32, n_out, n_in, "dw_in")
+        pin, ldin = _matrix(dw_in, torch.float32, n_out, n_in, "dw_in", dev)
         if ldin != lddw:
             raise ValueError("dw_in and dw must have the same row stride")
-    ws, nbytes = _workspace(workspace)
+    ws, nbytes = _workspace(workspace, dev)
     _check(lib().pp_linear_backward_weight(type_, rows, n_in, n_out, pdy, lddy, xc, xs, pin, pdw, lddw,
-                                           _vector(db, n_out, "db"), ws, nbytes, _stream()))
+                                           _vector(db, n_out, "db", dev), ws, nbytes, _stream(dev)))
