@@ -5,6 +5,10 @@ the current device), checks dtype, device, shape and strides, and passes raw poi
 current HIP stream to the C entry point of the same name; outputs and workspaces are the caller's.  A matrix is a tensor of two
 dimensions whose rows are consecutive values (stride(1) == 1); a packed matrix is the pair
 (codes, scales) that `empty_packed` makes.
+
+Autograd does not see these calls.  In grad mode an operand that requires a gradient is refused (but for
+pp_pack, whose results are whole numbers); the backward operators give the gradients, of which a torch.autograd.Function can be made.  A buffer that
+autograd has saved must not be written to by a later call: its version does not change.
 """
 import ctypes
 
@@ -78,23 +82,32 @@ def _check(rc):
         raise PPError(rc)
 
 
-def _matrix(t, dtype, rows, cols, name, dev):
-    """(data pointer, row stride) of a matrix on device `dev`."""
+def _no_history(name):
+    """As torch's own functions with out=: what a call writes has no history, which would be gradients that are silently missing."""
+    if torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient, and autograd does not see what the layer operators do: call them under torch.no_grad() or "
+                         "with detached tensors, and their backward operators for the gradients" % name)
+
+
+def _matrix(t, dtype, rows, cols, name, dev, differentiable=True):
+    """(data pointer, row stride) of a matrix on device `dev`; differentiable: of which a gradient may be asked."""
     if t.get_device() != dev or t.dtype is not dtype or t.shape != (rows, cols):
         raise ValueError("%s must be a %s matrix of %d x %d on the GPU of the other operands" % (name, dtype, rows, cols))
+    if t.requires_grad and differentiable:
+        _no_history(name)
     ld, step = t.stride()
     if step != 1 and cols > 1 or ld < cols and rows > 1:
         raise ValueError("%s must have rows of consecutive values that do not overlap" % name)
     return t.data_ptr(), ld if ld > cols else cols
 
 
-def _first(t, name):
+def _first(t, name, differentiable=True):
     """(type code, rows, cols, data pointer, row stride, device) of the matrix that sets a call's type, sizes and device."""
     code, shape, dev = TYPES.get(t.dtype), t.shape, t.get_device()
     if code is None or len(shape) != 2 or dev < 0:
         raise ValueError("%s must be a matrix of float32, float16 or bfloat16 on the GPU" % name)
     rows, cols = shape
-    ptr, ld = _matrix(t, t.dtype, rows, cols, name, dev)
+    ptr, ld = _matrix(t, t.dtype, rows, cols, name, dev, differentiable)
     return code, rows, cols, ptr, ld, dev
 
 
@@ -117,6 +130,8 @@ def _vector(t, n, name, dev):
         return None
     if t.get_device() != dev or t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
         raise ValueError("%s must be %d contiguous float32 values on the GPU of the other operands" % (name, n))
+    if t.requires_grad:
+        _no_history(name)
     return t.data_ptr()
 
 
@@ -129,7 +144,7 @@ def _workspace(t, dev):
 
 
 def pp_pack(fmt, x, packed):
-    type_, rows, cols, px, ld, dev = _first(x, "x")
+    type_, rows, cols, px, ld, dev = _first(x, "x", False)    # (codes are whole numbers: nothing has a gradient through them)
     codes, scales = _packed(packed, fmt, rows, cols, "packed", dev)
     _check(lib().pp_pack(fmt, type_, rows, cols, px, ld, codes, scales, _stream(dev)))
 

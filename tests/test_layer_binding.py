@@ -87,3 +87,29 @@ def test_operands_on_another_device(pp, name):
     with pytest.raises(ValueError):
         getattr(layer, name)(*args)
     assert len(calls) == 1
+
+
+@pytest.mark.parametrize("name", list(operands()))
+def test_operands_that_require_a_gradient(pp, name):
+    """Refused in grad mode, where the result would lack its history, and taken without."""
+    layer, calls = pp
+    args = operands()[name]
+    parts = [o for o in args if isinstance(o, Operand) and o.dtype.is_floating_point]
+    assert parts
+    for o in parts:
+        o.requires_grad = True
+        if name == "pp_pack":      # whole numbers have no gradient: a parameter is packed as it is
+            getattr(layer, name)(*args)
+            assert len(calls) == 1
+            calls.clear()
+            continue
+        with pytest.raises(ValueError, match="autograd"):
+            getattr(layer, name)(*args)
+        assert not calls
+        with torch.no_grad():
+            getattr(layer, name)(*args)
+        assert len(calls) == 1
+        calls.clear()
+        o.requires_grad = False
+    getattr(layer, name)(*args)
+    assert len(calls) == 1
