@@ -210,7 +210,7 @@ def pp_linear_backward_weight(dy, x_kept, dw_in, dw, db, workspace):
     pin = None
     if dw_in is not None:
         pin, ldin = _matrix(dw_in, torch.float32, n_out, n_in, "dw_in", dev)
-        if ldin != lddw:
+        if ldin != lddw and n_out > 1:
             raise ValueError("dw_in and dw must have the same row stride")
     ws, nbytes = _workspace(workspace, dev)
     _check(lib().pp_linear_backward_weight(type_, rows, n_in, n_out, pdy, lddy, xc, xs, pin, pdw, lddw,

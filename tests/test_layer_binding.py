@@ -113,3 +113,18 @@ def test_operands_that_require_a_gradient(pp, name):
         o.requires_grad = False
     getattr(layer, name)(*args)
     assert len(calls) == 1
+
+
+def test_row_stride_of_one_row(pp):
+    """dw_in and dw have the same distance between their rows; one row has none."""
+    layer, calls = pp
+    kept = (Operand((ROWS, 2, 128), torch.int8), Operand((ROWS, 2, 4), torch.uint8))
+    ws = Operand((1 << 20,), torch.uint8)
+    for rows, right in ((1, True), (2, False)):
+        dy, dw_in, dw = Operand((ROWS, rows), torch.bfloat16), Operand((rows, N_IN), torch.float32, stride=(N_IN + 8, 1)), Operand((rows, N_IN), torch.float32)
+        if right:
+            layer.pp_linear_backward_weight(dy, kept, dw_in, dw, None, ws)
+            assert len(calls) == 1
+        else:
+            with pytest.raises(ValueError):
+                layer.pp_linear_backward_weight(dy, kept, dw_in, dw, None, ws)
