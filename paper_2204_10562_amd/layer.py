@@ -66,12 +66,16 @@ def packed_bytes(fmt, rows, cols):
     return rows * -(-cols // GROUP) * (_CODES[fmt][1] + 4)
 
 
-_device, _raw_stream = torch.cuda.current_device, torch._C._cuda_getCurrentRawStream
+def _public_stream(dev):
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+# (torch's own name for the stream without its object, which takes 3 us to make; where a torch has no such name, its public one)
+_device, _raw_stream = torch.cuda.current_device, getattr(torch._C, "_cuda_getCurrentRawStream", _public_stream)
 
 
 def _stream(dev):
-    """The current HIP stream of device `dev`, which has to be the current one (torch.cuda.current_stream() without its object, which
-    takes 3 us to make)."""
+    """The current HIP stream of device `dev`, which has to be the current one."""
     if dev != _device():
         raise ValueError("operands must be on the current device (they are on cuda:%d)" % dev)
     return _raw_stream(dev)

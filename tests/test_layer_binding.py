@@ -1,6 +1,11 @@
 """What the layer operators' binding refuses before the library is called (no GPU needed: operands are stand-ins)."""
+import subprocess
+import sys
+
 import pytest
 import torch
+
+from conftest import ROOT
 
 
 class Operand:
@@ -128,3 +133,19 @@ def test_row_stride_of_one_row(pp):
         else:
             with pytest.raises(ValueError):
                 layer.pp_linear_backward_weight(dy, kept, dw_in, dw, None, ws)
+
+
+def test_torch_without_raw_streams():
+    """A torch that lacks the name by which it gives a stream without its object: the public way, not a failing import."""
+    code = ("import torch\nvars(torch._C).pop('_cuda_getCurrentRawStream', None)\nfrom paper_2204_10562_amd import layer\n"
+            "assert layer._raw_stream is layer._public_stream")
+    res = subprocess.run([sys.executable, "-c", code], cwd=ROOT, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert res.returncode == 0, res.stdout[-2000:]
+
+
+@pytest.mark.gpu
+def test_both_ways_give_one_stream():
+    from paper_2204_10562_amd import layer
+    for s in (torch.cuda.current_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(s):
+            assert layer._stream(0) == layer._public_stream(0) == s.cuda_stream
