@@ -4,8 +4,8 @@
 
 // The outer operand in bf16 as `planes` matrices that add up to it (one, or more where its type has
 // more bits), `plane` values apart, each of rows x cols with rows ld values apart; every row starts
-// at a multiple of 16 bytes.  What lies between a row's end and the next row is not used, except that
-// for pg_launch_input, whose sum runs along the rows, cols is a multiple of 8.
+// at a multiple of 16 bytes.  What lies between a row's end and the next row is not used.  cols is a
+// multiple of 8 for pg_launch_input, whose sum runs along the rows, and even for pg_launch_weight.
 struct pg_outer {
     const uint8_t *p;
     long long rows, cols, ld, plane;

@@ -150,8 +150,8 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
         }
     }
     const unsigned to_o = base + L::SI + chunk * 1024;
-    // From the step on that is loaded next: address, and bytes that it may use (less than 2^32).  (Across
-    // the rows up to the end of the last value's four bytes: less than four count as beyond the buffer.)
+    // From the step on that is loaded next: address, and bytes that it may use (less than 2^32, and whole words: less than
+    // four bytes count as beyond the buffer).
     const int per_step = ALONG ? 128 : (int)(y.ld * 128);
     const int orows = y.rows - o0 < L::TO ? (int)(y.rows - o0) : L::TO, row_bytes = (int)(y.cols - (ALONG ? 0 : o0)) * 2;
     const uint8_t *oplane = y.p + (ALONG ? o0 * y.ld : o0) * 2 + (s0 / per_plane) * y.plane * 2;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product_grad(pr_plan p, pg_
             bytes = (unsigned)((orows - 1) * (int)y.ld) * 2 + ocols * 2;
         } else {
             const int left = (int)y.rows - 64 * oi, n = left < 64 ? left : 64;
-            bytes = n <= 0 ? 0 : (((unsigned)(n - 1) * (unsigned)y.ld) * 2 + row_bytes + 3) & ~3u;
+            bytes = n <= 0 ? 0 : ((unsigned)(n - 1) * (unsigned)y.ld) * 2 + row_bytes;
         }
         const unsigned long long at = (unsigned long long)oat;
         ob[0] = __builtin_amdgcn_readfirstlane((int)at);
