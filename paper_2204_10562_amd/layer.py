@@ -93,12 +93,17 @@ def _no_history(name):
                          "with detached tensors, and their backward operators for the gradients" % name)
 
 
-def _matrix(t, dtype, rows, cols, name, dev, differentiable=True):
-    """(data pointer, row stride) of a matrix on device `dev`; differentiable: of which a gradient may be asked."""
+def _matrix(t, dtype, rows, cols, name, dev):
+    """(data pointer, row stride) of a matrix on device `dev`."""
     if t.get_device() != dev or t.dtype is not dtype or t.shape != (rows, cols):
         raise ValueError("%s must be a %s matrix of %d x %d on the GPU of the other operands" % (name, dtype, rows, cols))
-    if t.requires_grad and differentiable:
+    if t.requires_grad:
         _no_history(name)
+    return _place(t, rows, cols, name)
+
+
+def _place(t, rows, cols, name):
+    """(data pointer, row stride)"""
     ld, step = t.stride()
     if step != 1 and cols > 1 or ld < cols and rows > 1:
         raise ValueError("%s must have rows of consecutive values that do not overlap" % name)
@@ -106,12 +111,15 @@ def _matrix(t, dtype, rows, cols, name, dev, differentiable=True):
 
 
 def _first(t, name, differentiable=True):
-    """(type code, rows, cols, data pointer, row stride, device) of the matrix that sets a call's type, sizes and device."""
+    """(type code, rows, cols, data pointer, row stride, device) of the matrix that sets a call's type, sizes and device;
+    differentiable: of which a gradient may be asked."""
     code, shape, dev = TYPES.get(t.dtype), t.shape, t.get_device()
     if code is None or len(shape) != 2 or dev < 0:
         raise ValueError("%s must be a matrix of float32, float16 or bfloat16 on the GPU" % name)
+    if differentiable and t.requires_grad:
+        _no_history(name)
     rows, cols = shape
-    ptr, ld = _matrix(t, t.dtype, rows, cols, name, dev, differentiable)
+    ptr, ld = _place(t, rows, cols, name)
     return code, rows, cols, ptr, ld, dev
 
 
