@@ -107,19 +107,19 @@ __device__ __forceinline__ float times_sigmoid(float x, float z) {
     return z < 0.0f ? x * t * r * 0x1p-16f : x * r;
 }
 
-// e = exp(-x^2 / 2), and Phi(x) = erfc(-x / sqrt 2) / 2 from it: Phi(-|x|) / e falls from 1/2 as slowly as 1 / |x|, which a
-// polynomial in t = 1 / (1 + p |x|) follows to 2^-25 of itself (least squares of the relative error, weighted until it
-// is even, over |x| <= 14.5, beyond which nothing is left; the first coefficient makes Phi(0) 1/2).  So what is left far on the negative side keeps
-// its digits, (5 + 1.2 x^2) 2^-24 of itself or better, where 1 + erf has none at -6.
+// e = exp(-x^2 / 2), and Phi(x) = erfc(-x / sqrt 2) / 2 from it: Phi(-|x|) / e falls from 1/2 as slowly as 1 / |x|, which
+// 1/2 - v Q(v) with v = p |x| / (1 + p |x|) follows to 2^-26 of itself (Q's coefficients by least squares of the relative
+// error over |x| <= 14.5, weighted until it was even; beyond, nothing is left).  So what is left far on the negative
+// side keeps its digits, to (8 + 1.2 x^2) 2^-24 of itself down to the last normal numbers, where 1 + erf has none at -6.
 __device__ __forceinline__ float gauss(float x, float &e) {
     const float h = __builtin_amdgcn_exp2f(-0.36067376f * (x * x));  // (of half the exponent: exp2 gives no subnormal numbers)
     e = h * h;
-    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.345f, __builtin_fabsf(x), 1.0f));
-    const float c[] = {0.13762012f, 0.13800524f, 0.11736195f, 0.111267924f, -0.036238503f, 0.1850556f, -0.26915452f, 0.1442341f, -0.028151914f};
+    const float m = __builtin_amdgcn_fmed3f(0.33f * __builtin_fabsf(x), 0.0f, 0x1p30f), v = m * __builtin_amdgcn_rcpf(1.0f + m);
+    const float c[] = {1.20891619f, -1.08676934f, 0.317839444f, 0.154287234f, -0.0652996749f, -0.0222513955f, -0.0651500002f, 0.0843002498f, -0.0258791298f};
     float q = c[8];
 #pragma unroll
-    for (int k = 7; k >= 0; --k) q = __builtin_fmaf(q, t, c[k]);
-    const float g = e * (q * t);
+    for (int k = 7; k >= 0; --k) q = __builtin_fmaf(q, v, c[k]);
+    const float g = e * __builtin_fmaf(-v, q, 0.5f);
     return x < 0.0f ? g : 1.0f - g;
 }
 
