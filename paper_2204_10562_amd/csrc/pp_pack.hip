@@ -97,15 +97,20 @@ __global__ __launch_bounds__(PK_THREADS) void k_unpack(pk_shape s, const uint8_t
     pp_store8<Y>(dst + r * ld + 8 * q, left, v);
 }
 
-// f and f'.  exp2 and the reciprocal are the hardware's (a unit or two of the last place), which
-// give zero for what is no normal number: x sigmoid(z) is taken from exp(-|z|), for z < 0 held 2^16
-// times as large until x has been multiplied in.  tanh is 2 sigmoid(2 z) - 1, which loses nothing
-// where it is near -1.
-__device__ __forceinline__ float times_sigmoid(float x, float z) {
-    const float t = __builtin_amdgcn_exp2f(__builtin_fmaf(-1.4426950408889634f, __builtin_fabsf(z), 16.0f));
-    const float r = __builtin_amdgcn_rcpf(__builtin_fmaf(t, 0x1p-16f, 1.0f));
-    return z < 0.0f ? x * t * r * 0x1p-16f : x * r;
-}
+// f and f'.  exp2 and the reciprocal are the hardware's (a unit or two of the last place), which give zero for what is no normal
+// number.  sigmoid(z) is taken from h = exp(-|z| / 2) and hr = h / (1 + h^2): h hr for z < 0, else 1 - h hr, whose rounding is
+// the last place's alone; its derivative is hr^2, without a difference of which nothing is left where sigmoid is near 1.  (x h) hr
+// loses nothing while it is a normal number.  tanh is 2 sigmoid(2 z) - 1, which loses nothing where it is near -1.
+struct pk_sigmoid {
+    float h, hr;
+    bool low;
+    __device__ __forceinline__ pk_sigmoid(float z) : low(z < 0.0f) {
+        h = __builtin_amdgcn_exp2f(-0.72134752f * __builtin_fabsf(z));
+        hr = h * __builtin_amdgcn_rcpf(__builtin_fmaf(h, h, 1.0f));
+    }
+    __device__ __forceinline__ float value() const { return low ? h * hr : __builtin_fmaf(-h, hr, 1.0f); }
+    __device__ __forceinline__ float times(float x) const { return low ? x * h * hr : x * __builtin_fmaf(-h, hr, 1.0f); }
+};
 
 // e = exp(-x^2 / 2), and Phi(x) = erfc(-x / sqrt 2) / 2 from it: Phi(-|x|) / e falls from 1/2 as slowly as 1 / |x|, which
 // 1/2 - v Q(v) with v = p |x| / (1 + p |x|) follows to 2^-26 of itself (Q's coefficients by least squares of the relative
@@ -124,8 +129,8 @@ __device__ __forceinline__ float gauss(float x, float &e) {
 }
 
 template <int KIND> __device__ __forceinline__ float act(float x) {
-    if constexpr (KIND == PP_ACT_SILU) return times_sigmoid(x, x);
-    if constexpr (KIND == PP_ACT_GELU_TANH) return times_sigmoid(x, 1.5957691216057308f * (x + 0.044715f * x * x * x));
+    if constexpr (KIND == PP_ACT_SILU) return pk_sigmoid(x).times(x);
+    if constexpr (KIND == PP_ACT_GELU_TANH) return pk_sigmoid(1.5957691216057308f * (x + 0.044715f * x * x * x)).times(x);
     float e;
     return x * gauss(x, e);
 }
@@ -138,12 +143,12 @@ template <int KIND> __device__ __forceinline__ void act_both(float x, float &f, 
         f = x * g;
         d = __builtin_fmaf(x * e, 0.39894228040143268f, g);
     } else {
-        f = act<KIND>(x);
-        const float c = KIND == PP_ACT_SILU ? x : __builtin_amdgcn_fmed3f(x, -32.0f, 32.0f);  // beyond, g is 0 or 1 and the second term 0
+        const float c = KIND == PP_ACT_SILU ? x : __builtin_amdgcn_fmed3f(x, -32.0f, 32.0f);  // beyond, f is x or 0 and f' 1 or 0
         const float z = KIND == PP_ACT_SILU ? x : 1.5957691216057308f * (c + 0.044715f * c * c * c);
         const float dz = KIND == PP_ACT_SILU ? 1.0f : 1.5957691216057308f * (1.0f + 3.0f * 0.044715f * c * c);
-        const float g = times_sigmoid(1.0f, z);
-        d = g + c * g * (1.0f - g) * dz;
+        const pk_sigmoid s(z);
+        f = s.times(x);
+        d = __builtin_fmaf(c * dz, s.hr * s.hr, s.value());
         if (KIND == PP_ACT_GELU_TANH) d = x != x ? x : d;
     }
 }
