@@ -115,7 +115,9 @@ int pp_linear_backward_input(int type, int64_t rows, int64_t n_in, int64_t n_out
                              size_t workspace_bytes, void *stream);
 
 /*
- * dw = dw_in + dy^T xk, db = sum over the rows of dy, with xk the kept x (PP_PACK_INT8).
+ * dw = dw_in + dy^T xk, db = sum over the rows of dy, with xk the kept x (PP_PACK_INT8).  (The forward pass
+ * multiplied x in 4 bits; xk is nearer to x than that, so dw is the gradient of x W^T, with rounding passed
+ * straight through, and not the derivative of what the forward pass computed.  For dx the same holds of rounding x.)
  *   dy [rows][n_out] of `type`; dw_in, dw float [n_out][n_in] with rows ld_dw apart
  *   dw_in   NULL = zero; may be dw (rows of both at most PP_LAYER_MAX_LD_DW apart)
  *   db      float [n_out], or NULL = not wanted

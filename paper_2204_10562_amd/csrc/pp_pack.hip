@@ -3,12 +3,13 @@
 //
 // A thread takes eight neighbours (16 bytes of a 16-bit type), the four threads of a quad make a
 // block of 32 and find its largest value by two moves between lanes; nothing goes through LDS.
-// All four operators are bound by the bytes they move, each read and written once: gated silu of
-// 8192 x 16384 bf16 with both checkpoints (1.08 GB) takes 181 us forward and as long backward, 6.0 TB/s
-// where a copy of 1 GiB reaches 5.2; float32 5003 x 4099 into 4 bits 14 us, 6.6 TB/s (its rows start at
+// Each byte is read and written once, and bytes bound all four at a size: gated silu of 8192 x 16384 bf16
+// with both checkpoints (1.08 GB) takes 185 us forward and as long backward, 5.8 TB/s where a copy of 1 GiB
+// reaches 5.2, gated gelu the same; without a gate (0.68 GB) silu 104 to 107 us forward, 6.4 TB/s, and 122 backward, gelu
+// 124 to 134 either way, where its instructions show; float32 5003 x 4099 into 4 bits 14 us, 6.6 TB/s (its rows start at
 // no multiple of 16 bytes; loads and stores of 16 bytes are made all the same); small ones a launch,
 // 1.5 to 2 us.  Four rows to a thread, their loads in flight together, were slower but for packing alone
-// (197 us, and 2 % the other way): a chip full of threads has enough in flight.
+// (8 %, and 2 % the other way): a chip full of threads has enough in flight.
 // Values are scaled and rounded in 32 bits, once for each result.
 #include "pp_layer_common.h"
 

@@ -141,7 +141,9 @@ template <class Y, int WI> struct PrRows {
     }
 };
 
-// A wave's results: columns i0.., rows o0...
+// A wave's results: columns i0.., rows o0...  What is known at run time alone (whole or partial, a bias, a matrix to add, ends) is
+// decided for every fragment, and the largest tiles have no registers left for it: 256 x 256 puts 48 of them away (float: 192)
+// in the 4-bit product and 32 (114) in the gradients', here, behind the loops, which hold none.
 template <class Y, int WI, int WO, class ACC>
 __device__ __forceinline__ void pr_leave(const pr_plan &p, const pr_out<Y> &out, ACC &acc, uint8_t *room, int lane, long long i0, long long o0, int piece) {
     const int r = lane & 31, g = lane >> 5;

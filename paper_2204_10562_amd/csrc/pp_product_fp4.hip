@@ -7,13 +7,14 @@
 // are for: a product of blocks is exact, and sums are in 32 bits.
 //
 // What bounds it.  Tiles of 256 x 256 with 16 fragments of 32 x 32 to a wave read each byte from LDS once
-// for 128 results, which leaves LDS half idle; 8192 rows, 4096 -> 16384 (1.1 TFLOP) take 350 to 425 us, 2.6 to
-// 3.1 PFLOP/s, by how warm the card is, and 324 us of zeros: the card's power, then what goes on around a tile
-// (of its 40 us 12 are the start and the way out), then waits on memory (with buffers of no bytes, so that
-// loads find nothing, a step takes a fifth less).  The matrix instructions by themselves, on random values in
+// for 128 results, which leaves LDS idle for four cycles of five; 8192 rows, 4096 -> 16384 (1.1 TFLOP) take 390 to 440 us, 2.5 to
+// 2.8 PFLOP/s, by how warm the card is.  The matrix units work in 39 % of the cycles: of a tile's 40 us 12 are the
+// start and the way out, with nothing beside them, and waves wait 28 % of their time (with buffers of no
+// bytes, so that loads find nothing, a step takes a fifth less).  Then comes power: the clock is 1.7 GHz, and
+// 2.2 with zeros (335 us).  The matrix instructions by themselves, on random values in
 // registers, reach 5.1 PFLOP/s, on zeros 9.  Where 256 x 256 does not fill the chip, 128 x 128 with two
 // workgroups to a compute unit does, and 256 x 32 for a few dozen rows: both wait for LDS and each other
-// between short runs of products.  333 rows, 4100 -> 5000 (fp16): 17 us, 0.8 PFLOP/s.
+// between short runs of products.  333 rows, 4100 -> 5000 (fp16): 18 to 20 us, 0.7 PFLOP/s, 120 tiles on 256 units.
 #include "pp_product_fp4.h"
 
 // Of the four scales of a row's step, the lane's own of either half become the bytes 0 and 2.  Three
@@ -32,7 +33,8 @@ template <int HALF> __device__ __forceinline__ void p4_multiply(pr_f16 &acc, pp_
 }
 
 // The 16-byte pieces of a row lie exchanged by this (an exclusive or): LDS serves 64 lanes of 16 bytes
-// in four turns of 16, whose rows (0-3, 12-15, 20-23 and 24-27, and so on) then fall on different banks.
+// in four turns of 16, whose rows (0-3, 12-15, 20-23 and 24-27, and so on) then fall on different banks.  (The
+// conflicts that are counted, 48 of the 128 LDS cycles of a wave's step, fit the reads of scales, from rows 16 bytes apart.)
 __device__ __forceinline__ int p4_turn(int row) { return (row >> 2) & 3; }
 
 // WI x WO fragments of 32 x 32 to a wave, NI x NO waves
@@ -209,8 +211,8 @@ __global__ __launch_bounds__(64 * NI * NO, 1) void k_product4(pr_plan p, p4_oper
     pr_leave<Y, WI, WO>(p, out, acc, sm + wave * (32 * 32 * WI * 4), lane, i0 + wi * WI * 32, o0 + wo * WO * 32, piece);
 }
 
-// k_rows4: few rows of x (16 NB at most), bound by the weight's bytes: a row, 4096 -> 16384 (36 MB), takes 9.1 us,
-// 3.9 TB/s, of which 2 are the launch; 32 rows, 4096 -> 4096 8.0 us.  The weight is read once, straight into registers, by waves
+// k_rows4: few rows of x (16 NB at most), bound by the weight's bytes: a row, 4096 -> 16384 (36 MB), takes 9 to 10 us,
+// 3.6 to 4 TB/s, of which 2 are the launch; 32 rows, 4096 -> 4096 8.0 us.  The weight is read once, straight into registers, by waves
 // that divide the sum among them: a wave takes 16 rows of W and up to eight groups at a time, and what
 // the waves of a workgroup have found is added in LDS.  With FUSED the workgroup also packs x itself
 // (rows of it are little beside 16 rows of W) and, for pp_linear_backward_weight, a part of x in 8 bits.

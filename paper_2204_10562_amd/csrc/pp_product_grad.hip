@@ -9,15 +9,16 @@
 // Nothing is rounded on the way: products are exact in 32 bits, sums are held there.
 //
 // What bounds it.  Tiles of 256 x 256, eight waves with eight fragments each: 8192 rows, 16384 -> 4096
-// (1.1 TFLOP) take 860 us for dx, 1.28 PFLOP/s (the library's product of two bf16 matrices of 8192 reaches
-// 1.2 to 1.4), and 1080 us for dw, whose 0.8 GB of results and of what they are added to come on top; 727 and
-// 952 us of zeros: power first.  (Four waves with sixteen fragments each have no registers left for
+// (1.1 TFLOP) take 830 to 930 us for dx, 1.2 to 1.3 PFLOP/s (the library's product of two bf16 matrices of 8192 reaches
+// 1.2 to 1.4), and 1060 to 1160 us for dw, whose 0.8 GB of results and of what they are added to come on top; of zeros
+// 730 and 920: power first, with the clock at 1.5 GHz (zeros 2.1) and the matrix units at work in 73 % of the cycles for dx; for dw in
+// 56 %, the rest the way out.  (Four waves with sixteen fragments each have no registers left for
 // what is on its way.)  Smaller tiles are bound by instruction issue: 16 products to 170 or 190 other instructions
 // (250 of 8 bits) a step and wave.  256 x 128 for dx, eight waves, turns a packed value for twice as many products as
 // 128 x 128 with two workgroups to a compute unit, which wastes less where there are few: 333 rows, 5000 -> 4100 from
-// fp16, two planes, in four pieces 40 us (44).  For dw the same (128 x 256) is 5 % faster where the operands are in
+// fp16, two planes, in five pieces 40 us (44).  For dw the same (128 x 256) is 5 % faster where the operands are in
 // cache and 8 % slower where they come from memory, with one workgroup to wait for them, so it is left out; dw and db
-// of 32771 rows, 520 -> 1000, take 66 us in twelve pieces, 0.52 PFLOP/s.  256 x 32 is for few rows of dy: 16 rows,
+// of 32771 rows, 520 -> 1000, take 62 to 66 us in twelve pieces, 0.53 PFLOP/s.  256 x 32 is for few rows of dy: 16 rows,
 // 16384 -> 4096 takes 16 us.
 #include "pp_product_grad.h"
 
@@ -29,7 +30,9 @@ template <int WI, int WO, int NI, int NO> struct PgTile {
 };
 
 // 32-byte units of a row of the sum are swapped by this (an exclusive or), so that the 16 rows which
-// the lanes of a transposed read take fall on different banks.
+// the lanes of a transposed read take are spread over the banks.  (Not all of them: what is counted of two lengths of the sum, 96
+// of a wave's 224 LDS cycles a step for dx and 128 of 256 for dw, fits two cycles more than two for each such read, and eight
+// more than eight for each write of turned values.  LDS is busy 55 to 65 % of the time.)
 __device__ __forceinline__ int pg_turn(int row) { return (row & 3) | ((row >> 3) & 1) << 2; }
 
 __device__ __forceinline__ pr_bf8 pg_read_t(const uint8_t *p, int second) {  // rows c..c+3 and c+4..c+7
