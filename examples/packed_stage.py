@@ -57,7 +57,8 @@ class PackedLinear:
 
 
 class PackedBlock:
-    """y = down(silu(gate(x)) * up(x)).  forward gives y and what backward needs of this microbatch: four packed matrices."""
+    """y = down(silu(gate(x)) * up(x)), for microbatches of `rows` rows or fewer.  forward gives y and what backward needs of this
+    microbatch: four packed matrices."""
 
     def __init__(self, width, hidden, rows, dtype, seed=0):
         g = torch.Generator(device="cuda").manual_seed(seed)
