@@ -208,7 +208,8 @@ extern "C" int pp_linear_forward(int type, int64_t rows, int64_t n_in, int64_t n
 
 // dy as the products take it: as it is where it can be loaded so, else copied into `room`.  (As it is: bf16,
 // rows at multiples of 16 bytes, and so near each other that 256 of them are within the reach of 32-bit offsets; along the sum
-// whole 16 bytes of it, across it whole words: the last word of an odd row would reach two bytes behind the matrix.)
+// whole 16 bytes of it, across it whole words: the last word of an odd row would reach two bytes behind the matrix; the copy takes
+// 15 of 271 us at 8192 rows, 4096 -> 4095, and 19 of 87 at 32771 rows, 520 -> 1001.)
 static int outer_of(int type, bool along_sum, int64_t rows, int64_t cols, const void *dy, int64_t ld, void *room, pg_outer *out, hipStream_t st) {
     if (rows < 2) ld = cols;
     if (type == PP_TYPE_BF16 && !((uintptr_t)dy & 15) && (rows < 2 || (!(ld & 7) && ld <= PP_LAYER_MAX_COLS)) && !(cols & (along_sum ? 7 : 1))) {
