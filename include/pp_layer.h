@@ -127,6 +127,138 @@ int pp_linear_backward_weight(int type, int64_t rows, int64_t n_in, int64_t n_ou
                               const void *x_codes, const void *x_scales, const float *dw_in, float *dw, int64_t ld_dw,
                               float *db, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Root-mean-square norm of rows with the residual's addition, forward:
+ *   s = x + res (x alone where res is NULL);  inv = 1 / sqrt(mean over the row of s^2 + eps);  y = s inv gain
+ *   x, res, total, y  [rows][cols], all of `type`
+ *   gain    float [cols], or NULL = 1
+ *   eps     a normal positive float, at most 2^126
+ *   total   s, or NULL = not wanted; may be res or x (same base and ld)
+ *   y, y_codes/y_scales          out: y and y packed with PP_PACK_INT8 (as pp_linear_backward_weight reads it);
+ *                                either may be NULL, not both
+ *   total_codes/total_scales     out: s packed with PP_PACK_INT8 for pp_norm_backward, or both NULL
+ *   inv     float [rows] for pp_norm_backward, or NULL
+ * Results are made from s in 32 bits, each rounded once.  (The sum of a row's squares has to be a float.)
+ */
+int pp_norm_forward(int type, int64_t rows, int64_t cols, const void *x, int64_t ld_x, const void *res, int64_t ld_res,
+                    const float *gain, float eps, void *total, int64_t ld_total, void *y, int64_t ld_y, void *y_codes,
+                    void *y_scales, void *total_codes, void *total_scales, float *inv, void *stream);
+
+/*
+ * Its backward pass.  With z = s inv:
+ *   dx = inv (gain dy - z mean over the row of (gain dy z)) + dtotal;   dgain = dgain_in + sum over the rows of dy z
+ * (dx is the gradient of x and of res.)
+ *   dy, dtotal, dx  [rows][cols], all of `type`; dtotal: the gradient that reaches s beside the norm, or NULL = none;
+ *                   dx may be dy or dtotal (same base and ld)
+ *   s      the matrix `total` of `type`, or total_codes/total_scales; one of the two, the other NULL
+ *   inv    float [rows], as pp_norm_forward gave it
+ *   dgain  float [cols], or NULL = not wanted; dgain_in NULL = zero; may be dgain
+ * The workspace (256-byte aligned; not needed where dgain is NULL and a row has at most 32768 columns) need not be kept.
+ * What so many rows need serves fewer.  With rows = 0, dgain = dgain_in.
+ */
+size_t pp_norm_workspace_bytes(int type, int64_t rows, int64_t cols);
+int pp_norm_backward(int type, int64_t rows, int64_t cols, const void *dy, int64_t ld_dy, const void *total, int64_t ld_total,
+                     const void *total_codes, const void *total_scales, const float *inv, const float *gain, const void *dtotal,
+                     int64_t ld_dtotal, void *dx, int64_t ld_dx, const float *dgain_in, float *dgain, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/*
+ * Gated linear recurrence over the rows (tokens) of sequences that lie one behind the other, channel by channel:
+ *   h_t = a_t h_(t-1) + (1 - a_t) v_t,   a_t = 1 / (1 + exp(-gate_t))
+ * Sequence n has rows starts[n] .. starts[n+1] - 1 (none: an empty one); before its first token h is h0[n].
+ *   gate, v, h       [rows][cols], all of `type`
+ *   starts  int32 [seqs + 1], not falling, in 0 .. rows (what is not so is held to it); NULL = one sequence of all rows
+ *           (seqs 1).  Rows before the first sequence and behind the last are neither read nor written.
+ *   h0      float [seqs][cols], or NULL = zero
+ *   h_last  float [seqs][cols] out: h behind the last token (h0 for an empty sequence), or NULL = not wanted
+ *   kept    float [pp_scan_kept_rows][cols] out: states for pp_scan_backward, or NULL = not wanted
+ * States are held in 32 bits.  A state moves by the smaller of a and 1 - a, so one that is kept for many tokens does not drift.
+ * The workspaces (256-byte aligned) need not be kept; what so many rows need serves fewer.  pp_scan_kept_rows (host function;
+ * -1 if a size or the type is out of range): both calls need the same type, rows and cols.
+ */
+#define PP_SCAN_FORWARD 0
+#define PP_SCAN_BACKWARD 1
+size_t pp_scan_workspace_bytes(int call, int type, int64_t rows, int64_t cols);
+int64_t pp_scan_kept_rows(int type, int64_t rows, int64_t cols);
+int pp_scan_forward(int type, int64_t rows, int64_t cols, const void *gate, int64_t ld_gate, const void *v, int64_t ld_v,
+                    int64_t seqs, const int32_t *starts, const float *h0, void *h, int64_t ld_h, float *h_last, float *kept,
+                    void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its backward pass.  With g_t = dh_t + a_(t+1) g_(t+1) within a sequence, and dh_last added to the last token's:
+ *   dv = (1 - a) g;   dgate = a (1 - a) (h_(t-1) - v) g;   dh0 = a g of the first token (dh_last for an empty sequence)
+ *   dh, gate, v, dgate, dv  [rows][cols], all of `type`; dgate, dv of rows in no sequence stay as they are
+ *   h0, kept          as in pp_scan_forward (h is computed again from them in 32 bits, and not read)
+ *   dh_last, dh0      float [seqs][cols]; NULL = zero, not wanted
+ */
+int pp_scan_backward(int type, int64_t rows, int64_t cols, const void *dh, int64_t ld_dh, const void *gate, int64_t ld_gate,
+                     const void *v, int64_t ld_v, int64_t seqs, const int32_t *starts, const float *h0, const float *kept,
+                     const float *dh_last, void *dgate, int64_t ld_dgate, void *dv, int64_t ld_dv, float *dh0, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/*
+ * One token of each of `rows` sequences:  h = a state[slots[r]] + (1 - a) v, which also is the slot's new state.
+ *   gate, v, h   [rows][cols], all of `type`
+ *   slots   int32 [rows], different from each other, or NULL = row r has slot r; a row whose slot is not in
+ *           0 .. n_slots - 1 (padding) is left out, and its h stays as it is
+ *   state   float [n_slots][cols], in and out
+ */
+int pp_scan_step(int type, int64_t rows, int64_t cols, const void *gate, int64_t ld_gate, const void *v, int64_t ld_v,
+                 int64_t n_slots, const int32_t *slots, float *state, void *h, int64_t ld_h, void *stream);
+
+/*
+ * Log probabilities of rows of logits.  With z = logits / temperature and p = softmax(z) over a row:
+ *   logp     float [rows] out: ln p of tokens[r], or NULL; 0 for a token < 0 (padding), NaN for one >= cols
+ *   entropy  float [rows] out: -sum p ln p, or NULL
+ *   norm     float [rows][2] out for pp_logprob_backward (8-byte aligned): the largest logit m and the sum of
+ *            exp((logits - m) / temperature); or NULL
+ *   top      0 .. PP_TOP_MAX: how many of the largest logits are wanted, largest first, equal ones by their column
+ *   top_index int32 [rows][top], top_logp float [rows][top]  out: their columns and ln p
+ *   logits   [rows][cols] of `type`;  tokens int32 [rows] (NULL only without logp);  2^-20 <= temperature <= 2^20
+ * A logit of -infinity (a mask) has p = 0 and is no alternative: what is missing at the end of a list has index -1 and logp
+ * -infinity.  In a row of nothing else logp is -infinity and the entropy 0.  A row that holds a NaN or +infinity gives NaN, and
+ * index -1.  The workspace (256-byte aligned) need not be kept; what so many rows, or a larger top, needs serves fewer.
+ */
+#define PP_TOP_MAX 128
+size_t pp_logprob_workspace_bytes(int type, int64_t rows, int64_t cols, int top);
+int pp_logprob_forward(int type, int64_t rows, int64_t cols, const void *logits, int64_t ld_logits, float temperature,
+                       const int32_t *tokens, float *logp, float *entropy, float *norm, int top, int32_t *top_index,
+                       float *top_logp, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gradient of logp and entropy (dlogp, dentropy float [rows]; NULL = zero; entropy is needed with dentropy alone):
+ *   dlogits_j = (dlogp ([j = token] - p_j) - dentropy p_j (ln p_j + entropy)) / temperature
+ * dlogits of `type`, may be logits (same base and ld).  Rows without a token take no dlogp; rows of nothing but -infinity
+ * have gradient 0.
+ */
+int pp_logprob_backward(int type, int64_t rows, int64_t cols, const void *logits, int64_t ld_logits, float temperature,
+                        const int32_t *tokens, const float *norm, const float *dlogp, const float *entropy, const float *dentropy,
+                        void *dlogits, int64_t ld_dlogits, void *stream);
+
+/*
+ * Distillation: the divergence of p = softmax(logits / temperature) from a teacher of whom each row's `top` entries are known
+ * (as pp_logprob_forward gives them), and its gradient, in one call.
+ *   PP_DISTILL_TOP   top_value are logits (or log probabilities); q = softmax(top_value / temperature) over the list:
+ *                    loss = weight sum q (ln q - ln p),                          dlogits_j = weight (p_j - q_j) / temperature
+ *   PP_DISTILL_REST  top_value are log probabilities (at this temperature); q = exp(top_value), and all columns that are not
+ *                    listed are one more outcome, of r = 1 - sum q (0 if that is below 2^-20) and p_rest:
+ *                    loss = weight (sum q (ln q - ln p) + r (ln r - ln p_rest)), dlogits_j as above for what is listed, beside it
+ *                    weight p_j (1 - r / p_rest) / temperature
+ *   top_index int32 [rows][top], top_value float [rows][top]; 1 <= top <= PP_TOP_MAX.  An index outside 0 .. cols - 1 is none; a
+ *             column listed twice has the sum of the two q.  A row with no q at all (PP_DISTILL_TOP) has loss and gradient 0.
+ *   weight    float [rows], or NULL = 1.  A row of weight 0 (padding) has loss and gradient 0 whatever it holds.
+ *   loss      float [rows] out
+ *   dlogits   [rows][cols] of `type` out, or NULL = not wanted; may be logits (same base and ld)
+ * In a row of nothing but -infinity the loss is infinite (0 if the list has no q) and the gradient 0; one that holds a NaN or
+ * +infinity gives NaN.  The workspace (256-byte aligned) need not be kept; what so many rows, or a longer list, needs serves fewer.
+ */
+#define PP_DISTILL_TOP 0
+#define PP_DISTILL_REST 1
+size_t pp_distill_workspace_bytes(int type, int64_t rows, int64_t cols, int top);
+int pp_distill_loss(int kind, int type, int64_t rows, int64_t cols, const void *logits, int64_t ld_logits, float temperature, int top,
+                    const int32_t *top_index, const float *top_value, const float *weight, float *loss, void *dlogits,
+                    int64_t ld_dlogits, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

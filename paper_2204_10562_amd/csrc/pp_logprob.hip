@@ -1,0 +1,372 @@
+// pp_logprob_forward, pp_logprob_backward: log probabilities of given tokens, entropies and the top alternatives of rows of
+// logits, and their gradient.
+//
+// With z = x / T, p = exp(z) / sum exp(z):  logp = ln p[token],  H = -sum p ln p,
+//   dx = (dlogp ([j = token] - p_j) - dH p_j (ln p_j + H)) / T
+// A workgroup holds a segment of a row in registers: its maximum, then its sums, then the alternatives; rows of more than one
+// segment are joined by a second kernel.  Bytes bound both passes where there are many rows.
+//
+// Alternatives: each thread knows its chunks' maxima.  The K-th largest of the 256 threads' maxima, found bit by bit by one wave,
+// is at most the K-th largest logit, and the logits from there on lie in the chunks of at most K threads (or tie with them): they
+// are read again, ranked by counting and written in order.  Where ties make them too many, the K-th largest pair of logit and
+// index is found bit by bit by all threads.  Equal logits are ordered by their index, so the order is one.
+#include "pp_loss.h"
+
+struct lp_args {
+    long long rows, cols, size, ld;
+    int segs, top;
+    float k, inv_t;
+    const int *tokens;
+    float *logp, *entropy, *norm, *top_logp;
+    int *top_index;
+    pp_f4 *sums;   // [rows][segs]: m, s, w
+    pp_u2 *kept;   // [rows][segs][top]: key, index, in order; key 0: none
+};
+
+// What a row's sums say: s NaN: no numbers; s = 0: nothing but -infinity.
+struct lp_row {
+    float m, s, log2_s;
+    __device__ __forceinline__ float logp(float x, float k) const { return 0.69314718f * ((x - m) * k - log2_s); }
+};
+
+template <class Y> __device__ __forceinline__ void put_row(const lp_args &a, long long row, const typename Y::T *x, float m, float s, float w) {
+    const lp_row r = {m, s, __builtin_amdgcn_logf(s)};
+    if (a.norm) {
+        a.norm[2 * row] = m;
+        a.norm[2 * row + 1] = s;
+    }
+    if (a.entropy) a.entropy[row] = s == 0.0f ? 0.0f : __builtin_fmaxf(0.0f, 0.69314718f * (r.log2_s - w / s)) + (s != s ? s : 0.0f);
+    if (a.logp) {
+        const int tok = a.tokens[row];
+        float v = 0.0f;
+        if (tok >= 0) v = tok >= a.cols ? __builtin_nanf("") : s == 0.0f ? -__builtin_inff() : r.logp(Y::get(x[tok]), a.k);
+        a.logp[row] = v;
+    }
+}
+
+__device__ __forceinline__ void put_top(const lp_args &a, long long row, int rank, unsigned key, unsigned index, const lp_row &r) {
+    const bool bad = r.s != r.s;
+    a.top_index[row * a.top + rank] = key && !bad ? (int)index : -1;
+    a.top_logp[row * a.top + rank] = bad ? r.s : key ? r.logp(ls_value(key), a.k) : -__builtin_inff();
+}
+
+struct lp_room {
+    float wave[8], max[LS_THREADS];
+    unsigned counts[2];
+    float tau;
+    unsigned key[LS_CAP], index[LS_CAP];
+};
+
+// whether (key, index) comes at or before (tk, ti)
+__device__ __forceinline__ bool at_least(unsigned key, unsigned index, unsigned tk, unsigned ti) { return key > tk || (key == tk && index <= ti); }
+
+// Sum of a count over the workgroup; room[0 .. 3] free again behind the next barrier.
+__device__ __forceinline__ unsigned group_count(unsigned c, unsigned *room) {
+    for (int d = 1; d < PP_WAVE; d <<= 1) c += __shfl_xor(c, d);
+    if (!(threadIdx.x & (PP_WAVE - 1))) room[threadIdx.x / PP_WAVE] = c;
+    __syncthreads();
+    c = room[0] + room[1] + room[2] + room[3];
+    __syncthreads();
+    return c;
+}
+
+// The top of a segment x[0 .. n) that starts at column `first`, in order into put(rank, key, index); x is read again.
+template <class Y, int HELD, class F>
+__device__ __forceinline__ void select_top(lp_room &room, const typename Y::T *x, long long n, long long first, int top, const float *chunk_max,
+                                           float thread_max, F put) {
+    const int t = threadIdx.x;
+    room.max[t] = thread_max;
+    if (!t) room.counts[0] = 0;
+    __syncthreads();
+    if (t < PP_WAVE) {
+        const int low = sizeof(typename Y::T) == 4 ? 0 : __is_same(Y, PpBF16) ? 16 : 13;  // (bits below are the same for all)
+        unsigned key[4], tau = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key[i] = ls_key(room.max[t + i * PP_WAVE]);
+        for (int bit = 31; bit >= low; --bit) {
+            const unsigned to = tau | 1u << bit;
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c += __popcll(__ballot(key[i] >= to));
+            if (c >= top) tau = to;
+        }
+        if (!t) room.tau = tau > ls_key(-3.4028235e38f) ? ls_value(tau) : -3.4028235e38f;
+    }
+    __syncthreads();
+    const float tau = room.tau;
+    unsigned todo = 0;
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) todo |= (chunk_max[i] >= tau ? 1u : 0u) << i;
+    while (todo) {
+        const int i = __builtin_ctz(todo);
+        todo &= todo - 1;
+        const long long c = 8ll * (t + i * LS_THREADS);
+        float v[8];
+        pp_values<Y>(ls_load<Y>(x + c, n - c), v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (v[j] >= tau) {
+                const unsigned at = atomicAdd(&room.counts[0], 1u);
+                if (at < LS_CAP) {
+                    room.key[at] = ls_key(v[j]);
+                    room.index[at] = (unsigned)(first + c + j);
+                }
+            }
+    }
+    __syncthreads();
+    unsigned found = room.counts[0];
+    if (found > LS_CAP) {  // (the same for the whole workgroup)
+        unsigned *part = (unsigned *)room.wave, tk = 0, ti = 2 * PP_LAYER_MAX_COLS - 1;
+        auto count = [&](unsigned k, unsigned last) {
+            unsigned c = 0;
+            for (int i = 0; i < HELD; ++i) {
+                const long long at = 8ll * (t + i * LS_THREADS);
+                float v[8];
+                pp_values<Y>(ls_load<Y>(x + at, n - at), v);
+                for (int j = 0; j < 8; ++j) {
+                    const unsigned key = v[j] != v[j] ? 0 : ls_key(v[j]);
+                    c += key && at_least(key, (unsigned)(first + at + j), k, last);
+                }
+            }
+            return group_count(c, part);
+        };
+        for (int bit = 31; bit >= 0; --bit)
+            if (count(tk | 1u << bit, 0xffffffffu) >= (unsigned)top) tk |= 1u << bit;
+        for (int bit = 22; bit >= 0; --bit)  // the least last index with which there are enough
+            if (count(tk, ti & ~(1u << bit)) >= (unsigned)top) ti &= ~(1u << bit);
+        if (!t) room.counts[0] = 0;
+        __syncthreads();
+        for (int i = 0; i < HELD; ++i) {
+            const long long c = 8ll * (t + i * LS_THREADS);
+            float v[8];
+            pp_values<Y>(ls_load<Y>(x + c, n - c), v);
+            for (int j = 0; j < 8; ++j) {
+                const unsigned key = v[j] != v[j] ? 0 : ls_key(v[j]), index = (unsigned)(first + c + j);
+                if (key && at_least(key, index, tk, ti)) {
+                    const unsigned at = atomicAdd(&room.counts[0], 1u);
+                    if (at < LS_CAP) {
+                        room.key[at] = key;
+                        room.index[at] = index;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        found = room.counts[0] < LS_CAP ? room.counts[0] : LS_CAP;
+    }
+    for (unsigned i = t; i < found; i += LS_THREADS) {
+        const unsigned key = room.key[i], index = room.index[i];
+        int rank = 0;
+        for (unsigned o = 0; o < found; ++o) rank += room.key[o] > key || (room.key[o] == key && room.index[o] < index);
+        if (rank < top) put(rank, key, index);
+    }
+    for (int rank = t; rank < top; rank += LS_THREADS)
+        if (rank >= (int)found) put(rank, 0u, 0u);
+}
+
+template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_logprob(lp_args a, const typename Y::T *__restrict__ logits) {
+    __shared__ lp_room room;
+    const int t = threadIdx.x;
+    for (long long item = blockIdx.x; item < a.rows * a.segs; item += gridDim.x) {
+        const long long row = a.segs == 1 ? item : item / a.segs, seg = item - row * a.segs, first = seg * a.size;
+        const typename Y::T *x = logits + row * a.ld + first;
+        const long long n = a.cols - first < a.size ? a.cols - first : a.size;
+        PpRaw<Y> raw[HELD];
+        float chunk_max[HELD], v[8], m = -__builtin_inff();
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const long long c = 8ll * (t + i * LS_THREADS);
+            raw[i] = ls_load<Y>(x + c, n - c);
+        }
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            pp_values<Y>(raw[i], v);
+            chunk_max[i] = ls_max8(v);
+            m = __builtin_fmaxf(m, chunk_max[i]);
+        }
+        const float base = ls_base(ls_group_max<4>(m, room.wave));
+        float s = 0.0f, w = 0.0f;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            pp_values<Y>(raw[i], v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = (v[j] - base) * a.k, e = __builtin_amdgcn_exp2f(d);
+                s += e;
+                w = __builtin_fmaf(e, __builtin_fmaxf(d, -256.0f), w);  // (-infinity: 0)
+            }
+        }
+        __syncthreads();
+        s = pp_group_sum<4>(s, room.wave);
+        w = pp_group_sum<4>(w, room.wave + 4);
+        if (!t) {
+            if (a.segs == 1) put_row<Y>(a, row, x, base, s, w);
+            else a.sums[item] = pp_f4{base, s, w, 0.0f};
+        }
+        if (a.top) {
+            const lp_row r = {base, s, __builtin_amdgcn_logf(s)};
+            select_top<Y, HELD>(room, x, n, first, a.top, chunk_max, m, [&](int rank, unsigned key, unsigned index) {
+                if (a.segs == 1) put_top(a, row, rank, key, index, r);
+                else a.kept[item * a.top + rank] = pp_u2{key, index};
+            });
+        }
+        __syncthreads();
+    }
+}
+
+// Sums of segments on the largest maximum: with d = (a segment's - the largest) k, its s and w are multiplied by 2^d, and d is added
+// to every exponent of w.
+template <class Y> __global__ __launch_bounds__(LS_THREADS) void k_logprob_join(lp_args a, const typename Y::T *__restrict__ logits) {
+    __shared__ float room[8];
+    const int t = threadIdx.x;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const pp_f4 *sums = a.sums + row * a.segs;
+        float m = -__builtin_inff(), s = 0.0f, w = 0.0f;
+        for (int i = t; i < a.segs; i += LS_THREADS)
+            if (sums[i][1] != 0.0f) m = __builtin_fmaxf(m, sums[i][0]);
+        m = ls_base(ls_group_max<4>(m, room));
+        for (int i = t; i < a.segs; i += LS_THREADS) {
+            const pp_f4 p = sums[i];
+            if (p[1] == 0.0f) continue;
+            const float d = (p[0] - m) * a.k, e = __builtin_amdgcn_exp2f(d);
+            s = __builtin_fmaf(e, p[1], s);
+            w = __builtin_fmaf(e, __builtin_fmaf(p[1], __builtin_fmaxf(d, -256.0f), p[2]), w);
+        }
+        __syncthreads();
+        s = pp_group_sum<4>(s, room);
+        w = pp_group_sum<4>(w, room + 4);
+        if (!t) put_row<Y>(a, row, logits + row * a.ld, m, s, w);
+        if (a.top) {
+            const lp_row r = {m, s, __builtin_amdgcn_logf(s)};
+            const pp_u2 *kept = a.kept + row * a.segs * a.top;
+            int some = 0;
+            for (int c = t; c < a.segs * a.top; c += LS_THREADS) {
+                const pp_u2 one = kept[c];
+                if (!one[0]) continue;
+                ++some;
+                const int seg = c / a.top;
+                int rank = c - seg * a.top;
+                for (int o = 0; o < a.segs && rank < a.top; ++o) {  // entries before this one in the other segments' order
+                    if (o == seg) continue;
+                    const pp_u2 *list = kept + o * a.top;
+                    int lo = 0, hi = a.top;
+                    while (lo < hi) {
+                        const int mid = (lo + hi) / 2;
+                        const pp_u2 e = list[mid];
+                        if (e[0] && at_least(e[0], e[1], one[0], one[1])) lo = mid + 1;
+                        else hi = mid;
+                    }
+                    rank += lo;
+                }
+                if (rank < a.top) put_top(a, row, rank, one[0], one[1], r);
+            }
+            __syncthreads();
+            const int all = (int)pp_group_sum<4>((float)some, room);  // (at most 2^22: exact)
+            for (int rank = t; rank < a.top; rank += LS_THREADS)
+                if (rank >= all) put_top(a, row, rank, 0u, 0u, r);
+        }
+        __syncthreads();
+    }
+}
+
+struct lp_back {
+    long long rows, cols, size, ld, ld_d;
+    int segs;
+    float k, inv_t;
+    const int *tokens;
+    const float *norm, *dlogp, *entropy, *dentropy;
+};
+
+// logits and dlogits may be one matrix: a thread reads its values before it writes them
+template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_logprob_back(lp_back a, const typename Y::T *logits, typename Y::T *dlogits) {
+    for (long long item = blockIdx.x; item < a.rows * a.segs; item += gridDim.x) {
+        const long long row = item / a.segs, first = (item - row * a.segs) * a.size;
+        const float m = a.norm[2 * row], s = a.norm[2 * row + 1];
+        const long long tok = a.tokens ? a.tokens[row] : -1;
+        float g = a.dlogp && tok >= 0 ? a.dlogp[row] * a.inv_t : 0.0f;
+        if (tok >= a.cols) g = __builtin_nanf("");
+        const float dh = a.dentropy ? a.dentropy[row] * a.inv_t : 0.0f, h = a.dentropy ? a.entropy[row] : 0.0f;
+        // p (-g - dh (ln p + H)), with ln p = ln 2 (d - log2 s)
+        const float scale = s == 0.0f ? 0.0f : 1.0f / s, log2_s = __builtin_amdgcn_logf(s);
+        const float slope = -dh * 0.69314718f * scale, level = s == 0.0f ? 0.0f : (-g - dh * (h - 0.69314718f * log2_s)) * scale;
+        const long long end = first + a.size < a.cols ? first + a.size : a.cols;
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const long long c = first + 8ll * (threadIdx.x + i * LS_THREADS), left = end - c;
+            if (left <= 0) break;
+            float v[8];
+            pp_values<Y>(ls_load<Y>(logits + row * a.ld + c, left), v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float d = (v[j] - m) * a.k, e = __builtin_amdgcn_exp2f(d);
+                v[j] = e * __builtin_fmaf(__builtin_fmaxf(d, -256.0f), slope, level);
+                if (c + j == tok && s != 0.0f) v[j] += g;
+            }
+            pp_store8<Y>(dlogits + row * a.ld_d + c, left, v);
+        }
+    }
+}
+
+// Calls f with the chunks that a thread holds as a constant.
+template <class F> static void by_held(int held, F f) {
+    if (held == 16) f(std::integral_constant<int, 16>());
+    else if (held == 8) f(std::integral_constant<int, 8>());
+    else if (held == 4) f(std::integral_constant<int, 4>());
+    else f(std::integral_constant<int, 1>());
+}
+
+static unsigned grid_of(int64_t items) { return (unsigned)(items < LS_MAX_GRID ? items : LS_MAX_GRID); }
+
+static bool bad_temperature(float t) { return !(t >= 0x1p-20f && t <= 0x1p20f); }
+static bool bad4(const void *p) { return ((uintptr_t)p & 3) != 0; }
+
+extern "C" size_t pp_logprob_workspace_bytes(int type, int64_t rows, int64_t cols, int top) {
+    if (pp_bad_sizes(type, rows, cols) || top < 0 || top > PP_TOP_MAX) return 0;
+    const size_t most = (size_t)ls_most(type, rows, cols);
+    return pp_align256(most * sizeof(pp_f4)) + pp_align256(most * top * sizeof(pp_u2)) + 256;
+}
+
+extern "C" int pp_logprob_forward(int type, int64_t rows, int64_t cols, const void *logits, int64_t ld, float temperature, const int32_t *tokens,
+                                  float *logp, float *entropy, float *norm, int top, int32_t *top_index, float *top_logp, void *workspace,
+                                  size_t workspace_bytes, void *stream) {
+    if (pp_bad_sizes(type, rows, cols) || pp_bad_matrix(logits, type, rows, cols, ld) || bad_temperature(temperature)) return PP_ERR_INVALID_ARG;
+    if (bad4(tokens) || bad4(logp) || bad4(entropy) || ((uintptr_t)norm & 7) || bad4(top_index) || bad4(top_logp)) return PP_ERR_INVALID_ARG;
+    if (top < 0 || top > PP_TOP_MAX || (rows && ((logp && !tokens) || (top && (!top_index || !top_logp))))) return PP_ERR_INVALID_ARG;
+    if (!rows) return PP_OK;
+    const ls_plan p = ls_divide(type, rows, cols);
+    if (p.segs > 1)
+        if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < pp_logprob_workspace_bytes(type, rows, cols, top)) return PP_ERR_WORKSPACE;
+    pp_f4 *sums = (pp_f4 *)workspace;
+    pp_u2 *kept = (pp_u2 *)((char *)workspace + pp_align256((size_t)rows * p.segs * sizeof(pp_f4)));
+    const lp_args a = {rows, cols, p.size, ld, p.segs, top, (float)(1.4426950408889634 / temperature), 1.0f / temperature, tokens, logp, entropy, norm, top_logp, top_index, sums, kept};
+    hipStream_t st = (hipStream_t)stream;
+    return pp_by_type(type, [&](auto tag) {
+        typedef decltype(tag) Y;
+        typedef typename Y::T T;
+        by_held(p.held, [&](auto h) {
+            if constexpr (decltype(h)::value * sizeof(T) <= 32) k_logprob<Y, decltype(h)::value><<<grid_of(rows * p.segs), LS_THREADS, 0, st>>>(a, (const T *)logits);
+        });
+        if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
+        if (p.segs > 1) k_logprob_join<Y><<<grid_of(rows), LS_THREADS, 0, st>>>(a, (const T *)logits);
+        return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+    });
+}
+
+extern "C" int pp_logprob_backward(int type, int64_t rows, int64_t cols, const void *logits, int64_t ld, float temperature, const int32_t *tokens,
+                                   const float *norm, const float *dlogp, const float *entropy, const float *dentropy, void *dlogits, int64_t ld_d,
+                                   void *stream) {
+    if (pp_bad_sizes(type, rows, cols) || pp_bad_matrix(logits, type, rows, cols, ld) || pp_bad_matrix(dlogits, type, rows, cols, ld_d)) return PP_ERR_INVALID_ARG;
+    if (bad_temperature(temperature) || bad4(tokens) || ((uintptr_t)norm & 7) || bad4(dlogp) || bad4(entropy) || bad4(dentropy)) return PP_ERR_INVALID_ARG;
+    if (rows && (!norm || (dlogp && !tokens) || (dentropy && !entropy))) return PP_ERR_INVALID_ARG;
+    if (!rows) return PP_OK;
+    const int held = type == PP_TYPE_F32 ? 2 : 4;
+    const int64_t size = (int64_t)held * LS_STEP, segs = (cols + size - 1) / size;
+    const lp_back a = {rows, cols, size, ld, ld_d, (int)segs, (float)(1.4426950408889634 / temperature), 1.0f / temperature, tokens, norm, dlogp, entropy, dentropy};
+    hipStream_t st = (hipStream_t)stream;
+    return pp_by_type(type, [&](auto tag) {
+        typedef decltype(tag) Y;
+        typedef typename Y::T T;
+        k_logprob_back<Y, sizeof(T) == 4 ? 2 : 4><<<grid_of(rows * segs), LS_THREADS, 0, st>>>(a, (const T *)logits, (T *)dlogits);
+        return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+    });
+}

@@ -1,0 +1,85 @@
+// How the losses (pp_logprob.hip, pp_distill.hip) divide rows of logits, and what they share.
+//
+// With k = log2(e) / T and m = max x, a segment of a row has s = sum 2^((x - m) k).  The difference comes first: k x - k m in one
+// multiply-add would be an instruction less, and nothing where m k passes 2^31, as in rows masked with a type's lowest value.
+#pragma once
+
+#include "pp_rows.h"
+
+#define LS_THREADS 256
+#define LS_STEP (LS_THREADS * 8)  // logits that a workgroup reads at a time
+#define LS_MAX_GRID (1 << 22)
+#define LS_ENOUGH 1024           // workgroups that fill the chip
+#define LS_CAP 512                // candidates of a segment that are ranked at once
+
+// Rows of `cols` in `segs` segments of `size` (the last shorter), `held` chunks of eight to a thread.
+struct ls_plan {
+    int held;
+    int segs;
+    long long size;
+};
+
+// The largest segments, for their fewer partial results; smaller ones where those are as few, and to spread few rows over the chip.
+static inline ls_plan ls_divide(int type, int64_t rows, int64_t cols) {
+    const int sizes[3] = {type == PP_TYPE_F32 ? 8 : 16, 4, 1};
+    ls_plan p = {};
+    for (int i = 0;; ++i) {
+        p.held = sizes[i];
+        p.size = (long long)sizes[i] * LS_STEP;
+        p.segs = (int)((cols + p.size - 1) / p.size);
+        if (i == 2) return p;
+        const int64_t next = (cols + (int64_t)sizes[i + 1] * LS_STEP - 1) / ((int64_t)sizes[i + 1] * LS_STEP);
+        if (next > p.segs && (next > 64 || rows * p.segs >= LS_ENOUGH)) return p;
+    }
+}
+
+// No more segments than this of any number of rows up to `rows` (those that are not the largest are less than LS_ENOUGH
+// segments of the size before, of at most four each).
+static inline int64_t ls_most(int type, int64_t rows, int64_t cols) {
+    const int64_t size = (int64_t)(type == PP_TYPE_F32 ? 8 : 16) * LS_STEP, most = rows * ((cols + size - 1) / size);
+    return most > 4 * LS_ENOUGH ? most : 4 * LS_ENOUGH;
+}
+
+// Eight logits as floats, -infinity behind the n-th
+template <class Y> __device__ __forceinline__ PpRaw<Y> ls_load(const typename Y::T *p, long long n) {
+    typedef typename Y::T T;
+    PpRaw<Y> r;
+    if (n >= 8) {
+#pragma unroll
+        for (int i = 0; i < PpRaw<Y>::W; ++i) r.w[i] = ((const pp_any16<sizeof(T)> *)p)[i].v;
+    } else {
+        T t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = i < n ? p[i] : (T)-__builtin_inff();
+        __builtin_memcpy(&r, t, sizeof(r));
+    }
+    return r;
+}
+
+__device__ __forceinline__ float ls_max8(const float *v) {
+    float m = __builtin_fmaxf(__builtin_fmaxf(v[0], v[1]), v[2]);
+    m = __builtin_fmaxf(__builtin_fmaxf(m, v[3]), v[4]);
+    m = __builtin_fmaxf(__builtin_fmaxf(m, v[5]), v[6]);
+    return __builtin_fmaxf(m, v[7]);
+}
+
+// What a maximum is subtracted as: 0 where there is nothing but -infinity (then every term is 0)
+__device__ __forceinline__ float ls_base(float m) { return m == -__builtin_inff() ? 0.0f : m; }
+
+template <int WAVES> __device__ __forceinline__ float ls_group_max(float v, float *room) {
+    v = pp_wave_max(v);
+    if (!(threadIdx.x & (PP_WAVE - 1))) room[threadIdx.x / PP_WAVE] = v;
+    __syncthreads();
+    v = room[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) v = __builtin_fmaxf(v, room[w]);
+    return v;
+}
+
+// Numbers in the order of their keys; -0 as 0.  -infinity: key 0, which stands for none.
+__device__ __forceinline__ unsigned ls_key(float x) {
+    if (x == -__builtin_inff()) return 0;
+    const unsigned b = pp_bits(x + 0.0f);
+    return b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float ls_value(unsigned key) { return pp_bits(key ^ (key & 0x80000000u ? 0x80000000u : 0xffffffffu)); }

@@ -21,11 +21,17 @@ PP_TYPE_F32, PP_TYPE_F16, PP_TYPE_BF16 = 0, 1, 2
 PP_PACK_INT8, PP_PACK_FP4 = 0, 1
 PP_ACT_GELU, PP_ACT_GELU_TANH, PP_ACT_SILU = 0, 1, 2
 PP_LINEAR_FORWARD, PP_LINEAR_BACKWARD_INPUT, PP_LINEAR_BACKWARD_WEIGHT = 0, 1, 2
+PP_SCAN_FORWARD, PP_SCAN_BACKWARD = 0, 1
+PP_DISTILL_TOP, PP_DISTILL_REST = 0, 1
+PP_TOP_MAX = 128
 PP_LAYER_MAX_ROWS, PP_LAYER_MAX_COLS, PP_LAYER_MAX_LD_DW = 1 << 30, 1 << 22, 1 << 24
 BLOCK, GROUP = 32, 128
 
 EXPORTS = ("pp_pack", "pp_unpack", "pp_act_forward", "pp_act_backward", "pp_linear_workspace_bytes",
-           "pp_linear_forward", "pp_linear_backward_input", "pp_linear_backward_weight")
+           "pp_linear_forward", "pp_linear_backward_input", "pp_linear_backward_weight",
+           "pp_norm_forward", "pp_norm_workspace_bytes", "pp_norm_backward", "pp_scan_workspace_bytes", "pp_scan_kept_rows",
+           "pp_scan_forward", "pp_scan_backward", "pp_scan_step", "pp_logprob_workspace_bytes", "pp_logprob_forward",
+           "pp_logprob_backward", "pp_distill_workspace_bytes", "pp_distill_loss")
 
 TYPES = {torch.float32: PP_TYPE_F32, torch.float16: PP_TYPE_F16, torch.bfloat16: PP_TYPE_BF16}
 _CODES = {PP_PACK_INT8: (torch.int8, GROUP), PP_PACK_FP4: (torch.uint8, GROUP // 2)}
@@ -46,9 +52,22 @@ def lib():
         L.pp_linear_forward.argtypes = [i32, i64, i64, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, sz, vp]
         L.pp_linear_backward_input.argtypes = [i32, i64, i64, i64, vp, i64, vp, vp, vp, i64, vp, sz, vp]
         L.pp_linear_backward_weight.argtypes = [i32, i64, i64, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, sz, vp]
+        f32 = ctypes.c_float
+        L.pp_norm_forward.argtypes = [i32, i64, i64] + [vp, i64] * 2 + [vp, f32] + [vp, i64] * 2 + [vp] * 6
+        L.pp_norm_workspace_bytes.argtypes = [i32, i64, i64]
+        L.pp_norm_backward.argtypes = [i32, i64, i64] + [vp, i64] * 2 + [vp] * 4 + [vp, i64] * 2 + [vp, vp, vp, sz, vp]
+        L.pp_scan_workspace_bytes.argtypes = [i32, i32, i64, i64]
+        L.pp_scan_kept_rows.argtypes = [i32, i64, i64]
+        L.pp_scan_forward.argtypes = [i32, i64, i64] + [vp, i64] * 2 + [i64, vp, vp, vp, i64, vp, vp, vp, sz, vp]
+        L.pp_scan_backward.argtypes = [i32, i64, i64] + [vp, i64] * 3 + [i64] + [vp] * 4 + [vp, i64] * 2 + [vp, vp, sz, vp]
+        L.pp_scan_step.argtypes = [i32, i64, i64] + [vp, i64] * 2 + [i64, vp, vp, vp, i64, vp]
+        L.pp_logprob_workspace_bytes.argtypes = [i32, i64, i64, i32]
+        L.pp_logprob_forward.argtypes = [i32, i64, i64, vp, i64, f32, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.pp_logprob_backward.argtypes = [i32, i64, i64, vp, i64, f32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.pp_distill_workspace_bytes.argtypes = [i32, i64, i64, i32]
+        L.pp_distill_loss.argtypes = [i32, i32, i64, i64, vp, i64, f32, i32, vp, vp, vp, vp, vp, i64, vp, sz, vp]
         for name in EXPORTS:
-            getattr(L, name).restype = i32
-        L.pp_linear_workspace_bytes.restype = sz
+            getattr(L, name).restype = sz if name.endswith("_bytes") else i64 if name.endswith("_rows") else i32
         _lib = L
     return _lib
 
@@ -137,14 +156,24 @@ def _packed(pair, fmt, rows, cols, name, dev):
     return codes.data_ptr(), scales.data_ptr()
 
 
-def _vector(t, n, name, dev):
+def _values(t, shape, dtype, name, dev):
+    """Pointer of contiguous values of this shape; None: none."""
     if t is None:
         return None
-    if t.get_device() != dev or t.dtype != torch.float32 or t.shape != (n,) or not t.is_contiguous():
-        raise ValueError("%s must be %d contiguous float32 values on the GPU of the other operands" % (name, n))
+    if t.get_device() != dev or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be %s contiguous %s values on the GPU of the other operands" % (name, " x ".join(map(str, shape)), dtype))
     if t.requires_grad:
         _no_history(name)
     return t.data_ptr()
+
+
+def _vector(t, n, name, dev):
+    return _values(t, (n,), torch.float32, name, dev)
+
+
+def _optional(t, dtype, rows, cols, name, dev):
+    """(data pointer, row stride) of a matrix; None: none."""
+    return (None, 0) if t is None else _matrix(t, dtype, rows, cols, name, dev)
 
 
 def _workspace(t, dev):
@@ -227,3 +256,142 @@ def pp_linear_backward_weight(dy, x_kept, dw_in, dw, db, workspace):
     ws, nbytes = _workspace(workspace, dev)
     _check(lib().pp_linear_backward_weight(type_, rows, n_in, n_out, pdy, lddy, xc, xs, pin, pdw, lddw,
                                            _vector(db, n_out, "db", dev), ws, nbytes, _stream(dev)))
+
+
+def pp_norm_forward(x, res, gain, eps, total, y, y_kept=None, total_kept=None, inv=None):
+    """res, gain: or None; total, y, y_kept, total_kept, inv: out, or None (y and y_kept not both)."""
+    type_, rows, cols, px, ldx, dev = _first(x, "x")
+    pr, ldr = _optional(res, x.dtype, rows, cols, "res", dev)
+    pt, ldt = _optional(total, x.dtype, rows, cols, "total", dev)
+    py, ldy = _optional(y, x.dtype, rows, cols, "y", dev)
+    yc, ys = _packed(y_kept, PP_PACK_INT8, rows, cols, "y_kept", dev)
+    tc, ts = _packed(total_kept, PP_PACK_INT8, rows, cols, "total_kept", dev)
+    _check(lib().pp_norm_forward(type_, rows, cols, px, ldx, pr, ldr, _vector(gain, cols, "gain", dev), eps, pt, ldt, py, ldy, yc, ys, tc, ts,
+                                 _vector(inv, rows, "inv", dev), _stream(dev)))
+
+
+def pp_norm_workspace_bytes(dtype, rows, cols):
+    """dtype: of dy, as torch's."""
+    return int(lib().pp_norm_workspace_bytes(TYPES.get(dtype, -1), rows, cols))
+
+
+def pp_norm_backward(dy, total, inv, gain, dtotal, dx, dgain_in, dgain, workspace):
+    """total: the forward pass's sum, as a matrix or packed (PP_PACK_INT8); dtotal: the gradient that reaches it beside the norm, or
+    None; dgain_in: what is added to (None = nothing; may be dgain); dgain: or None."""
+    type_, rows, cols, pdy, lddy, dev = _first(dy, "dy")
+    kept = isinstance(total, (tuple, list))
+    pt, ldt = (None, 0) if kept else _matrix(total, dy.dtype, rows, cols, "total", dev)
+    tc, ts = _packed(total if kept else None, PP_PACK_INT8, rows, cols, "total", dev)
+    pdt, lddt = _optional(dtotal, dy.dtype, rows, cols, "dtotal", dev)
+    pdx, lddx = _matrix(dx, dy.dtype, rows, cols, "dx", dev)
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().pp_norm_backward(type_, rows, cols, pdy, lddy, pt, ldt, tc, ts, _vector(inv, rows, "inv", dev), _vector(gain, cols, "gain", dev),
+                                  pdt, lddt, pdx, lddx, _vector(dgain_in, cols, "dgain_in", dev), _vector(dgain, cols, "dgain", dev), ws, nbytes,
+                                  _stream(dev)))
+
+
+def pp_scan_workspace_bytes(call, dtype, rows, cols):
+    """dtype: of gate, as torch's."""
+    return int(lib().pp_scan_workspace_bytes(call, TYPES.get(dtype, -1), rows, cols))
+
+
+def pp_scan_kept_rows(dtype, rows, cols):
+    """Rows of the states that pp_scan_forward keeps for pp_scan_backward; -1 if a size or the type is out of range."""
+    return int(lib().pp_scan_kept_rows(TYPES.get(dtype, -1), rows, cols))
+
+
+def _sequences(starts, dev):
+    """(number of sequences, pointer of where they start)"""
+    if starts is None:
+        return 1, None
+    if starts.dim() != 1 or starts.shape[0] < 1:
+        raise ValueError("starts must be int32 values, one more than there are sequences")
+    return starts.shape[0] - 1, _values(starts, tuple(starts.shape), torch.int32, "starts", dev)
+
+
+def _kept_states(kept, type_, rows, cols, dev):
+    return _values(kept, (lib().pp_scan_kept_rows(type_, rows, cols), cols), torch.float32, "kept", dev)
+
+
+def pp_scan_forward(gate, v, starts, h0, h, h_last, kept, workspace):
+    """starts: int32, the rows where sequences start and, last, where the last one ends; None = one sequence of all rows.  h0: float32
+    [sequences][cols] or None = zero; h_last (the same shape), kept (float32 [pp_scan_kept_rows][cols]): out, or None."""
+    type_, rows, cols, pg, ldg, dev = _first(gate, "gate")
+    pv, ldv = _matrix(v, gate.dtype, rows, cols, "v", dev)
+    seqs, ps = _sequences(starts, dev)
+    ph, ldh = _matrix(h, gate.dtype, rows, cols, "h", dev)
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().pp_scan_forward(type_, rows, cols, pg, ldg, pv, ldv, seqs, ps, _values(h0, (seqs, cols), torch.float32, "h0", dev), ph, ldh,
+                                 _values(h_last, (seqs, cols), torch.float32, "h_last", dev), _kept_states(kept, type_, rows, cols, dev), ws, nbytes,
+                                 _stream(dev)))
+
+
+def pp_scan_backward(dh, gate, v, starts, h0, kept, dh_last, dgate, dv, dh0, workspace):
+    """h0, kept: as in pp_scan_forward; dh_last: float32 [sequences][cols] or None = zero; dh0 (the same shape): out, or None."""
+    type_, rows, cols, pdh, lddh, dev = _first(dh, "dh")
+    pg, ldg = _matrix(gate, dh.dtype, rows, cols, "gate", dev)
+    pv, ldv = _matrix(v, dh.dtype, rows, cols, "v", dev)
+    seqs, ps = _sequences(starts, dev)
+    pdg, lddg = _matrix(dgate, dh.dtype, rows, cols, "dgate", dev)
+    pdv, lddv = _matrix(dv, dh.dtype, rows, cols, "dv", dev)
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().pp_scan_backward(type_, rows, cols, pdh, lddh, pg, ldg, pv, ldv, seqs, ps, _values(h0, (seqs, cols), torch.float32, "h0", dev),
+                                  _kept_states(kept, type_, rows, cols, dev), _values(dh_last, (seqs, cols), torch.float32, "dh_last", dev),
+                                  pdg, lddg, pdv, lddv, _values(dh0, (seqs, cols), torch.float32, "dh0", dev), ws, nbytes, _stream(dev)))
+
+
+def pp_scan_step(gate, v, slots, state, h):
+    """slots: int32 [rows] of different slots (one outside the pool: the row is padding), or None = row r has slot r; state: float32
+    [slots][cols], in and out."""
+    type_, rows, cols, pg, ldg, dev = _first(gate, "gate")
+    pv, ldv = _matrix(v, gate.dtype, rows, cols, "v", dev)
+    ph, ldh = _matrix(h, gate.dtype, rows, cols, "h", dev)
+    n_slots = state.shape[0]
+    _check(lib().pp_scan_step(type_, rows, cols, pg, ldg, pv, ldv, n_slots, _values(slots, (rows,), torch.int32, "slots", dev),
+                              _values(state, (n_slots, cols), torch.float32, "state", dev), ph, ldh, _stream(dev)))
+
+
+def pp_logprob_workspace_bytes(dtype, rows, cols, top):
+    """dtype: of the logits, as torch's."""
+    return int(lib().pp_logprob_workspace_bytes(TYPES.get(dtype, -1), rows, cols, top))
+
+
+def pp_logprob_forward(logits, temperature, tokens, logp, entropy, norm, top_index, top_logp, workspace):
+    """tokens: int32 [rows], or None without logp; logp, entropy: float32 [rows], norm: float32 [rows][2], top_index, top_logp: int32 and
+    float32 [rows][top] (both or none): out, or None."""
+    type_, rows, cols, pl, ld, dev = _first(logits, "logits")
+    if (top_index is None) != (top_logp is None):
+        raise ValueError("top_index and top_logp are given both or not at all")
+    top = 0 if top_index is None else top_index.shape[-1]
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().pp_logprob_forward(type_, rows, cols, pl, ld, temperature, _values(tokens, (rows,), torch.int32, "tokens", dev),
+                                    _vector(logp, rows, "logp", dev), _vector(entropy, rows, "entropy", dev),
+                                    _values(norm, (rows, 2), torch.float32, "norm", dev), top,
+                                    _values(top_index, (rows, top), torch.int32, "top_index", dev),
+                                    _values(top_logp, (rows, top), torch.float32, "top_logp", dev), ws, nbytes, _stream(dev)))
+
+
+def pp_logprob_backward(logits, temperature, tokens, norm, dlogp, entropy, dentropy, dlogits):
+    """dlogp, dentropy: float32 [rows] or None = zero; entropy: as the forward pass gave it, needed with dentropy; dlogits may be logits."""
+    type_, rows, cols, pl, ld, dev = _first(logits, "logits")
+    pd, ldd = _matrix(dlogits, logits.dtype, rows, cols, "dlogits", dev)
+    _check(lib().pp_logprob_backward(type_, rows, cols, pl, ld, temperature, _values(tokens, (rows,), torch.int32, "tokens", dev),
+                                     _values(norm, (rows, 2), torch.float32, "norm", dev), _vector(dlogp, rows, "dlogp", dev),
+                                     _vector(entropy, rows, "entropy", dev), _vector(dentropy, rows, "dentropy", dev), pd, ldd, _stream(dev)))
+
+
+def pp_distill_workspace_bytes(dtype, rows, cols, top):
+    """dtype: of the logits, as torch's."""
+    return int(lib().pp_distill_workspace_bytes(TYPES.get(dtype, -1), rows, cols, top))
+
+
+def pp_distill_loss(kind, logits, temperature, top_index, top_value, weight, loss, dlogits, workspace):
+    """kind: PP_DISTILL_TOP or PP_DISTILL_REST; top_index, top_value: int32 and float32 [rows][top], the teacher's; weight: float32 [rows] or
+    None = 1; loss: float32 [rows]; dlogits: or None; may be logits."""
+    type_, rows, cols, pl, ld, dev = _first(logits, "logits")
+    pd, ldd = _optional(dlogits, logits.dtype, rows, cols, "dlogits", dev)
+    top = top_index.shape[-1]
+    ws, nbytes = _workspace(workspace, dev)
+    _check(lib().pp_distill_loss(kind, type_, rows, cols, pl, ld, temperature, top, _values(top_index, (rows, top), torch.int32, "top_index", dev),
+                                 _values(top_value, (rows, top), torch.float32, "top_value", dev), _vector(weight, rows, "weight", dev),
+                                 _vector(loss, rows, "loss", dev), pd, ldd, ws, nbytes, _stream(dev)))

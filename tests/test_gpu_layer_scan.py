@@ -1,0 +1,265 @@
+"""The gated recurrence against the formula in 64 bits, token by token (marker gpu).
+
+Bounds, with u = 2^-24: s = sigmoid(-|gate|) is right to (8 + 2 |gate|) u of itself (exp2 of a product, a reciprocal, two units each).  A step
+adds 2 roundings of values of at most M, the largest state or value so far, and s |v - h| (8 + 2 |gate|) u; what a state is off by
+before it counts with a.  Where a sequence is divided, a chunk's share of what came before it is rounded like a step, at most once for every
+token: 4 roundings of M a step are taken.  The backward recurrence is the same with g.  exp2 gives 0 for what is no normal number: s may
+also be off by 2^-126.
+"""
+import numpy as np
+import pytest
+
+from layer_helpers import Guarded, assert_within, on_gpu, torch_type
+from oracle import rows as o
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def lists(rows, kind, rng):
+    if kind == "one":
+        return [0, rows]
+    if kind == "padded":        # rows before and behind, empty sequences in every place
+        lo, hi = rows // 7, rows - rows // 5
+        cuts = sorted(int(x) for x in rng.integers(lo, hi + 1, 5))
+        return [lo, lo] + cuts + [cuts[-1], hi, hi]
+    if kind == "tokens":        # every sequence one token
+        return list(range(rows + 1))
+    cuts = sorted(set(int(x) for x in rng.integers(0, rows + 1, max(1, rows // 9))))
+    return [0] + cuts + [rows]
+
+
+def case(rows, cols, kind, seed, spread=2.0):
+    rng = np.random.default_rng(seed)
+    starts = lists(rows, kind, rng)
+    n = len(starts) - 1
+    draw = lambda *s: rng.standard_normal(s)  # noqa: E731
+    return starts, draw(rows, cols) * spread + draw(1, cols), draw(rows, cols), draw(n, cols), draw(rows, cols) * 0.1, draw(n, cols) * 0.1
+
+
+def state_bounds(gate, v, starts, h0):
+    """How far h may be off, and what a token finds."""
+    err, found = np.zeros_like(v), np.zeros_like(v)
+    a, s = o.sigmoid(gate), o.sigmoid(-np.abs(gate))
+    before = o.scan_forward(gate, v, starts, h0)[2]
+    for n in range(len(starts) - 1):
+        e, m = np.zeros(v.shape[1]), np.abs(h0[n])
+        for t in range(starts[n], starts[n + 1]):
+            found[t] = e
+            m = np.maximum(m, np.abs(v[t]))
+            e = a[t] * e + U * (4 * m + s[t] * np.abs(v[t] - before[t]) * (8 + 2 * np.abs(gate[t])))
+            err[t] = e
+    return err, found
+
+
+def gradient_bounds(dh, gate, starts, dh_last, g):
+    """How far g may be off, and dh0."""
+    err, first = np.zeros_like(dh), np.zeros((len(starts) - 1, dh.shape[1]))
+    a, s = o.sigmoid(gate), o.sigmoid(-np.abs(gate))
+    for n in range(len(starts) - 1):
+        e, m = np.zeros(dh.shape[1]), np.abs(dh_last[n])
+        for t in range(starts[n + 1] - 1, starts[n] - 1, -1):
+            m = np.maximum(m, np.maximum(np.abs(g[t]), np.abs(dh[t])))
+            e = e + 2 * U * m
+            err[t] = e
+            e = a[t] * e + U * (2 * m + s[t] * np.abs(g[t]) * (8 + 2 * np.abs(gate[t])))
+        first[n] = e
+    return err, first
+
+
+def floats(v):
+    import torch
+    t = torch.from_numpy(v).float().cuda()
+    return t, t.double().cpu().numpy()
+
+
+def workspace(call, t, rows, cols):
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    return torch.full((pp.pp_scan_workspace_bytes(call, torch_type(t), rows, cols),), 255, dtype=torch.uint8, device="cuda")
+
+
+def run(t, starts, gate, v, h0, dh, dh_last, carried=True, pad=0, off=0, null=False):
+    """Forward and backward, checked; h0 and dh_last not given where not carried."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    rows, cols = gate.shape
+    mg, gate = on_gpu(gate, t, pad, off)
+    mv, v = on_gpu(v, t, 0, off)
+    md, dh = on_gpu(dh, t, pad, 0)
+    n = len(starts) - 1
+    th0, h0 = floats(h0 if carried else h0 * 0)
+    tdl, dh_last = floats(dh_last if carried else dh_last * 0)
+    ts = None if null else torch.tensor(starts, dtype=torch.int32, device="cuda")
+    h, dg, dv = Guarded(rows, cols, t, pad, off), Guarded(rows, cols, t, 0, off), Guarded(rows, cols, t, pad, 0)
+    last, dh0 = (torch.full((n * cols + 9,), 7.0, device="cuda") for _ in range(2))
+    view = lambda x: x[:n * cols].view(n, cols)  # noqa: E731
+    kept = torch.full((pp.pp_scan_kept_rows(torch_type(t), rows, cols), cols), 7.0, device="cuda")
+    pp.pp_scan_forward(mg, mv, ts, th0 if carried else None, h.m, view(last), kept, workspace(0, t, rows, cols))
+    pp.pp_scan_backward(md, mg, mv, ts, th0 if carried else None, kept, tdl if carried else None, dg.m, dv.m, view(dh0), workspace(1, t, rows, cols))
+    want, want_last, before = o.scan_forward(gate, v, starts, h0)
+    err, found = state_bounds(gate, v, starts, h0)
+    used = slice(starts[0], starts[-1])
+    outside = np.r_[0:starts[0], starts[-1]:rows]
+    got = h.values()
+    assert_within(got[used], want[used], err[used], t)
+    assert (got[outside] == 77).all()
+    last_err = np.array([err[starts[i + 1] - 1] if starts[i + 1] > starts[i] else np.zeros(cols) for i in range(n)])
+    assert_within(view(last).double().cpu().numpy(), want_last, last_err, "f32")
+    dgate, dvalue, want0, g = o.scan_backward(dh, gate, v, starts, h0, dh_last)
+    ge, first = gradient_bounds(dh, gate, starts, dh_last, g)
+    a, b = o.sigmoid(gate), o.sigmoid(-gate)
+    rel = (12 + 2 * np.abs(gate)) * U
+    gv, gg = dv.values(), dg.values()
+    assert_within(gv[used], dvalue[used], (b * ge + rel * np.abs(dvalue) + 2.0 ** -126 * np.abs(g))[used], t)
+    near = a * b * (np.abs(before - v) * ge + np.abs(g) * (found + 2 * U * (np.abs(before) + np.abs(v)))) + 2 * rel * np.abs(dgate) + 2.0 ** -126 * np.abs((before - v) * g)
+    assert_within(gg[used], dgate[used], near[used], t)
+    assert (gv[outside] == 77).all() and (gg[outside] == 77).all()
+    assert_within(view(dh0).double().cpu().numpy(), want0, first, "f32")
+    assert (last[n * cols:] == 7).all() and (dh0[n * cols:] == 7).all()
+
+
+@pytest.mark.parametrize("kind", ["one", "padded", "tokens", "mixed"])
+@pytest.mark.parametrize("rows, cols", [(1, 1), (2, 70), (31, 8), (33, 130), (64, 64), (127, 5), (200, 300), (513, 129), (1000, 66)])
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+def test_sequences(t, rows, cols, kind):
+    if kind == "padded" and rows < 30:
+        pytest.skip("no room for padding")
+    starts, gate, v, h0, dh, dh_last = case(rows, cols, kind, rows * 7 + cols)
+    run(t, starts, gate, v, h0, dh, dh_last, True, 0, 0)
+    run(t, starts, gate, v, h0, dh, dh_last, rows % 2 == 0, 3, 1, null=kind == "one")
+
+
+@pytest.mark.parametrize("cols", [3, 258])
+@pytest.mark.parametrize("kind", ["one", "padded"])
+def test_long(kind, cols):
+    starts, gate, v, h0, dh, dh_last = case(9001, cols, kind, cols)
+    run("f32", starts, gate, v, h0, dh, dh_last)
+    run("bf16", starts, gate + 3, v, h0, dh, dh_last)
+
+
+def test_gates_at_their_ends():
+    """A gate that forgets everything, one that forgets nothing, and all between; infinite ones too."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    gate = np.repeat(np.array([[-300.0, -90.0, -17.0, -1.0, 0.0, 1.0, 17.0, 90.0, 300.0]]), 70, 0)
+    rng = np.random.default_rng(1)
+    v, h0, dh = rng.standard_normal((70, 9)), rng.standard_normal((1, 9)), rng.standard_normal((70, 9))
+    run("f32", [0, 70], gate, v, h0, dh, rng.standard_normal((1, 9)))
+    for inf, want in ((np.inf, h0), (-np.inf, v)):
+        tg, tv, th0 = (floats(x)[0] for x in (np.full((70, 9), inf), v, h0))
+        h = torch.empty_like(tv)
+        pp.pp_scan_forward(tg, tv, None, th0, h, None, None, workspace(0, "f32", 70, 9))
+        assert torch.equal(h, floats(np.broadcast_to(want, (70, 9)).copy())[0])
+
+
+def test_a_state_that_is_kept_does_not_drift():
+    """With one gate of 9 throughout (1 - a = 1.2e-4) and one value, the state comes to the value.  Each step is rounded to u M: err = a err + u M, at
+    most u M / (1 - a) = 4.9e-4 M; 1 - a, right to 26 u of itself, changes the way there by 26 u n (1 - a) a^n < 1e-6 M."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    rows, cols = 60000, 64
+    gate = torch.full((rows, cols), 9.0, device="cuda")
+    v = torch.linspace(0.5, 2, cols, device="cuda").expand(rows, cols).contiguous()
+    h = torch.empty_like(v)
+    pp.pp_scan_forward(gate, v, None, None, h, None, None, workspace(0, "f32", rows, cols))
+    a = 1 / (1 + np.exp(-9.0))
+    want = v.double() * (1 - a ** torch.arange(1, rows + 1, device="cuda", dtype=torch.float64))[:, None]
+    assert ((h - want).abs() <= 4.9e-4 * v).all()
+
+
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_one_sequence_does_not_reach_another(t):
+    """NaN and infinity stay in their sequence and channel, wherever it ends."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    starts, gate, v, h0, dh, dh_last = case(700, 40, "mixed", 5)
+    n = len(starts) - 1
+    bad = next(i for i in range(n // 2, n) if starts[i + 1] - starts[i] >= 2)
+    clean = [None] * 2
+    for k in range(2):
+        if k:
+            v[starts[bad], 3], h0[bad, 7], dh[starts[bad + 1] - 1, 9], v[starts[bad] + 1, 11] = np.nan, np.inf, np.nan, -np.inf
+        mg, mv, md = (on_gpu(x, t)[0] for x in (gate, v, dh))
+        th0, tdl = floats(h0)[0], floats(dh_last)[0]
+        ts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        h, dg, dv, last, dh0 = torch.zeros_like(mv), torch.zeros_like(mv), torch.zeros_like(mv), torch.zeros_like(th0), torch.zeros_like(th0)
+        kept = torch.empty(pp.pp_scan_kept_rows(torch_type(t), 700, 40), 40, device="cuda")
+        pp.pp_scan_forward(mg, mv, ts, th0, h, last, kept, workspace(0, t, 700, 40))
+        pp.pp_scan_backward(md, mg, mv, ts, th0, kept, tdl, dg, dv, dh0, workspace(1, t, 700, 40))
+        clean[k] = (h, dg, dv, last, dh0)
+    lo, hi = starts[bad], starts[bad + 1]
+    rows = torch.ones(700, 40, dtype=torch.bool, device="cuda")
+    rows[lo:hi, [3, 7, 9, 11]] = False
+    seqs = torch.ones(n, 40, dtype=torch.bool, device="cuda")
+    seqs[bad, [3, 7, 9, 11]] = False
+    for a, b, where in zip(clean[0], clean[1], (rows, rows, rows, seqs, seqs)):
+        assert torch.equal(a[where], b[where])
+    assert not torch.isfinite(clean[1][0][lo:hi, 3]).any() and not torch.isfinite(clean[1][0][lo, 7])
+
+
+def test_starts_that_are_held_to_the_rows():
+    """Starts outside the rows, and falling ones: nothing outside is touched (what falling ones give is not said)."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    rows, cols = 100, 33
+    for starts, exact in (([-5, 40, 900], [0, 40, 100]), ([60, 20, 80, 10], None)):
+        ts = torch.tensor(starts, dtype=torch.int32, device="cuda")
+        mg, gate = on_gpu(np.random.default_rng(1).standard_normal((rows, cols)), "f32")
+        h, dg, dv = (Guarded(rows, cols, "f32") for _ in range(3))
+        n = len(starts) - 1
+        last, dh0 = torch.full((n, cols), 7.0, device="cuda"), torch.full((n, cols), 7.0, device="cuda")
+        kept = torch.zeros(pp.pp_scan_kept_rows(torch.float32, rows, cols), cols, device="cuda")
+        pp.pp_scan_forward(mg, mg, ts, None, h.m, last, kept, workspace(0, "f32", rows, cols))
+        pp.pp_scan_backward(mg, mg, mg, ts, None, kept, None, dg.m, dv.m, dh0, workspace(1, "f32", rows, cols))
+        for x in (h, dg, dv):
+            x.values()
+        if exact:
+            want, want_last, _ = o.scan_forward(gate, gate, exact, None)
+            np.testing.assert_allclose(h.values(), want, atol=1e-5)
+            np.testing.assert_allclose(last.cpu().numpy(), want_last, atol=1e-5)
+
+
+def test_no_rows_and_no_sequences():
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    x, h0 = torch.empty(0, 9, device="cuda"), torch.randn(2, 9, device="cuda")
+    ts, last, dh0 = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(2, 9, device="cuda"), torch.zeros(2, 9, device="cuda")
+    pp.pp_scan_forward(x, x, ts, h0, x, last, None, workspace(0, "f32", 0, 9))
+    pp.pp_scan_backward(x, x, x, ts, h0, x, h0, x, x, dh0, workspace(1, "f32", 0, 9))
+    assert torch.equal(last, h0) and torch.equal(dh0, h0)
+    y = torch.full((4, 9), 3.0, device="cuda")
+    pp.pp_scan_forward(torch.randn_like(y), torch.randn_like(y), ts[:1], None, y, None, None, workspace(0, "f32", 4, 9))
+    assert (y == 3).all()
+
+
+@pytest.mark.parametrize("rows, cols", [(1, 1), (1, 4096), (7, 33), (64, 130), (300, 1000)])
+@pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
+def test_step(t, rows, cols):
+    """One token a row, against the same step of the formula: states in slots, some rows padding."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    rng = np.random.default_rng(rows + cols)
+    n = rows + 5
+    mg, gate = on_gpu(rng.standard_normal((rows, cols)) * 3, t, 3, 1)
+    mv, v = on_gpu(rng.standard_normal((rows, cols)), t)
+    state, sv = floats(rng.standard_normal((n, cols)))
+    slots = rng.permutation(n)[:rows].astype(np.int32)
+    slots[3::5] = [-1, n, 2 ** 31 - 1, -2 ** 31][rows % 4]
+    for which in (torch.from_numpy(slots).cuda(), None):
+        at = slots if which is not None else np.arange(rows)
+        h, s = Guarded(rows, cols, t, 0, 3), state.clone()
+        pp.pp_scan_step(mg, mv, which, s, h.m)
+        on = (at >= 0) & (at < n)
+        want = np.full((rows, cols), 77.0)
+        old = sv[at[on]]
+        want[on] = o.sigmoid(gate[on]) * old + o.sigmoid(-gate[on]) * v[on]
+        m = np.maximum(np.abs(old), np.abs(v[on]))
+        bound = U * (4 * m + o.sigmoid(-np.abs(gate[on])) * np.abs(v[on] - old) * (8 + 2 * np.abs(gate[on])))
+        got = h.values()
+        assert_within(got[on], want[on], bound, t)
+        assert (got[~on] == 77).all()
+        new = s.double().cpu().numpy()
+        assert_within(new[at[on]], want[on], bound, "f32")
+        rest = np.setdiff1d(np.arange(n), at[on])
+        assert (new[rest] == sv[rest]).all()
