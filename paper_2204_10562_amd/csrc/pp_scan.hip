@@ -1,7 +1,11 @@
 // pp_scan_forward, pp_scan_backward, pp_scan_step: the gated linear recurrence h_t = a_t h_(t-1) + (1 - a_t) v_t, a = sigmoid(gate).
 #include "pp_rows.h"
 
-#define SC_CHUNK 32  // tokens between kept states
+#define SC_CHUNK 32               // tokens that a wave holds, and between kept states
+#define SC_WAVES 4                // of a workgroup, one behind the other in time
+#define SC_TILE (SC_CHUNK * SC_WAVES)
+#define SC_GROUP 16               // tiles between states that are passed on whole
+#define SC_MAX_TILES (1 << 24)    // of a launch
 #define SC_MAX_SEQS (1 << 30)
 
 // A token's gate.  s = sigmoid(-|gate|) is the smaller of a and 1 - a; the state moves by it from the nearer end, so that one that
@@ -22,68 +26,457 @@ struct sc_gate {
     __device__ __forceinline__ float slope() const { return __builtin_fmaf(-s, s, s); }                        // a (1 - a)
 };
 
+// A stretch of tokens as what it makes of the state before it, h -> A h + H.  x says A: 1 - A where that is below 1/2 (so that a
+// state which is kept loses nothing), -A otherwise, and SC_CUT where a sequence starts in the stretch: then nothing of h is left.
+// H and 1 - A come from the same recurrence, so for one value throughout H = (1 - A) v, however long.
+#define SC_CUT 2.0f
+#define SC_EMPTY (~0ull)  // no stretch yet
+
+__device__ __forceinline__ float sc_after(float x, float H, float h) {
+    const float r = __builtin_fmaf(-x, h, H);
+    const float near = h + (__builtin_isinf(h) ? H : r);  // (an infinite state stays one)
+    return x == SC_CUT ? H : pp_bits(x) >> 31 ? r : near;
+}
+__device__ __forceinline__ float sc_share(float A, float D) { return D < 0.5f ? D : A != A ? pp_bits(0x7fc00000u) : -A; }
+// (x, H) and behind it (x2, H2)
+__device__ __forceinline__ void sc_join(float &x, float &H, float x2, float H2) {
+    const bool n1 = pp_bits(x) >> 31, n2 = pp_bits(x2) >> 31;
+    const float A = n1 ? -x : 1.0f - x, D = n1 ? 1.0f + x : x, A2 = n2 ? -x2 : 1.0f - x2, D2 = n2 ? 1.0f + x2 : x2;
+    H = sc_after(x2, H2, H);
+    x = x == SC_CUT || x2 == SC_CUT ? SC_CUT : sc_share(A * A2, __builtin_fmaf(A, D2, D));
+}
+__device__ __forceinline__ unsigned long long sc_word(float x, float H) { return (unsigned long long)pp_bits(H) << 32 | pp_bits(x); }
+
 struct sc_args {
     long long rows, cols, seqs;
     const int *starts;
-    const float *h0;
-    float *kept;
+    int tiles, lanes_tiles;         // in time, and over the channels
+    unsigned *ticket;
+    unsigned long long *stretch;    // [tiles][width] what a tile makes of the state before it
+    unsigned long long *whole;      // [tiles / SC_GROUP][width] the state before a group of tiles
+    long long width;
 };
 
-// Rows lo .. hi - 1 of sequence n
-__device__ __forceinline__ void sc_bounds(const sc_args &a, long long n, long long &lo, long long &hi) {
-    lo = a.starts ? a.starts[n] : 0;
-    hi = a.starts ? a.starts[n + 1] : a.rows;
-    lo = lo < 0 ? 0 : lo > a.rows ? a.rows : lo;
-    hi = hi < lo ? lo : hi > a.rows ? a.rows : hi;
+// What a wave's tokens t0 .. t0 + 31 have to do with sequences, a bit each: whether a sequence has them, starts with them, ends with
+// them; and the sequence of the first of them.
+struct sc_marks {
+    unsigned in, first, last;
+    int seq;
+};
+__device__ __forceinline__ long long sc_start(const int *starts, long long rows, long long n) {
+    const long long t = starts[n];
+    return t < 0 ? 0 : t > rows ? rows : t;
+}
+__device__ __forceinline__ unsigned sc_from(long long t) { return t <= 0 ? ~0u : t >= 32 ? 0u : ~0u << t; }  // bits t and above
+
+__device__ __forceinline__ sc_marks sc_mark(const int *__restrict__ starts, long long rows, int seqs, long long t0) {
+    sc_marks m;
+    if (!starts) {
+        m.in = ~sc_from(rows - t0);
+        m.first = t0 == 0;
+        m.last = rows - 1 - t0 >= 0 && rows - 1 - t0 < 32 ? 1u << (rows - 1 - t0) : 0u;
+        m.seq = 0;
+        return m;
+    }
+    const long long begin = sc_start(starts, rows, 0), end = sc_start(starts, rows, seqs);
+    m.in = sc_from(begin - t0) & ~sc_from(end - t0);
+    int lo = 0, hi = seqs;  // the first n with starts[n] >= t0, seqs if none before
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (sc_start(starts, rows, mid) >= t0) hi = mid;
+        else lo = mid + 1;
+    }
+    m.seq = lo - 1;
+    m.first = 0;
+    unsigned next = 0;
+    for (int n = lo; n <= seqs; ++n) {
+        const long long t = sc_start(starts, rows, n) - t0;
+        if (t == 32) next = 1;
+        if (t < 0 || t >= 32) break;
+        if (n < seqs) m.first |= 1u << t;
+    }
+    m.last = m.first >> 1 | next << 31;
+    if (end - t0 > 0 && end - t0 <= 32) m.last |= 1u << (end - t0 - 1);
+    m.first &= m.in;
+    m.last &= m.in;
+    return m;
+}
+// the sequence that starts with token t, where `n` is that of a token before (or -1)
+__device__ __forceinline__ int sc_next(const int *__restrict__ starts, int seqs, int n, long long rows, long long t) {
+    if (!starts) return 0;
+    do ++n;
+    while (n < seqs - 1 && sc_start(starts, rows, n + 1) <= t);
+    return n < seqs ? n : seqs - 1;
+}
+// the one that ends with token t, where `n` is that of a token behind (or seqs)
+__device__ __forceinline__ int sc_previous(const int *__restrict__ starts, int n, long long rows, long long t) {
+    if (!starts) return 0;
+    do --n;
+    while (n > 0 && sc_start(starts, rows, n) > t);
+    return n < 0 ? 0 : n;
 }
 
-template <class Y>
-__global__ __launch_bounds__(64) void k_scan_forward(sc_args a, const typename Y::T *__restrict__ gate, long long ld_gate, const typename Y::T *__restrict__ v,
-                                                     long long ld_v, typename Y::T *__restrict__ h, long long ld_h, float *__restrict__ h_last) {
-    const long long c = blockIdx.x * 64ll + threadIdx.x;
-    if (c >= a.cols) return;
-    for (long long n = blockIdx.y; n < a.seqs; n += gridDim.y) {
-        long long lo, hi;
-        sc_bounds(a, n, lo, hi);
-        float s = a.h0 ? a.h0[n * a.cols + c] : 0.0f;
-        for (long long t = lo; t < hi; ++t) {
-            if (a.kept && !(t % SC_CHUNK)) a.kept[t / SC_CHUNK * a.cols + c] = s;
-            s = sc_gate(Y::get(gate[t * ld_gate + c])).next(s, Y::get(v[t * ld_v + c]));
-            h[t * ld_h + c] = Y::put(s);
+// W channels of a token, W of a 4-byte word's 16-bit values or one value
+template <class Y, int W> struct sc_lane {
+    typedef typename Y::T T;
+    long long c;   // first channel
+    int n;         // channels that there are
+    long long at;  // where a whole word is read from
+    unsigned shift;
+    bool full;     // all lanes have W
+    __device__ __forceinline__ sc_lane(long long tile, long long cols) {
+        c = (tile * PP_WAVE + (threadIdx.x & (PP_WAVE - 1))) * W;
+        n = cols - c >= W ? W : cols > c ? (int)(cols - c) : 0;
+        at = c + W <= cols ? c : cols - W;
+        shift = n == 1 && W == 2 ? 16 : 0;
+        full = (tile + 1) * PP_WAVE * W <= cols;
+    }
+    __device__ __forceinline__ unsigned load(const T *row) const {
+        if constexpr (sizeof(T) * W == 4) {
+            unsigned u;
+            __builtin_memcpy(&u, row + at, 4);
+            return u;
+        } else return __builtin_bit_cast(unsigned short, row[at]);
+    }
+    __device__ __forceinline__ static float get(unsigned raw, int w) {
+        if constexpr (sizeof(T) == 4) return pp_bits(raw);
+        else return Y::get(__builtin_bit_cast(T, (unsigned short)(raw >> (16 * w))));
+    }
+    __device__ __forceinline__ void store(T *row, const float *v) const {
+        T t[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) t[w] = Y::put(v[w]);
+        if (full) __builtin_memcpy(row + c, t, sizeof(t));
+        else
+#pragma unroll
+            for (int w = 0; w < W; ++w)
+                if (w < n) row[c + w] = t[w];
+    }
+    __device__ __forceinline__ void get_floats(const float *row, float *v) const {  // zeros where row is NULL
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[w] = row && w < n ? row[c + w] : 0.0f;
+    }
+    __device__ __forceinline__ void put_floats(float *row, const float *v) const {
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            if (w < n) row[c + w] = v[w];
+    }
+};
+
+template <int W> struct sc_room {
+    float x[SC_WAVES][W * PP_WAVE], H[SC_WAVES][W * PP_WAVE];
+    float bx[SC_WAVES][W * PP_WAVE], bH[SC_WAVES][W * PP_WAVE];
+    float whole[W * PP_WAVE];
+    unsigned ticket;
+};
+
+__device__ __forceinline__ unsigned long long sc_peek(const unsigned long long *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void sc_tell(unsigned long long *p, unsigned long long v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// The state (of W channels a lane) before wave `wave` of tile number `order` of its channels, in the order of the recurrence, from the waves' own
+// stretches in room.x, room.H; and what the tile's successors need.  Every wave takes part.
+//
+// A tile waits for tiles of its channels that took a lower ticket only.  These run already and wait for lower ones in turn, so every wait
+// ends.  A word says by itself whether it is there (SC_EMPTY: not yet), so no other memory has to be ordered with it, and
+// what is added up in which order depends on the tile's number alone.
+template <int W>
+__device__ __forceinline__ void sc_carry(const sc_args &a, sc_room<W> &room, int order, long long lanes_tile, int wave, float *h) {
+    const int lane = threadIdx.x & (PP_WAVE - 1), group = order / SC_GROUP, place = order % SC_GROUP;
+    const long long col = (lanes_tile * PP_WAVE + lane) * W;
+#pragma unroll
+    for (int w = 0; w < W; ++w) h[w] = 0.0f;
+    if (a.tiles > 1) {
+        if (wave == 0) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const int l = lane * W + w;
+                float x = room.x[0][l], H = room.H[0][l];
+#pragma unroll
+                for (int k = 1; k < SC_WAVES; ++k) sc_join(x, H, room.x[k][l], room.H[k][l]);
+                sc_tell(a.stretch + order * a.width + col + w, sc_word(x, H));
+            }
         }
-        if (h_last) h_last[n * a.cols + c] = s;
+        const int begin = wave * (SC_GROUP / SC_WAVES);
+        if (begin < place) {
+            unsigned long long word[SC_GROUP / SC_WAVES][W];
+            bool wait = true;
+            while (wait) {
+                wait = false;
+#pragma unroll
+                for (int k = 0; k < SC_GROUP / SC_WAVES; ++k)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) word[k][w] = begin + k < place ? sc_peek(a.stretch + (order - place + begin + k) * a.width + col + w) : 0;
+#pragma unroll
+                for (int k = 0; k < SC_GROUP / SC_WAVES; ++k)
+#pragma unroll
+                    for (int w = 0; w < W; ++w) wait = wait || (unsigned)word[k][w] == (unsigned)SC_EMPTY;
+                wait = __any(wait);
+                if (wait) __builtin_amdgcn_s_sleep(8);
+            }
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                float x = pp_bits((unsigned)word[0][w]), H = pp_bits((unsigned)(word[0][w] >> 32));
+#pragma unroll
+                for (int k = 1; k < SC_GROUP / SC_WAVES; ++k)
+                    if (begin + k < place) sc_join(x, H, pp_bits((unsigned)word[k][w]), pp_bits((unsigned)(word[k][w] >> 32)));
+                room.bx[wave][lane * W + w] = x;
+                room.bH[wave][lane * W + w] = H;
+            }
+        }
+        if (wave == SC_WAVES - 1) {
+            unsigned long long word[W];
+            bool wait = group > 0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) word[w] = 0;
+            while (wait) {
+                wait = false;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    word[w] = sc_peek(a.whole + group * a.width + col + w);
+                    wait = wait || (unsigned)word[w] == (unsigned)SC_EMPTY;
+                }
+                wait = __any(wait);
+                if (wait) __builtin_amdgcn_s_sleep(8);
+            }
+#pragma unroll
+            for (int w = 0; w < W; ++w) room.whole[lane * W + w] = pp_bits((unsigned)(word[w] >> 32));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const int l = lane * W + w;
+            h[w] = room.whole[l];
+#pragma unroll
+            for (int k = 0; k < SC_WAVES; ++k)
+                if (k * (SC_GROUP / SC_WAVES) < place) h[w] = sc_after(room.bx[k][l], room.bH[k][l], h[w]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < SC_WAVES; ++k) {
+        if (k == wave) break;
+#pragma unroll
+        for (int w = 0; w < W; ++w) h[w] = sc_after(room.x[k][lane * W + w], room.H[k][lane * W + w], h[w]);
+    }
+    if (a.tiles > 1 && wave == SC_WAVES - 1 && place == SC_GROUP - 1 && order + 1 < a.tiles)
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+            sc_tell(a.whole + (group + 1) * a.width + col + w, sc_word(0.0f, sc_after(room.x[wave][lane * W + w], room.H[wave][lane * W + w], h[w])));
+}
+
+// Number of the workgroup's tile: tickets, so that a tile's predecessors run before it
+template <int W> __device__ __forceinline__ unsigned sc_ticket(const sc_args &a, sc_room<W> &room) {
+    if (a.tiles == 1) return blockIdx.x;
+    if (!threadIdx.x) room.ticket = atomicAdd(a.ticket, 1u);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(room.ticket);
+}
+
+// a and 1 - a of a token from s, the smaller one, negative where that is a
+__device__ __forceinline__ void sc_sides(float s, float &a, float &u) {
+    const float m = __builtin_fabsf(s), r = 1.0f - m;
+    const bool keeps = !(pp_bits(s) >> 31);
+    a = keeps ? r : m;
+    u = keeps ? m : r;
+}
+
+template <class Y, int W>
+__global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_forward(sc_args a, const typename Y::T *__restrict__ gate, long long ld_gate,
+                                                                       const typename Y::T *__restrict__ v, long long ld_v, const float *__restrict__ h0,
+                                                                       typename Y::T *__restrict__ h, long long ld_h, float *__restrict__ h_last,
+                                                                       float *__restrict__ kept) {
+    __shared__ sc_room<W> room;
+    const unsigned ticket = sc_ticket(a, room);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PP_WAVE), lane = threadIdx.x & (PP_WAVE - 1);
+    const int order = ticket / a.lanes_tiles, lanes_tile = ticket % a.lanes_tiles;
+    const long long t0 = (long long)order * SC_TILE + wave * SC_CHUNK;
+    const sc_lane<Y, W> lanes(lanes_tile, a.cols);
+    unsigned f[SC_CHUNK], x[SC_CHUNK];
+#pragma unroll
+    for (int i = 0; i < SC_CHUNK; ++i) {
+        const long long t = t0 + i < a.rows ? t0 + i : a.rows - 1;
+        f[i] = lanes.load(gate + t * ld_gate);
+        x[i] = lanes.load(v + t * ld_v);
+    }
+    const sc_marks m = sc_mark(a.starts, a.rows, (int)a.seqs, t0);
+    if (!lanes.full)
+#pragma unroll
+        for (int i = 0; i < SC_CHUNK; ++i) f[i] >>= lanes.shift, x[i] >>= lanes.shift;
+    float s[SC_CHUNK][W], H[W], A[W], D[W], from[W];
+    // the wave's own stretch; of the sequences that start in it the last one counts
+    const int cut = m.first ? 31 - __builtin_clz(m.first) : -1;
+    if (cut >= 0) {
+        int n = m.seq;
+        for (unsigned left = m.first; left; left &= left - 1) n = sc_next(a.starts, (int)a.seqs, n, a.rows, t0 + __builtin_ctz(left));
+        lanes.get_floats(h0 ? h0 + n * a.cols : NULL, from);
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) H[w] = 0.0f, A[w] = 1.0f, D[w] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < SC_CHUNK; ++i) {
+        if (!(m.in >> i & 1)) continue;
+        if (i == cut)
+#pragma unroll
+            for (int w = 0; w < W; ++w) H[w] = from[w];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float g = lanes.get(f[i], w), e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e);
+            const float small = e * r;
+            const bool keeps = g >= 0.0f;
+            s[i][w] = keeps ? small : -small;
+            const float ka = keeps ? r : small, ku = keeps ? small : r;
+            H[w] = __builtin_fmaf(ka, H[w], ku * lanes.get(x[i], w));
+            D[w] = __builtin_fmaf(ka, D[w], ku);
+            A[w] *= ka;
+        }
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        room.x[wave][lane * W + w] = cut >= 0 ? SC_CUT : sc_share(A[w], D[w]);
+        room.H[wave][lane * W + w] = H[w];
+    }
+    __syncthreads();
+    sc_carry<W>(a, room, order, lanes_tile, wave, H);
+    if (kept && t0 < a.rows) lanes.put_floats(kept + t0 / SC_CHUNK * a.cols, H);
+    int n = m.seq;
+#pragma unroll
+    for (int i = 0; i < SC_CHUNK; ++i) {
+        if (!(m.in >> i & 1)) continue;
+        if (m.first >> i & 1) {
+            n = sc_next(a.starts, (int)a.seqs, n, a.rows, t0 + i);
+            lanes.get_floats(h0 ? h0 + n * a.cols : NULL, H);
+        }
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            float ka, ku;
+            sc_sides(s[i][w], ka, ku);
+            H[w] = __builtin_fmaf(ka, H[w], ku * lanes.get(x[i], w));
+        }
+        lanes.store(h + (t0 + i) * ld_h, H);
+        if (h_last && (m.last >> i & 1)) lanes.put_floats(h_last + n * a.cols, H);
     }
 }
 
-template <class Y>
-__global__ __launch_bounds__(64) void k_scan_backward(sc_args a, const typename Y::T *__restrict__ dh, long long ld_dh, const typename Y::T *__restrict__ gate,
-                                                      long long ld_gate, const typename Y::T *__restrict__ v, long long ld_v,
-                                                      const float *__restrict__ dh_last, typename Y::T *__restrict__ dgate, long long ld_dgate,
-                                                      typename Y::T *__restrict__ dv, long long ld_dv, float *__restrict__ dh0) {
-    __shared__ float before[SC_CHUNK][64];
-    const long long c = blockIdx.x * 64ll + threadIdx.x;
-    if (c >= a.cols) return;
-    for (long long n = blockIdx.y; n < a.seqs; n += gridDim.y) {
-        long long lo, hi;
-        sc_bounds(a, n, lo, hi);
-        float g = dh_last ? dh_last[n * a.cols + c] : 0.0f;  // a_(t+1) g_(t+1)
-        for (long long end = hi; end > lo;) {
-            const long long chunk = (end - 1) / SC_CHUNK, begin = chunk * SC_CHUNK > lo ? chunk * SC_CHUNK : lo;
-            float s = begin > lo ? a.kept[chunk * a.cols + c] : a.h0 ? a.h0[n * a.cols + c] : 0.0f;
-            for (long long t = begin; t < end; ++t) {
-                before[t - begin][threadIdx.x] = s;
-                s = sc_gate(Y::get(gate[t * ld_gate + c])).next(s, Y::get(v[t * ld_v + c]));
-            }
-            for (long long t = end - 1; t >= begin; --t) {
-                const sc_gate p(Y::get(gate[t * ld_gate + c]));
-                g += Y::get(dh[t * ld_dh + c]);
-                dv[t * ld_dv + c] = Y::put(p.take(g));
-                dgate[t * ld_dgate + c] = Y::put(p.slope() * (before[t - begin][threadIdx.x] - Y::get(v[t * ld_v + c])) * g);
-                g = p.keep(g);
-            }
-            end = begin;
+// The same from the last tile to the first, for c = a_t g_t; the state before every 32 tokens was kept.
+template <class Y, int W>
+__global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_backward(sc_args a, const typename Y::T *__restrict__ dh, long long ld_dh,
+                                                                        const typename Y::T *__restrict__ gate, long long ld_gate,
+                                                                        const typename Y::T *__restrict__ v, long long ld_v, const float *__restrict__ h0,
+                                                                        const float *__restrict__ kept, const float *__restrict__ dh_last,
+                                                                        typename Y::T *__restrict__ dgate, long long ld_dgate, typename Y::T *__restrict__ dv,
+                                                                        long long ld_dv, float *__restrict__ dh0) {
+    __shared__ sc_room<W> room;
+    const unsigned ticket = sc_ticket(a, room);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PP_WAVE), lane = threadIdx.x & (PP_WAVE - 1);
+    const int order = ticket / a.lanes_tiles, lanes_tile = ticket % a.lanes_tiles;
+    const long long t0 = (long long)(a.tiles - 1 - order) * SC_TILE + (SC_WAVES - 1 - wave) * SC_CHUNK;
+    const sc_lane<Y, W> lanes(lanes_tile, a.cols);
+    unsigned f[SC_CHUNK], x[SC_CHUNK], d[SC_CHUNK];
+#pragma unroll
+    for (int i = 0; i < SC_CHUNK; ++i) {
+        const long long t = t0 + i < a.rows ? t0 + i : a.rows - 1;
+        f[i] = lanes.load(gate + t * ld_gate);
+        d[i] = lanes.load(dh + t * ld_dh);
+        x[i] = lanes.load(v + t * ld_v);
+    }
+    float state[W];
+    lanes.get_floats(t0 < a.rows ? kept + t0 / SC_CHUNK * a.cols : NULL, state);
+    const sc_marks m = sc_mark(a.starts, a.rows, (int)a.seqs, t0);
+    if (!lanes.full)
+#pragma unroll
+        for (int i = 0; i < SC_CHUNK; ++i) f[i] >>= lanes.shift, x[i] >>= lanes.shift, d[i] >>= lanes.shift;
+    float s[SC_CHUNK][W], C[W], A[W], D[W], from[W];
+    // of the sequences that end in the stretch the first one counts, which may have begun before
+    const int cut = m.last ? __builtin_ctz(m.last) : -1;
+    int behind = m.seq, ends = m.seq;  // the sequence of the last token, and that of token `cut`
+    for (unsigned left = m.first; left; left &= left - 1) {
+        const int t = __builtin_ctz(left);
+        behind = sc_next(a.starts, (int)a.seqs, behind, a.rows, t0 + t);
+        if (t <= cut) ends = behind;
+    }
+    if (cut >= 0) lanes.get_floats(dh_last ? dh_last + ends * a.cols : NULL, from);
+#pragma unroll
+    for (int w = 0; w < W; ++w) C[w] = 0.0f, A[w] = 1.0f, D[w] = 0.0f;
+#pragma unroll
+    for (int i = SC_CHUNK - 1; i >= 0; --i) {
+        if (!(m.in >> i & 1)) continue;
+        if (i == cut)
+#pragma unroll
+            for (int w = 0; w < W; ++w) C[w] = from[w];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float g = lanes.get(f[i], w), e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e);
+            const float small = e * r;
+            const bool keeps = g >= 0.0f;
+            s[i][w] = keeps ? small : -small;
+            const float ka = keeps ? r : small, ku = keeps ? small : r;
+            C[w] = ka * (lanes.get(d[i], w) + C[w]);
+            D[w] = __builtin_fmaf(ka, D[w], ku);
+            A[w] *= ka;
         }
-        if (dh0) dh0[n * a.cols + c] = g;
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        room.x[wave][lane * W + w] = cut >= 0 ? SC_CUT : sc_share(A[w], D[w]);
+        room.H[wave][lane * W + w] = C[w];
+    }
+    // the states that the tokens find, less their values
+    float p[SC_CHUNK][W];
+    int n = m.seq;
+#pragma unroll
+    for (int i = 0; i < SC_CHUNK; ++i) {
+        if (!(m.in >> i & 1)) continue;
+        if (m.first >> i & 1) {
+            n = sc_next(a.starts, (int)a.seqs, n, a.rows, t0 + i);
+            lanes.get_floats(h0 ? h0 + n * a.cols : NULL, state);
+        }
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            const float value = lanes.get(x[i], w);
+            float ka, ku;
+            sc_sides(s[i][w], ka, ku);
+            p[i][w] = state[w] - value;
+            state[w] = __builtin_fmaf(ka, state[w], ku * value);
+        }
+    }
+    __syncthreads();
+    sc_carry<W>(a, room, order, lanes_tile, wave, C);
+    n = behind;
+    bool own = true;  // whether `n` is the sequence of what comes next
+#pragma unroll
+    for (int i = SC_CHUNK - 1; i >= 0; --i) {
+        if (!(m.in >> i & 1)) continue;
+        if (m.last >> i & 1) {
+            if (!own) n = sc_previous(a.starts, n, a.rows, t0 + i);
+            lanes.get_floats(dh_last ? dh_last + n * a.cols : NULL, C);
+        }
+        own = !(m.first >> i & 1);
+        float df[W], dx[W];
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            float ka, ku;
+            sc_sides(s[i][w], ka, ku);
+            const float g = lanes.get(d[i], w) + C[w];
+            dx[w] = ku * g;
+            C[w] = ka * g;
+            df[w] = p[i][w] * ku * C[w];
+        }
+        lanes.store(dgate + (t0 + i) * ld_dgate, df);
+        lanes.store(dv + (t0 + i) * ld_dv, dx);
+        if (dh0 && (m.first >> i & 1)) lanes.put_floats(dh0 + n * a.cols, C);
+    }
+}
+
+// What tiles wait for is not there yet.
+__global__ __launch_bounds__(256) void k_scan_clear(unsigned *ticket, unsigned long long *words, long long n) {
+    if (blockIdx.x == 0 && !threadIdx.x) *ticket = 0;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) words[i] = SC_EMPTY;
+}
+
+// Sequences without tokens: what they begin with is what they end with.
+__global__ __launch_bounds__(256) void k_scan_empty(sc_args a, const float *__restrict__ from, float *__restrict__ to) {
+    for (long long n = blockIdx.x; n < a.seqs; n += gridDim.x) {
+        if (a.starts ? sc_start(a.starts, a.rows, n) < sc_start(a.starts, a.rows, n + 1) : a.rows > 0) continue;
+        for (long long c = threadIdx.x; c < a.cols; c += 256) to[n * a.cols + c] = from ? from[n * a.cols + c] : 0.0f;
     }
 }
 
@@ -108,24 +501,55 @@ __global__ __launch_bounds__(256) void k_scan_step(long long rows, long long col
     }
 }
 
+static int64_t sc_tiles(int64_t rows) { return (rows + SC_TILE - 1) / SC_TILE; }
+
 static bool sc_bad(int type, int64_t rows, int64_t cols, int64_t seqs, const int32_t *starts, const float *h0, const float *kept, const float *x,
                    const float *y) {
     if (pp_bad_sizes(type, rows, cols) || seqs < 0 || seqs > SC_MAX_SEQS || (!starts && seqs != 1)) return true;
     for (const void *p : {(const void *)starts, (const void *)h0, (const void *)kept, (const void *)x, (const void *)y})
         if ((uintptr_t)p & 3) return true;
-    return false;
+    return sc_tiles(rows) * ((cols + PP_WAVE - 1) / PP_WAVE) > SC_MAX_TILES;
 }
+
+static int64_t sc_width(int64_t cols) { return (cols + 2 * PP_WAVE - 1) / (2 * PP_WAVE) * (2 * PP_WAVE); }
 
 extern "C" size_t pp_scan_workspace_bytes(int call, int type, int64_t rows, int64_t cols) {
     if (pp_bad_sizes(type, rows, cols) || (call != PP_SCAN_FORWARD && call != PP_SCAN_BACKWARD)) return 0;
-    return 256;
+    const int64_t tiles = sc_tiles(rows);
+    return 256 + pp_align256((size_t)(tiles + tiles / SC_GROUP + 1) * sc_width(cols) * 8);
 }
 
 extern "C" int64_t pp_scan_kept_rows(int type, int64_t rows, int64_t cols) {
     return pp_bad_sizes(type, rows, cols) ? -1 : (rows + SC_CHUNK - 1) / SC_CHUNK;
 }
 
-static dim3 sc_grid(int64_t cols, int64_t seqs) { return dim3((unsigned)((cols + 63) / 64), (unsigned)(seqs < 4096 ? seqs : 4096)); }
+// The tiles of a call, and its workspace made ready.  launch(args, grid, channels to a lane as a constant)
+template <class Y, class F>
+static int sc_run(int64_t rows, int64_t cols, int64_t seqs, const int32_t *starts, void *workspace, hipStream_t st, const float *from, float *to, F launch) {
+    sc_args a = {rows, cols, seqs, starts};
+    if (to) {
+        k_scan_empty<<<(unsigned)(seqs < 65536 ? seqs : 65536), 256, 0, st>>>(a, from, to);
+        if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
+    }
+    if (!rows) return PP_OK;
+    const bool pairs = sizeof(typename Y::T) == 2 && cols > 1;
+    const int64_t per = pairs ? 2 * PP_WAVE : PP_WAVE, lanes = (cols + per - 1) / per, tiles = sc_tiles(rows);
+    a.tiles = (int)tiles;
+    a.lanes_tiles = (int)lanes;
+    a.width = sc_width(cols);
+    a.ticket = (unsigned *)workspace;
+    a.stretch = (unsigned long long *)((char *)workspace + 256);
+    a.whole = a.stretch + tiles * a.width;
+    if (tiles > 1) {
+        const int64_t words = (tiles + tiles / SC_GROUP + 1) * a.width, groups = (words + 1023) / 1024;
+        k_scan_clear<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.ticket, a.stretch, words);
+        if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
+    }
+    if (pairs) {
+        if constexpr (sizeof(typename Y::T) == 2) launch(a, (unsigned)(tiles * lanes), std::integral_constant<int, 2>());
+    } else launch(a, (unsigned)(tiles * lanes), std::integral_constant<int, 1>());
+    return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+}
 
 extern "C" int pp_scan_forward(int type, int64_t rows, int64_t cols, const void *gate, int64_t ld_gate, const void *v, int64_t ld_v, int64_t seqs,
                                const int32_t *starts, const float *h0, void *h, int64_t ld_h, float *h_last, float *kept, void *workspace,
@@ -135,12 +559,13 @@ extern "C" int pp_scan_forward(int type, int64_t rows, int64_t cols, const void 
         return PP_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < pp_scan_workspace_bytes(PP_SCAN_FORWARD, type, rows, cols)) return PP_ERR_WORKSPACE;
     if (!seqs) return PP_OK;
-    const sc_args a = {rows, cols, seqs, starts, h0, kept};
+    hipStream_t st = (hipStream_t)stream;
     return pp_by_type(type, [&](auto tag) {
         typedef decltype(tag) Y;
         typedef typename Y::T T;
-        k_scan_forward<Y><<<sc_grid(cols, seqs), 64, 0, (hipStream_t)stream>>>(a, (const T *)gate, ld_gate, (const T *)v, ld_v, (T *)h, ld_h, h_last);
-        return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+        return sc_run<Y>(rows, cols, seqs, starts, workspace, st, h0, h_last, [&](const sc_args &a, unsigned grid, auto w) {
+            k_scan_forward<Y, decltype(w)::value><<<grid, SC_WAVES * PP_WAVE, 0, st>>>(a, (const T *)gate, ld_gate, (const T *)v, ld_v, h0, (T *)h, ld_h, h_last, kept);
+        });
     });
 }
 
@@ -153,13 +578,14 @@ extern "C" int pp_scan_backward(int type, int64_t rows, int64_t cols, const void
         return PP_ERR_INVALID_ARG;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < pp_scan_workspace_bytes(PP_SCAN_BACKWARD, type, rows, cols)) return PP_ERR_WORKSPACE;
     if (!seqs) return PP_OK;
-    const sc_args a = {rows, cols, seqs, starts, h0, (float *)kept};
+    hipStream_t st = (hipStream_t)stream;
     return pp_by_type(type, [&](auto tag) {
         typedef decltype(tag) Y;
         typedef typename Y::T T;
-        k_scan_backward<Y><<<sc_grid(cols, seqs), 64, 0, (hipStream_t)stream>>>(a, (const T *)dh, ld_dh, (const T *)gate, ld_gate, (const T *)v, ld_v, dh_last,
-                                                                                (T *)dgate, ld_dgate, (T *)dv, ld_dv, dh0);
-        return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+        return sc_run<Y>(rows, cols, seqs, starts, workspace, st, dh_last, dh0, [&](const sc_args &a, unsigned grid, auto w) {
+            k_scan_backward<Y, decltype(w)::value><<<grid, SC_WAVES * PP_WAVE, 0, st>>>(a, (const T *)dh, ld_dh, (const T *)gate, ld_gate, (const T *)v, ld_v, h0, kept,
+                                                                                           dh_last, (T *)dgate, ld_dgate, (T *)dv, ld_dv, dh0);
+        });
     });
 }
 

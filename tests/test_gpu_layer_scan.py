@@ -92,8 +92,9 @@ def run(t, starts, gate, v, h0, dh, dh_last, carried=True, pad=0, off=0, null=Fa
     tdl, dh_last = floats(dh_last if carried else dh_last * 0)
     ts = None if null else torch.tensor(starts, dtype=torch.int32, device="cuda")
     h, dg, dv = Guarded(rows, cols, t, pad, off), Guarded(rows, cols, t, 0, off), Guarded(rows, cols, t, pad, 0)
-    last, dh0 = (torch.full((n * cols + 9,), 7.0, device="cuda") for _ in range(2))
-    view = lambda x: x[:n * cols].view(n, cols)  # noqa: E731
+    front, size = 2 * cols, n * cols
+    last, dh0 = (torch.full((front + size + 9,), 7.0, device="cuda") for _ in range(2))
+    view = lambda x: x[front:front + size].view(n, cols)  # noqa: E731
     kept = torch.full((pp.pp_scan_kept_rows(torch_type(t), rows, cols), cols), 7.0, device="cuda")
     pp.pp_scan_forward(mg, mv, ts, th0 if carried else None, h.m, view(last), kept, workspace(0, t, rows, cols))
     pp.pp_scan_backward(md, mg, mv, ts, th0 if carried else None, kept, tdl if carried else None, dg.m, dv.m, view(dh0), workspace(1, t, rows, cols))
@@ -116,7 +117,7 @@ def run(t, starts, gate, v, h0, dh, dh_last, carried=True, pad=0, off=0, null=Fa
     assert_within(gg[used], dgate[used], near[used], t)
     assert (gv[outside] == 77).all() and (gg[outside] == 77).all()
     assert_within(view(dh0).double().cpu().numpy(), want0, first, "f32")
-    assert (last[n * cols:] == 7).all() and (dh0[n * cols:] == 7).all()
+    assert all((x[:front] == 7).all() and (x[front + size:] == 7).all() for x in (last, dh0))
 
 
 @pytest.mark.parametrize("kind", ["one", "padded", "tokens", "mixed"])
@@ -154,8 +155,10 @@ def test_gates_at_their_ends():
 
 
 def test_a_state_that_is_kept_does_not_drift():
-    """With one gate of 9 throughout (1 - a = 1.2e-4) and one value, the state comes to the value.  Each step is rounded to u M: err = a err + u M, at
-    most u M / (1 - a) = 4.9e-4 M; 1 - a, right to 26 u of itself, changes the way there by 26 u n (1 - a) a^n < 1e-6 M."""
+    """With one gate of 9 throughout (1 - a = 1.2e-4) and one value, the state comes to the value.  A sum of products that were rounded one by one
+    would be off by u M / (1 - a) = 4.9e-4 M.  What 32 tokens do is h + (H - D h) with D = 1 - a^32 = 3.9e-3: a rounding of M, and H and D, which
+    come from one recurrence of 64 roundings each, are 66 u D M off together.  err = (1 - D) err + u M (1 + 66 D) stays below u M (254 + 66), and
+    within the 32 tokens 64 u M more: 2.3e-5 M.  1 - a, right to 26 u of itself, changes the way there by 26 u n (1 - a) a^n < 1e-6 M."""
     import torch
     from paper_2204_10562_amd import layer as pp
     rows, cols = 60000, 64
@@ -165,7 +168,7 @@ def test_a_state_that_is_kept_does_not_drift():
     pp.pp_scan_forward(gate, v, None, None, h, None, None, workspace(0, "f32", rows, cols))
     a = 1 / (1 + np.exp(-9.0))
     want = v.double() * (1 - a ** torch.arange(1, rows + 1, device="cuda", dtype=torch.float64))[:, None]
-    assert ((h - want).abs() <= 4.9e-4 * v).all()
+    assert ((h - want).abs() <= 2.4e-5 * v).all()
 
 
 @pytest.mark.parametrize("t", ["bf16", "f32"])
