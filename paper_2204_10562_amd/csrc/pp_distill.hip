@@ -37,7 +37,7 @@ template <int HELD> __device__ __forceinline__ void mark_listed(const ds_args &a
     __syncthreads();
 }
 
-template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_distill_sums(ds_args a, const typename Y::T *__restrict__ logits) {
+template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS, 4) void k_distill_sums(ds_args a, const typename Y::T *__restrict__ logits) {
     const int t = threadIdx.x, words = (HELD + 3) / 4;
     __shared__ unsigned marks[LS_THREADS * ((HELD + 3) / 4)];
     __shared__ float room[8];
@@ -47,11 +47,7 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_dis
         const typename Y::T *x = logits + row * a.ld + first;
         const long long n = a.cols - first < a.size ? a.cols - first : a.size;
         PpRaw<Y> raw[HELD];
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            const long long c = 8ll * (t + i * LS_THREADS);
-            raw[i] = ls_load<Y>(x + c, n - c);
-        }
+        ls_load_all<Y, HELD>(raw, x, n);
         mark_listed<HELD>(a, row, first, marks);
         float v[8], m = -__builtin_inff();
 #pragma unroll
@@ -69,6 +65,7 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_dis
         }
         const float base = ls_base(ls_group_max<4>(m, room));
         float s = 0.0f;
+        ls_hold<Y>(raw);
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
             pp_values<Y>(raw[i], v);

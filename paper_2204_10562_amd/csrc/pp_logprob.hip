@@ -9,7 +9,7 @@
 // Alternatives: each thread knows its chunks' maxima.  The K-th largest of the 256 threads' maxima, found bit by bit by one wave,
 // is at most the K-th largest logit, and the logits from there on lie in the chunks of at most K threads (or tie with them): they
 // are read again, ranked by counting and written in order.  Where ties make them too many, the K-th largest pair of logit and
-// index is found bit by bit by all threads.  Equal logits are ordered by their index, so the order is one.
+// column is found bit by bit by all threads.  Segments' lists are joined in the same way.
 #include "pp_loss.h"
 
 struct lp_args {
@@ -20,7 +20,7 @@ struct lp_args {
     float *logp, *entropy, *norm, *top_logp;
     int *top_index;
     pp_f4 *sums;   // [rows][segs]: m, s, w
-    pp_u2 *kept;   // [rows][segs][top]: key, index, in order; key 0: none
+    unsigned long long *kept;  // [rows][segs][top]: lp_entry, in order
 };
 
 // What a row's sums say: s NaN: no numbers; s = 0: nothing but -infinity.
@@ -44,56 +44,107 @@ template <class Y> __device__ __forceinline__ void put_row(const lp_args &a, lon
     }
 }
 
-__device__ __forceinline__ void put_top(const lp_args &a, long long row, int rank, unsigned key, unsigned index, const lp_row &r) {
+// A logit and its column as one number that orders as the alternatives do: the larger logit first, then the lower column. 0: none.
+typedef unsigned long long lp_entry;
+__device__ __forceinline__ lp_entry lp_make(unsigned key, long long column) { return key ? (lp_entry)key << 32 | (0xffffffffu - (unsigned)column) : 0; }
+__device__ __forceinline__ unsigned lp_key(lp_entry e) { return (unsigned)(e >> 32); }
+__device__ __forceinline__ unsigned lp_column(lp_entry e) { return 0xffffffffu - (unsigned)e; }
+
+__device__ __forceinline__ void put_top(const lp_args &a, long long row, int rank, lp_entry e, const lp_row &r) {
     const bool bad = r.s != r.s;
-    a.top_index[row * a.top + rank] = key && !bad ? (int)index : -1;
-    a.top_logp[row * a.top + rank] = bad ? r.s : key ? r.logp(ls_value(key), a.k) : -__builtin_inff();
+    a.top_index[row * a.top + rank] = e && !bad ? (int)lp_column(e) : -1;
+    a.top_logp[row * a.top + rank] = bad ? r.s : e ? r.logp(ls_value(lp_key(e)), a.k) : -__builtin_inff();
 }
 
 struct lp_room {
-    float wave[8], max[LS_THREADS];
-    unsigned counts[2];
-    float tau;
-    unsigned key[LS_CAP], index[LS_CAP];
+    float wave[8];
+    unsigned max[LS_THREADS];
+    unsigned found, tau, count[4];
+    lp_entry entry[LS_CAP + 8];
 };
 
-// whether (key, index) comes at or before (tk, ti)
-__device__ __forceinline__ bool at_least(unsigned key, unsigned index, unsigned tk, unsigned ti) { return key > tk || (key == tk && index <= ti); }
-
-// Sum of a count over the workgroup; room[0 .. 3] free again behind the next barrier.
-__device__ __forceinline__ unsigned group_count(unsigned c, unsigned *room) {
-    for (int d = 1; d < PP_WAVE; d <<= 1) c += __shfl_xor(c, d);
-    if (!(threadIdx.x & (PP_WAVE - 1))) room[threadIdx.x / PP_WAVE] = c;
-    __syncthreads();
-    c = room[0] + room[1] + room[2] + room[3];
-    __syncthreads();
-    return c;
+// The K-th largest of the 256 keys in room.max, by one wave: bits below `low` are the same for all.  0 if there are fewer.
+__device__ __forceinline__ void find_threshold(lp_room &room, int top, int low) {
+    if (threadIdx.x >= PP_WAVE) return;
+    unsigned key[4], tau = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) key[i] = room.max[threadIdx.x + i * PP_WAVE];
+    for (int bit = 31; bit >= low; --bit) {
+        const unsigned to = tau | 1u << bit;
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c += __popcll(__ballot(key[i] >= to));
+        if (c >= top) tau = to;
+        if (c == top) break;
+    }
+    if (!threadIdx.x) room.tau = tau, room.found = 0;
 }
 
-// The top of a segment x[0 .. n) that starts at column `first`, in order into put(rank, key, index); x is read again.
+// Entries of this thread, `mine` of them wanted, into the room's list.
+template <class F> __device__ __forceinline__ void append(lp_room &room, int mine, F each) {
+    if (!mine) return;
+    unsigned at = atomicAdd(&room.found, (unsigned)mine);
+    each([&](lp_entry e) {
+        if (at < LS_CAP) room.entry[at] = e;
+        ++at;
+    });
+}
+
+__device__ __forceinline__ unsigned group_count(unsigned c, unsigned *room) {
+    for (int d = 1; d < PP_WAVE; d <<= 1) c += __shfl_xor(c, d);
+    __syncthreads();
+    if (!(threadIdx.x & (PP_WAVE - 1))) room[threadIdx.x / PP_WAVE] = c;
+    __syncthreads();
+    return room[0] + room[1] + room[2] + room[3];
+}
+
+// Where ties are too many for the list: the K-th largest entry bit by bit.  all(f) calls f for every entry of this thread.
+template <class F> __device__ __forceinline__ void narrow(lp_room &room, int top, F all) {
+    lp_entry tau = 0;
+#pragma unroll 1
+    for (int bit = 63; bit >= 0; --bit) {
+        const lp_entry to = tau | 1ull << bit;
+        unsigned c = 0;
+        all([&](lp_entry e) { c += e >= to; });
+        if (group_count(c, room.count) >= (unsigned)top) tau = to;
+    }
+    __syncthreads();
+    if (!threadIdx.x) room.found = 0;
+    __syncthreads();
+    all([&](lp_entry e) {
+        if (e && e >= tau) append(room, 1, [&](auto put) { put(e); });
+    });
+    __syncthreads();
+}
+
+// The list's first `top` entries in order into put(rank, entry), and none behind them.  Four lanes to an entry, each with a
+// quarter of the others.
+template <class F> __device__ __forceinline__ void rank_list(lp_room &room, int top, F put) {
+    const int t = threadIdx.x, found = (int)(room.found < LS_CAP ? room.found : LS_CAP), ends = (found + 7) & ~7;
+    if (t < ends - found) room.entry[found + t] = 0;
+    __syncthreads();
+    for (int i = t >> 2; i < ends; i += LS_THREADS / 4) {
+        const lp_entry mine = room.entry[i];
+        unsigned rank = 0;
+        for (int o = t & 3; o < ends; o += 8) rank += (room.entry[o] > mine) + (room.entry[o + 4] > mine);
+        rank += pp_moved<0xB1>(rank);
+        rank += pp_moved<0x4E>(rank);
+        if (!(t & 3) && mine && rank < (unsigned)top) put((int)rank, mine);
+    }
+    for (int rank = found + t; rank < top; rank += LS_THREADS) put(rank, (lp_entry)0);
+}
+
+// The top of a segment x[0 .. n) that starts at column `first`; x is read again.
 template <class Y, int HELD, class F>
 __device__ __forceinline__ void select_top(lp_room &room, const typename Y::T *x, long long n, long long first, int top, const float *chunk_max,
                                            float thread_max, F put) {
     const int t = threadIdx.x;
-    room.max[t] = thread_max;
-    if (!t) room.counts[0] = 0;
+    room.max[t] = ls_key(thread_max);
     __syncthreads();
-    if (t < PP_WAVE) {
-        const int low = sizeof(typename Y::T) == 4 ? 0 : __is_same(Y, PpBF16) ? 16 : 13;  // (bits below are the same for all)
-        unsigned key[4], tau = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) key[i] = ls_key(room.max[t + i * PP_WAVE]);
-        for (int bit = 31; bit >= low; --bit) {
-            const unsigned to = tau | 1u << bit;
-            int c = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) c += __popcll(__ballot(key[i] >= to));
-            if (c >= top) tau = to;
-        }
-        if (!t) room.tau = tau > ls_key(-3.4028235e38f) ? ls_value(tau) : -3.4028235e38f;
-    }
+    find_threshold(room, top, sizeof(typename Y::T) == 4 ? 0 : __is_same(Y, PpBF16) ? 16 : 13);
     __syncthreads();
-    const float tau = room.tau;
+    const unsigned low = 0x00800000u;  // the key of the lowest float
+    const float tau = ls_value(room.tau > low ? room.tau : low);
     unsigned todo = 0;
 #pragma unroll
     for (int i = 0; i < HELD; ++i) todo |= (chunk_max[i] >= tau ? 1u : 0u) << i;
@@ -103,68 +154,31 @@ __device__ __forceinline__ void select_top(lp_room &room, const typename Y::T *x
         const long long c = 8ll * (t + i * LS_THREADS);
         float v[8];
         pp_values<Y>(ls_load<Y>(x + c, n - c), v);
+        int mine = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (v[j] >= tau) {
-                const unsigned at = atomicAdd(&room.counts[0], 1u);
-                if (at < LS_CAP) {
-                    room.key[at] = ls_key(v[j]);
-                    room.index[at] = (unsigned)(first + c + j);
-                }
-            }
+        for (int j = 0; j < 8; ++j) mine += v[j] >= tau;
+        append(room, mine, [&](auto put_one) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (v[j] >= tau) put_one(lp_make(ls_key(v[j]), first + c + j));
+        });
     }
     __syncthreads();
-    unsigned found = room.counts[0];
-    if (found > LS_CAP) {  // (the same for the whole workgroup)
-        unsigned *part = (unsigned *)room.wave, tk = 0, ti = 2 * PP_LAYER_MAX_COLS - 1;
-        auto count = [&](unsigned k, unsigned last) {
-            unsigned c = 0;
+    if (room.found > LS_CAP)
+        narrow(room, top, [&](auto f) {
+#pragma unroll 1
             for (int i = 0; i < HELD; ++i) {
-                const long long at = 8ll * (t + i * LS_THREADS);
+                const long long c = 8ll * (t + i * LS_THREADS);
                 float v[8];
-                pp_values<Y>(ls_load<Y>(x + at, n - at), v);
-                for (int j = 0; j < 8; ++j) {
-                    const unsigned key = v[j] != v[j] ? 0 : ls_key(v[j]);
-                    c += key && at_least(key, (unsigned)(first + at + j), k, last);
-                }
+                pp_values<Y>(ls_load<Y>(x + c, n - c), v);
+                for (int j = 0; j < 8; ++j)
+                    if (v[j] == v[j]) f(lp_make(ls_key(v[j]), first + c + j));
             }
-            return group_count(c, part);
-        };
-        for (int bit = 31; bit >= 0; --bit)
-            if (count(tk | 1u << bit, 0xffffffffu) >= (unsigned)top) tk |= 1u << bit;
-        for (int bit = 22; bit >= 0; --bit)  // the least last index with which there are enough
-            if (count(tk, ti & ~(1u << bit)) >= (unsigned)top) ti &= ~(1u << bit);
-        if (!t) room.counts[0] = 0;
-        __syncthreads();
-        for (int i = 0; i < HELD; ++i) {
-            const long long c = 8ll * (t + i * LS_THREADS);
-            float v[8];
-            pp_values<Y>(ls_load<Y>(x + c, n - c), v);
-            for (int j = 0; j < 8; ++j) {
-                const unsigned key = v[j] != v[j] ? 0 : ls_key(v[j]), index = (unsigned)(first + c + j);
-                if (key && at_least(key, index, tk, ti)) {
-                    const unsigned at = atomicAdd(&room.counts[0], 1u);
-                    if (at < LS_CAP) {
-                        room.key[at] = key;
-                        room.index[at] = index;
-                    }
-                }
-            }
-        }
-        __syncthreads();
-        found = room.counts[0] < LS_CAP ? room.counts[0] : LS_CAP;
-    }
-    for (unsigned i = t; i < found; i += LS_THREADS) {
-        const unsigned key = room.key[i], index = room.index[i];
-        int rank = 0;
-        for (unsigned o = 0; o < found; ++o) rank += room.key[o] > key || (room.key[o] == key && room.index[o] < index);
-        if (rank < top) put(rank, key, index);
-    }
-    for (int rank = t; rank < top; rank += LS_THREADS)
-        if (rank >= (int)found) put(rank, 0u, 0u);
+        });
+    rank_list(room, top, put);
 }
 
-template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_logprob(lp_args a, const typename Y::T *__restrict__ logits) {
+template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS, 4) void k_logprob(lp_args a, const typename Y::T *__restrict__ logits) {
     __shared__ lp_room room;
     const int t = threadIdx.x;
     for (long long item = blockIdx.x; item < a.rows * a.segs; item += gridDim.x) {
@@ -173,19 +187,17 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_log
         const long long n = a.cols - first < a.size ? a.cols - first : a.size;
         PpRaw<Y> raw[HELD];
         float chunk_max[HELD], v[8], m = -__builtin_inff();
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            const long long c = 8ll * (t + i * LS_THREADS);
-            raw[i] = ls_load<Y>(x + c, n - c);
-        }
+        ls_load_all<Y, HELD>(raw, x, n);
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
             pp_values<Y>(raw[i], v);
             chunk_max[i] = ls_max8(v);
             m = __builtin_fmaxf(m, chunk_max[i]);
+            __builtin_amdgcn_sched_barrier(0);  // (chunk by chunk: else all are converted first, and put away)
         }
         const float base = ls_base(ls_group_max<4>(m, room.wave));
         float s = 0.0f, w = 0.0f;
+        ls_hold<Y>(raw);
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
             pp_values<Y>(raw[i], v);
@@ -195,6 +207,7 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_log
                 s += e;
                 w = __builtin_fmaf(e, __builtin_fmaxf(d, -256.0f), w);  // (-infinity: 0)
             }
+            asm volatile("" : "+v"(s), "+v"(w));  // (here and not behind the sums of s, with all that is added put away until then)
         }
         __syncthreads();
         s = pp_group_sum<4>(s, room.wave);
@@ -205,9 +218,9 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_log
         }
         if (a.top) {
             const lp_row r = {base, s, __builtin_amdgcn_logf(s)};
-            select_top<Y, HELD>(room, x, n, first, a.top, chunk_max, m, [&](int rank, unsigned key, unsigned index) {
-                if (a.segs == 1) put_top(a, row, rank, key, index, r);
-                else a.kept[item * a.top + rank] = pp_u2{key, index};
+            select_top<Y, HELD>(room, x, n, first, a.top, chunk_max, m, [&](int rank, lp_entry e) {
+                if (a.segs == 1) put_top(a, row, rank, e, r);
+                else a.kept[item * a.top + rank] = e;
             });
         }
         __syncthreads();
@@ -217,14 +230,14 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_log
 // Sums of segments on the largest maximum: with d = (a segment's - the largest) k, its s and w are multiplied by 2^d, and d is added
 // to every exponent of w.
 template <class Y> __global__ __launch_bounds__(LS_THREADS) void k_logprob_join(lp_args a, const typename Y::T *__restrict__ logits) {
-    __shared__ float room[8];
+    __shared__ lp_room room;
     const int t = threadIdx.x;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const pp_f4 *sums = a.sums + row * a.segs;
         float m = -__builtin_inff(), s = 0.0f, w = 0.0f;
         for (int i = t; i < a.segs; i += LS_THREADS)
             if (sums[i][1] != 0.0f) m = __builtin_fmaxf(m, sums[i][0]);
-        m = ls_base(ls_group_max<4>(m, room));
+        m = ls_base(ls_group_max<4>(m, room.wave));
         for (int i = t; i < a.segs; i += LS_THREADS) {
             const pp_f4 p = sums[i];
             if (p[1] == 0.0f) continue;
@@ -233,37 +246,33 @@ template <class Y> __global__ __launch_bounds__(LS_THREADS) void k_logprob_join(
             w = __builtin_fmaf(e, __builtin_fmaf(p[1], __builtin_fmaxf(d, -256.0f), p[2]), w);
         }
         __syncthreads();
-        s = pp_group_sum<4>(s, room);
-        w = pp_group_sum<4>(w, room + 4);
+        s = pp_group_sum<4>(s, room.wave);
+        w = pp_group_sum<4>(w, room.wave + 4);
         if (!t) put_row<Y>(a, row, logits + row * a.ld, m, s, w);
         if (a.top) {
             const lp_row r = {m, s, __builtin_amdgcn_logf(s)};
-            const pp_u2 *kept = a.kept + row * a.segs * a.top;
-            int some = 0;
-            for (int c = t; c < a.segs * a.top; c += LS_THREADS) {
-                const pp_u2 one = kept[c];
-                if (!one[0]) continue;
-                ++some;
-                const int seg = c / a.top;
-                int rank = c - seg * a.top;
-                for (int o = 0; o < a.segs && rank < a.top; ++o) {  // entries before this one in the other segments' order
-                    if (o == seg) continue;
-                    const pp_u2 *list = kept + o * a.top;
-                    int lo = 0, hi = a.top;
-                    while (lo < hi) {
-                        const int mid = (lo + hi) / 2;
-                        const pp_u2 e = list[mid];
-                        if (e[0] && at_least(e[0], e[1], one[0], one[1])) lo = mid + 1;
-                        else hi = mid;
-                    }
-                    rank += lo;
-                }
-                if (rank < a.top) put_top(a, row, rank, one[0], one[1], r);
+            const lp_entry *kept = a.kept + row * a.segs * a.top;
+            const int n = a.segs * a.top;
+            unsigned most = 0;
+            for (int c = t; c < n; c += LS_THREADS) {
+                const unsigned key = lp_key(kept[c]);
+                most = key > most ? key : most;
+            }
+            room.max[t] = most;
+            __syncthreads();
+            find_threshold(room, a.top, 0);
+            __syncthreads();
+            const unsigned tau = room.tau > 1 ? room.tau : 1;
+            for (int c = t; c < n; c += LS_THREADS) {
+                const lp_entry e = kept[c];
+                append(room, lp_key(e) >= tau, [&](auto put_one) { put_one(e); });
             }
             __syncthreads();
-            const int all = (int)pp_group_sum<4>((float)some, room);  // (at most 2^22: exact)
-            for (int rank = t; rank < a.top; rank += LS_THREADS)
-                if (rank >= all) put_top(a, row, rank, 0u, 0u, r);
+            if (room.found > LS_CAP)
+                narrow(room, a.top, [&](auto f) {
+                    for (int c = t; c < n; c += LS_THREADS) f(kept[c]);
+                });
+            rank_list(room, a.top, [&](int rank, lp_entry e) { put_top(a, row, rank, e, r); });
         }
         __syncthreads();
     }
@@ -323,7 +332,7 @@ static bool bad4(const void *p) { return ((uintptr_t)p & 3) != 0; }
 extern "C" size_t pp_logprob_workspace_bytes(int type, int64_t rows, int64_t cols, int top) {
     if (pp_bad_sizes(type, rows, cols) || top < 0 || top > PP_TOP_MAX) return 0;
     const size_t most = (size_t)ls_most(type, rows, cols);
-    return pp_align256(most * sizeof(pp_f4)) + pp_align256(most * top * sizeof(pp_u2)) + 256;
+    return pp_align256(most * sizeof(pp_f4)) + pp_align256(most * top * sizeof(unsigned long long)) + 256;
 }
 
 extern "C" int pp_logprob_forward(int type, int64_t rows, int64_t cols, const void *logits, int64_t ld, float temperature, const int32_t *tokens,
@@ -337,7 +346,7 @@ extern "C" int pp_logprob_forward(int type, int64_t rows, int64_t cols, const vo
     if (p.segs > 1)
         if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < pp_logprob_workspace_bytes(type, rows, cols, top)) return PP_ERR_WORKSPACE;
     pp_f4 *sums = (pp_f4 *)workspace;
-    pp_u2 *kept = (pp_u2 *)((char *)workspace + pp_align256((size_t)rows * p.segs * sizeof(pp_f4)));
+    unsigned long long *kept = (unsigned long long *)((char *)workspace + pp_align256((size_t)rows * p.segs * sizeof(pp_f4)));
     const lp_args a = {rows, cols, p.size, ld, p.segs, top, (float)(1.4426950408889634 / temperature), 1.0f / temperature, tokens, logp, entropy, norm, top_logp, top_index, sums, kept};
     hipStream_t st = (hipStream_t)stream;
     return pp_by_type(type, [&](auto tag) {

@@ -56,6 +56,31 @@ template <class Y> __device__ __forceinline__ PpRaw<Y> ls_load(const typename Y:
     return r;
 }
 
+// A thread's chunks of a segment x[0 .. n); whole segments without a branch, so that all loads are on their way together
+template <class Y, int HELD> __device__ __forceinline__ void ls_load_all(PpRaw<Y> (&raw)[HELD], const typename Y::T *x, long long n) {
+    if (n >= (long long)HELD * LS_STEP) {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i)
+#pragma unroll
+            for (int j = 0; j < PpRaw<Y>::W; ++j)
+                raw[i].w[j] = ((const pp_any16<sizeof(typename Y::T)> *)(x + 8 * (threadIdx.x + i * LS_THREADS)))[j].v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) {
+            const long long c = 8ll * (threadIdx.x + i * LS_THREADS);
+            raw[i] = ls_load<Y>(x + c, n - c);
+        }
+    }
+}
+
+// Makes the compiler convert held values again where they are used again: kept as floats they would take twice the registers.
+template <class Y, int N> __device__ __forceinline__ void ls_hold(PpRaw<Y> (&raw)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int j = 0; j < PpRaw<Y>::W; ++j) asm volatile("" : "+v"(raw[i].w[j]));
+}
+
 __device__ __forceinline__ float ls_max8(const float *v) {
     float m = __builtin_fmaxf(__builtin_fmaxf(v[0], v[1]), v[2]);
     m = __builtin_fmaxf(__builtin_fmaxf(m, v[3]), v[4]);

@@ -10,7 +10,7 @@
 
 #define NM_MAX_GRID (1 << 20)
 #define NM_CHUNKS 8          // most chunks of eight columns that a thread holds
-#define NM_PARTS 1024        // most workgroups of a backward pass, each with its own part of dg
+#define NM_PART_WAVES 4096   // most waves of a backward pass (16 to a unit); each workgroup has its own part of dg
 #define NM_WIDE (1024 * 4)   // most chunks of a row in the backward pass that holds it
 
 // A row's values: a matrix of type Y, or what PP_PACK_INT8 left of one.
@@ -53,9 +53,8 @@ template <class Y> __device__ __forceinline__ void load_sum(nm_matrix<Y> x, nm_m
 
 template <class Y>
 __device__ __forceinline__ void put_forward(const nm_forward &f, typename Y::T *total, long long ld_total, typename Y::T *y, long long ld_y,
-                                            long long row, long long q, long long chunks, long long left, float inv, const float *s) {
-    float g[8], v[8];
-    load_gain(f.gain, 8 * q, left, g);
+                                            long long row, long long q, long long chunks, long long left, float inv, const float *s, const float *g) {
+    float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = left > j ? s[j] * inv * g[j] : 0.0f;
     if (total && left > 0) pp_store8<Y>(total + row * ld_total + 8 * q, left, s);
@@ -75,12 +74,17 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * PP_WAVE) void k_norm_for
     const long long per = WAVES == 1 ? 256 / PP_WAVE : 1;
     int turn = 0;
     for (long long row = blockIdx.x * per + (WAVES == 1 ? threadIdx.x / PP_WAVE : 0); row < f.rows; row += gridDim.x * per) {
-        float s[CH ? CH : 1][8], sum = 0.0f;
+        float s[CH ? CH : 1][8], g[CH ? CH : 1][8], sum = 0.0f;
         if constexpr (CH > 0) {
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 const long long q = t + i * WAVES * PP_WAVE;
                 load_sum<Y>(x, res, row, q, f.cols - 8 * q, s[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const long long q = t + i * WAVES * PP_WAVE;
+                load_gain(f.gain, 8 * q, f.cols - 8 * q, g[i]);
             }
 #pragma unroll
             for (int i = 0; i < CH; ++i)
@@ -103,18 +107,18 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : WAVES * PP_WAVE) void k_norm_for
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 const long long q = t + i * WAVES * PP_WAVE;
-                if (q < chunks) put_forward<Y>(f, total, ld_total, y, ld_y, row, q, chunks, f.cols - 8 * q, inv, s[i]);
+                if (q < chunks) put_forward<Y>(f, total, ld_total, y, ld_y, row, q, chunks, f.cols - 8 * q, inv, s[i], g[i]);
             }
         } else {
             for (long long q = t; q < chunks; q += WAVES * PP_WAVE) {
                 load_sum<Y>(x, res, row, q, f.cols - 8 * q, s[0]);
-                put_forward<Y>(f, total, ld_total, y, ld_y, row, q, chunks, f.cols - 8 * q, inv, s[0]);
+                load_gain(f.gain, 8 * q, f.cols - 8 * q, g[0]);
+                put_forward<Y>(f, total, ld_total, y, ld_y, row, q, chunks, f.cols - 8 * q, inv, s[0], g[0]);
             }
         }
     }
 }
 
-// Chunks of a row, and whether its matrices are ...
 static int64_t nm_chunks(int64_t cols) { return pp_groups(cols) * (PP_GROUP / 8); }
 
 template <class Y, int WAVES, int CH>
@@ -154,9 +158,11 @@ extern "C" int pp_norm_forward(int type, int64_t rows, int64_t cols, const void 
         else if (chunks <= 256 && rows >= 1024) go(I(1), I(4));
         else if (chunks <= 256) go(I(4), I(1));
         else if (chunks <= 512) go(I(4), I(2));
+        else if (chunks <= 768) go(I(4), I(3));
         else if (chunks <= 1024) go(I(4), I(4));
+        else if (chunks <= 1536) go(I(4), I(6));
         else if (chunks <= 2048) go(I(4), I(8));
-        else if (chunks <= 8192) go(I(16), I(8));
+        else if (chunks <= 4096) go(I(16), I(4));
         else go(I(16), I(0));
         return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
     });
@@ -171,47 +177,75 @@ struct nm_backward {
     nm_packed s8; // the kept sum; codes NULL: a matrix
 };
 
-template <class Y, int WAVES, int CH>
+// A chunk of a row as it was loaded
+template <class Y, bool PACKED> struct nm_chunk {
+    PpRaw<Y> dy, more, s[PACKED ? 0 : 1];
+    pp_u2 codes;
+    unsigned char scale;
+};
+template <class Y, bool PACKED>
+__device__ __forceinline__ nm_chunk<Y, PACKED> load_chunk(const nm_backward &b, nm_matrix<Y> dy, nm_matrix<Y> s, nm_matrix<Y> dtotal, long long row, long long q,
+                                                          long long chunks) {
+    nm_chunk<Y, PACKED> c = {};
+    const long long left = b.cols - 8 * q;
+    c.dy = pp_load8<Y>(dy.p + row * dy.ld + 8 * q, left);
+    if constexpr (!PACKED) c.s[0] = pp_load8<Y>(s.p + row * s.ld + 8 * q, left);
+    else if (left > 0) {
+        c.codes = *(const pp_u2 *)(b.s8.codes + (row * chunks + q) * 8);
+        c.scale = b.s8.scales[(row * chunks + q) >> 2];
+    }
+    if (dtotal.p) c.more = pp_load8<Y>(dtotal.p + row * dtotal.ld + 8 * q, left);
+    return c;
+}
+
+// With one chunk to a thread the next row is on its way while a row's sum is made (with more the registers for it cost more than
+// it gives).  dx may be dy or dtotal: their values of a row have been read before it is written.
+template <class Y, int WAVES, int CH, bool PACKED>
 __global__ __launch_bounds__(WAVES *PP_WAVE) void k_norm_backward(nm_backward b, nm_matrix<Y> dy, nm_matrix<Y> s, nm_matrix<Y> dtotal, typename Y::T *dx,
                                                                    long long ld_dx) {
     __shared__ float room[2][WAVES];
     const int t = threadIdx.x;
     const long long chunks = (b.cols + PP_GROUP - 1) / PP_GROUP * (PP_GROUP / 8);
-    float dg[CH][8] = {};
+    float dg[CH][8] = {}, g[CH][8];
+    nm_chunk<Y, PACKED> c[CH];
     int turn = 0;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        const long long q = t + i * WAVES * PP_WAVE;
+        if constexpr (CH == 1) c[i] = load_chunk<Y, PACKED>(b, dy, s, dtotal, blockIdx.x, q, chunks);
+        load_gain(b.gain, 8 * q, b.cols - 8 * q, g[i]);
+    }
     for (long long row = blockIdx.x; row < b.rows; row += gridDim.x) {
         const float inv = b.inv[row];
         float d[CH][8], z[CH][8], dot = 0.0f;
+        if constexpr (CH > 1)
+#pragma unroll
+            for (int i = 0; i < CH; ++i) c[i] = load_chunk<Y, PACKED>(b, dy, s, dtotal, row, t + i * WAVES * PP_WAVE, chunks);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const long long q = t + i * WAVES * PP_WAVE, left = b.cols - 8 * q;
-            pp_values<Y>(pp_load8<Y>(dy.p + row * dy.ld + 8 * q, left), d[i]);
-            if (!b.s8.codes) pp_values<Y>(pp_load8<Y>(s.p + row * s.ld + 8 * q, left), z[i]);
-            else if (q < chunks) pp_get_codes8(row * chunks + q, b.s8.codes, b.s8.scales, z[i]);
-            else
-#pragma unroll
-                for (int j = 0; j < 8; ++j) z[i][j] = 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            const long long q = t + i * WAVES * PP_WAVE, left = b.cols - 8 * q;
-            float g[8];
-            load_gain(b.gain, 8 * q, left, g);
+            const long long left = b.cols - 8ll * (t + i * WAVES * PP_WAVE);
+            pp_values<Y>(c[i].dy, d[i]);
+            if constexpr (PACKED) pp_values8(c[i].codes, pp_unit8(c[i].scale), z[i]);
+            else pp_values<Y>(c[i].s[0], z[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 z[i][j] = left > j ? z[i][j] * inv : 0.0f;
                 dg[i][j] = __builtin_fmaf(d[i][j], z[i][j], dg[i][j]);
-                d[i][j] *= g[j];
+                d[i][j] *= g[i][j];
                 dot = __builtin_fmaf(d[i][j], z[i][j], dot);
             }
         }
+        PpRaw<Y> extra[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) extra[i] = c[i].more;
+        if (CH == 1 && row + gridDim.x < b.rows) c[0] = load_chunk<Y, PACKED>(b, dy, s, dtotal, row + gridDim.x, t, chunks);
         const float mean = pp_group_sum<WAVES>(dot, room[turn]) / (float)b.cols;
         turn ^= 1;
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             const long long q = t + i * WAVES * PP_WAVE, left = b.cols - 8 * q;
-            float more[8] = {};
-            if (dtotal.p) pp_values<Y>(pp_load8<Y>(dtotal.p + row * dtotal.ld + 8 * q, left), more);
+            float more[8];
+            pp_values<Y>(extra[i], more);
 #pragma unroll
             for (int j = 0; j < 8; ++j) d[i][j] = __builtin_fmaf(inv, __builtin_fmaf(-z[i][j], mean, d[i][j]), more[j]);
             if (left > 0) pp_store8<Y>(dx + row * ld_dx + 8 * q, left, d[i]);
@@ -276,25 +310,37 @@ __global__ __launch_bounds__(256) void k_norm_wide(nm_backward b, const float *m
     if (b.part) pp_store8<PpF32>(b.part + blockIdx.y * b.cols + 8 * q, left, dg);
 }
 
-// dg = dg_in + the parts, a thread to a column, eight threads to the parts
+// dg = dg_in + the parts: a workgroup to 32 columns, eight threads to four columns each by 32 groups of parts
 __global__ __launch_bounds__(256) void k_norm_gain(long long cols, int parts, const float *__restrict__ part, const float *dg_in, float *dg) {
-    __shared__ float room[8][32];
-    const int t = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const long long c = blockIdx.x * 32ll + t;
-    float sum = 0.0f;
-    if (c < cols)
-        for (int p = w; p < parts; p += 8) sum += part[p * cols + c];
-    room[w][t] = sum;
-    __syncthreads();
-    if (w || c >= cols) return;
+    __shared__ float room[32][33];
+    const int t = threadIdx.x & 7, w = threadIdx.x >> 3;
+    const long long c = blockIdx.x * 32ll + 4 * t;
+    float sum[4] = {};
+    if (c + 4 <= cols) {
+#pragma unroll 8
+        for (int p = w; p < parts; p += 32) {
+            const pp_u4 v = ((const pp_any16<4> *)(part + p * cols + c))->v;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) sum += room[k][t];
-    dg[c] = dg_in ? dg_in[c] + sum : sum;
+            for (int k = 0; k < 4; ++k) sum[k] += pp_bits(v[k]);
+        }
+    } else
+        for (int k = 0; c + k < cols; ++k)
+            for (int p = w; p < parts; p += 32) sum[k] += part[p * cols + c + k];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) room[w][4 * t + k] = sum[k];
+    __syncthreads();
+    const long long col = blockIdx.x * 32ll + threadIdx.x;
+    if (threadIdx.x >= 32 || col >= cols) return;
+    float all = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) all += room[k][threadIdx.x];
+    dg[col] = dg_in ? dg_in[col] + all : all;
 }
 
-// Workgroups that have parts of dg
+// Waves to a row of the backward pass that holds it, and workgroups that have parts of dg
+static int nm_waves(int64_t chunks) { return chunks <= 64 ? 1 : chunks <= 256 ? 4 : chunks <= 512 ? 8 : 16; }
 static int64_t nm_parts(int64_t rows, int64_t cols) {
-    const int64_t most = nm_chunks(cols) > NM_WIDE ? 16 : NM_PARTS;
+    const int64_t chunks = nm_chunks(cols), most = chunks > NM_WIDE ? 16 : NM_PART_WAVES / nm_waves(chunks);
     return rows < most ? rows : most;
 }
 
@@ -326,8 +372,9 @@ extern "C" int pp_norm_backward(int type, int64_t rows, int64_t cols, const void
             const nm_backward b = {rows, cols, inv, gain, dgain ? part : NULL, {(uint8_t *)total_codes, (uint8_t *)total_scales}};
             const nm_matrix<Y> md = {(const T *)dy, ld_dy}, ms = {(const T *)total, ld_total}, mt = {(const T *)dtotal, ld_dtotal};
             auto go = [&](auto waves, auto ch) {
-                k_norm_backward<Y, decltype(waves)::value, decltype(ch)::value>
-                    <<<(unsigned)parts, decltype(waves)::value * PP_WAVE, 0, st>>>(b, md, ms, mt, (T *)dx, ld_dx);
+                constexpr int W = decltype(waves)::value, C = decltype(ch)::value;
+                if (total_codes) k_norm_backward<Y, W, C, true><<<(unsigned)parts, W * PP_WAVE, 0, st>>>(b, md, ms, mt, (T *)dx, ld_dx);
+                else k_norm_backward<Y, W, C, false><<<(unsigned)parts, W * PP_WAVE, 0, st>>>(b, md, ms, mt, (T *)dx, ld_dx);
             };
             if (wide) {
                 k_norm_dot<Y><<<(unsigned)(rows < NM_MAX_GRID ? rows : NM_MAX_GRID), 1024, 0, st>>>(b, md, ms, means);
@@ -335,8 +382,8 @@ extern "C" int pp_norm_backward(int type, int64_t rows, int64_t cols, const void
                 k_norm_wide<Y><<<dim3((unsigned)((chunks + 255) / 256), (unsigned)parts), 256, 0, st>>>(b, means, md, ms, mt, (T *)dx, ld_dx);
             } else if (chunks <= 64) go(I(1), I(1));
             else if (chunks <= 256) go(I(4), I(1));
-            else if (chunks <= 512) go(I(4), I(2));
-            else if (chunks <= 1024) go(I(4), I(4));
+            else if (chunks <= 512) go(I(8), I(1));
+            else if (chunks <= 1024) go(I(16), I(1));
             else if (chunks <= 2048) go(I(16), I(2));
             else go(I(16), I(4));
             return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
