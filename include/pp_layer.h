@@ -172,7 +172,7 @@ int pp_norm_backward(int type, int64_t rows, int64_t cols, const void *dy, int64
  *   h0      float [seqs][cols], or NULL = zero
  *   h_last  float [seqs][cols] out: h behind the last token (h0 for an empty sequence), or NULL = not wanted
  *   kept    float [pp_scan_kept_rows][cols] out: states for pp_scan_backward, or NULL = not wanted
- * States are held in 32 bits, and what 32 tokens do to one is added up by itself, so one that is kept for many tokens does not drift.
+ * States are held in 32 bits, and what 16 tokens do to one is added up by itself, so one that is kept for many tokens does not drift.
  * rows and cols: ceil(rows / 128) ceil(cols / 64) <= 2^24.
  * The workspaces (256-byte aligned) need not be kept; what so many rows need serves fewer.  pp_scan_kept_rows (host function;
  * -1 if a size or the type is out of range): both calls need the same type, rows and cols.

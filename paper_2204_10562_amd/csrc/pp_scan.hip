@@ -1,8 +1,8 @@
 // pp_scan_forward, pp_scan_backward, pp_scan_step: the gated linear recurrence h_t = a_t h_(t-1) + (1 - a_t) v_t, a = sigmoid(gate).
 #include "pp_rows.h"
 
-#define SC_CHUNK 32               // tokens that a wave holds, and between kept states
-#define SC_WAVES 4                // of a workgroup, one behind the other in time
+#define SC_CHUNK 16               // tokens that a wave holds, and between kept states
+#define SC_WAVES 8                // of a workgroup, one behind the other in time
 #define SC_TILE (SC_CHUNK * SC_WAVES)
 #define SC_GROUP 16               // tiles between states that are passed on whole
 #define SC_MAX_TILES (1 << 24)    // of a launch
@@ -57,8 +57,8 @@ struct sc_args {
     long long width;
 };
 
-// What a wave's tokens t0 .. t0 + 31 have to do with sequences, a bit each: whether a sequence has them, starts with them, ends with
-// them; and the sequence of the first of them.
+// What a wave's tokens t0 .. t0 + SC_CHUNK - 1 have to do with sequences, a bit each: whether a sequence has them, starts with them,
+// ends with them; and the last sequence that starts before them (-1: none).
 struct sc_marks {
     unsigned in, first, last;
     int seq;
@@ -71,15 +71,15 @@ __device__ __forceinline__ unsigned sc_from(long long t) { return t <= 0 ? ~0u :
 
 __device__ __forceinline__ sc_marks sc_mark(const int *__restrict__ starts, long long rows, int seqs, long long t0) {
     sc_marks m;
+    const unsigned all = ~sc_from(SC_CHUNK);
+    const long long begin = starts ? sc_start(starts, rows, 0) : 0, end = starts ? sc_start(starts, rows, seqs) : rows;
+    m.in = sc_from(begin - t0) & ~sc_from(end - t0) & all;
+    m.last = end - t0 > 0 && end - t0 <= SC_CHUNK ? 1u << (end - t0 - 1) : 0u;
     if (!starts) {
-        m.in = ~sc_from(rows - t0);
         m.first = t0 == 0;
-        m.last = rows - 1 - t0 >= 0 && rows - 1 - t0 < 32 ? 1u << (rows - 1 - t0) : 0u;
         m.seq = 0;
         return m;
     }
-    const long long begin = sc_start(starts, rows, 0), end = sc_start(starts, rows, seqs);
-    m.in = sc_from(begin - t0) & ~sc_from(end - t0);
     int lo = 0, hi = seqs;  // the first n with starts[n] >= t0, seqs if none before
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
@@ -88,17 +88,13 @@ __device__ __forceinline__ sc_marks sc_mark(const int *__restrict__ starts, long
     }
     m.seq = lo - 1;
     m.first = 0;
-    unsigned next = 0;
-    for (int n = lo; n <= seqs; ++n) {
+    for (int n = lo; n < seqs; ++n) {
         const long long t = sc_start(starts, rows, n) - t0;
-        if (t == 32) next = 1;
-        if (t < 0 || t >= 32) break;
-        if (n < seqs) m.first |= 1u << t;
+        if (t < 0 || t > SC_CHUNK) break;
+        m.first |= 1u << t;  // (bit SC_CHUNK: the next wave's first token)
     }
-    m.last = m.first >> 1 | next << 31;
-    if (end - t0 > 0 && end - t0 <= 32) m.last |= 1u << (end - t0 - 1);
+    m.last = (m.last | m.first >> 1) & m.in;
     m.first &= m.in;
-    m.last &= m.in;
     return m;
 }
 // the sequence that starts with token t, where `n` is that of a token before (or -1)
@@ -119,14 +115,14 @@ __device__ __forceinline__ int sc_previous(const int *__restrict__ starts, int n
 // W channels of a token, W of a 4-byte word's 16-bit values or one value
 template <class Y, int W> struct sc_lane {
     typedef typename Y::T T;
-    long long c;   // first channel
+    unsigned c;    // first channel
     int n;         // channels that there are
-    long long at;  // where a whole word is read from
+    unsigned at;   // where a whole word is read from
     unsigned shift;
     bool full;     // all lanes have W
-    __device__ __forceinline__ sc_lane(long long tile, long long cols) {
+    __device__ __forceinline__ sc_lane(unsigned tile, unsigned cols) {
         c = (tile * PP_WAVE + (threadIdx.x & (PP_WAVE - 1))) * W;
-        n = cols - c >= W ? W : cols > c ? (int)(cols - c) : 0;
+        n = c + W <= cols ? W : cols > c ? (int)(cols - c) : 0;
         at = c + W <= cols ? c : cols - W;
         shift = n == 1 && W == 2 ? 16 : 0;
         full = (tile + 1) * PP_WAVE * W <= cols;
@@ -289,7 +285,7 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_forward(sc_args a, c
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PP_WAVE), lane = threadIdx.x & (PP_WAVE - 1);
     const int order = ticket / a.lanes_tiles, lanes_tile = ticket % a.lanes_tiles;
     const long long t0 = (long long)order * SC_TILE + wave * SC_CHUNK;
-    const sc_lane<Y, W> lanes(lanes_tile, a.cols);
+    const sc_lane<Y, W> lanes(lanes_tile, (unsigned)a.cols);
     unsigned f[SC_CHUNK], x[SC_CHUNK];
 #pragma unroll
     for (int i = 0; i < SC_CHUNK; ++i) {
@@ -369,7 +365,7 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_backward(sc_args a, 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PP_WAVE), lane = threadIdx.x & (PP_WAVE - 1);
     const int order = ticket / a.lanes_tiles, lanes_tile = ticket % a.lanes_tiles;
     const long long t0 = (long long)(a.tiles - 1 - order) * SC_TILE + (SC_WAVES - 1 - wave) * SC_CHUNK;
-    const sc_lane<Y, W> lanes(lanes_tile, a.cols);
+    const sc_lane<Y, W> lanes(lanes_tile, (unsigned)a.cols);
     unsigned f[SC_CHUNK], x[SC_CHUNK], d[SC_CHUNK];
 #pragma unroll
     for (int i = 0; i < SC_CHUNK; ++i) {

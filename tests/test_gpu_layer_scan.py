@@ -156,9 +156,11 @@ def test_gates_at_their_ends():
 
 def test_a_state_that_is_kept_does_not_drift():
     """With one gate of 9 throughout (1 - a = 1.2e-4) and one value, the state comes to the value.  A sum of products that were rounded one by one
-    would be off by u M / (1 - a) = 4.9e-4 M.  What 32 tokens do is h + (H - D h) with D = 1 - a^32 = 3.9e-3: a rounding of M, and H and D, which
-    come from one recurrence of 64 roundings each, are 66 u D M off together.  err = (1 - D) err + u M (1 + 66 D) stays below u M (254 + 66), and
-    within the 32 tokens 64 u M more: 2.3e-5 M.  1 - a, right to 26 u of itself, changes the way there by 26 u n (1 - a) a^n < 1e-6 M."""
+    would be off by u M / (1 - a) = 4.9e-4 M.  Here a state is passed on whole every 2048 tokens, by at most 16 stretches with a rounding of M each;
+    a stretch is h + (H - D h), where H and D come from one recurrence of 33 roundings and at most 16 joinings of 3, so they are 81 u D M off
+    together, and 2048 tokens have D = 0.25 in all: 36 u M every 2048 tokens, of which 0.78 is left after as many more, so 162 u M and below.
+    On the way to a token come those 36 u M once more and 2 u M for each of 16 tokens: 230 u M = 1.4e-5 M.  1 - a, right to 26 u of itself,
+    changes the way to the value by 26 u n (1 - a) a^n < 1e-6 M."""
     import torch
     from paper_2204_10562_amd import layer as pp
     rows, cols = 60000, 64
