@@ -112,27 +112,44 @@ __device__ __forceinline__ int sc_previous(const int *__restrict__ starts, int n
     return n < 0 ? 0 : n;
 }
 
-// W channels of a token, W of a 4-byte word's 16-bit values or one value
+// W channels of a token to a lane: two 16-bit values of a word, or one value.  A row's address is the same for all lanes, a lane's
+// offset 32 bits.
 template <class Y, int W> struct sc_lane {
     typedef typename Y::T T;
     unsigned c;    // first channel
     int n;         // channels that there are
-    unsigned at;   // where a whole word is read from
+    unsigned at;   // byte from which on a whole word is read
     unsigned shift;
     bool full;     // all lanes have W
     __device__ __forceinline__ sc_lane(unsigned tile, unsigned cols) {
         c = (tile * PP_WAVE + (threadIdx.x & (PP_WAVE - 1))) * W;
         n = c + W <= cols ? W : cols > c ? (int)(cols - c) : 0;
-        at = c + W <= cols ? c : cols - W;
+        at = (c + W <= cols ? c : cols - W) * (unsigned)sizeof(T);
         shift = n == 1 && W == 2 ? 16 : 0;
         full = (tile + 1) * PP_WAVE * W <= cols;
     }
     __device__ __forceinline__ unsigned load(const T *row) const {
+        const char *p = (const char *)row + at;
         if constexpr (sizeof(T) * W == 4) {
             unsigned u;
-            __builtin_memcpy(&u, row + at, 4);
+            __builtin_memcpy(&u, p, 4);
             return u;
-        } else return __builtin_bit_cast(unsigned short, row[at]);
+        } else return *(const unsigned short *)p;
+    }
+    // the tokens t0 .. t0 + SC_CHUNK - 1; the last row in the place of those behind it
+    __device__ __forceinline__ void load_all(unsigned (&raw)[SC_CHUNK], const T *m, long long ld, long long t0, long long rows) const {
+        const T *row = m + (t0 < rows ? t0 : rows - 1) * ld;
+        if (rows - t0 >= SC_CHUNK) {
+#pragma unroll
+            for (int i = 0; i < SC_CHUNK; ++i) raw[i] = load(row + i * ld);
+        } else {
+            const int more = rows > t0 ? (int)(rows - 1 - t0) : 0;
+#pragma unroll
+            for (int i = 0; i < SC_CHUNK; ++i) raw[i] = load(row + (i < more ? i : more) * ld);
+        }
+        if (!full)
+#pragma unroll
+            for (int i = 0; i < SC_CHUNK; ++i) raw[i] >>= shift;
     }
     __device__ __forceinline__ static float get(unsigned raw, int w) {
         if constexpr (sizeof(T) == 4) return pp_bits(raw);
@@ -142,7 +159,7 @@ template <class Y, int W> struct sc_lane {
         T t[W];
 #pragma unroll
         for (int w = 0; w < W; ++w) t[w] = Y::put(v[w]);
-        if (full) __builtin_memcpy(row + c, t, sizeof(t));
+        if (full) __builtin_memcpy((char *)row + at, t, sizeof(t));
         else
 #pragma unroll
             for (int w = 0; w < W; ++w)
@@ -162,7 +179,7 @@ template <class Y, int W> struct sc_lane {
 template <int W> struct sc_room {
     float x[SC_WAVES][W * PP_WAVE], H[SC_WAVES][W * PP_WAVE];
     float bx[SC_WAVES][W * PP_WAVE], bH[SC_WAVES][W * PP_WAVE];
-    float whole[W * PP_WAVE];
+    float mine_x[W * PP_WAVE], mine_H[W * PP_WAVE], whole[W * PP_WAVE];
     unsigned ticket;
 };
 
@@ -190,6 +207,8 @@ __device__ __forceinline__ void sc_carry(const sc_args &a, sc_room<W> &room, int
 #pragma unroll
                 for (int k = 1; k < SC_WAVES; ++k) sc_join(x, H, room.x[k][l], room.H[k][l]);
                 sc_tell(a.stretch + order * a.width + col + w, sc_word(x, H));
+                room.mine_x[l] = x;
+                room.mine_H[l] = H;
             }
         }
         const int begin = wave * (SC_GROUP / SC_WAVES);
@@ -219,7 +238,22 @@ __device__ __forceinline__ void sc_carry(const sc_args &a, sc_room<W> &room, int
                 room.bH[wave][lane * W + w] = H;
             }
         }
+        __syncthreads();
         if (wave == SC_WAVES - 1) {
+            // the last tile of a group knows what the group makes of a state before it knows the state
+            const bool last = place == SC_GROUP - 1 && order + 1 < a.tiles;
+            float x[W], H[W];
+            if (last)
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const int l = lane * W + w;
+                    x[w] = room.bx[0][l];
+                    H[w] = room.bH[0][l];
+#pragma unroll
+                    for (int k = 1; k < SC_WAVES; ++k)
+                        if (k * (SC_GROUP / SC_WAVES) < place) sc_join(x[w], H[w], room.bx[k][l], room.bH[k][l]);
+                    sc_join(x[w], H[w], room.mine_x[l], room.mine_H[l]);
+                }
             unsigned long long word[W];
             bool wait = group > 0;
 #pragma unroll
@@ -232,10 +266,14 @@ __device__ __forceinline__ void sc_carry(const sc_args &a, sc_room<W> &room, int
                     wait = wait || (unsigned)word[w] == (unsigned)SC_EMPTY;
                 }
                 wait = __any(wait);
-                if (wait) __builtin_amdgcn_s_sleep(8);
+                if (wait) __builtin_amdgcn_s_sleep(2);
             }
 #pragma unroll
-            for (int w = 0; w < W; ++w) room.whole[lane * W + w] = pp_bits((unsigned)(word[w] >> 32));
+            for (int w = 0; w < W; ++w) {
+                const float whole = pp_bits((unsigned)(word[w] >> 32));
+                if (last) sc_tell(a.whole + (group + 1) * a.width + col + w, sc_word(0.0f, sc_after(x[w], H[w], whole)));
+                room.whole[lane * W + w] = whole;
+            }
         }
         __syncthreads();
 #pragma unroll
@@ -253,13 +291,10 @@ __device__ __forceinline__ void sc_carry(const sc_args &a, sc_room<W> &room, int
 #pragma unroll
         for (int w = 0; w < W; ++w) h[w] = sc_after(room.x[k][lane * W + w], room.H[k][lane * W + w], h[w]);
     }
-    if (a.tiles > 1 && wave == SC_WAVES - 1 && place == SC_GROUP - 1 && order + 1 < a.tiles)
-#pragma unroll
-        for (int w = 0; w < W; ++w)
-            sc_tell(a.whole + (group + 1) * a.width + col + w, sc_word(0.0f, sc_after(room.x[wave][lane * W + w], room.H[wave][lane * W + w], h[w])));
 }
 
-// Number of the workgroup's tile: tickets, so that a tile's predecessors run before it
+// The workgroup's tile, by a ticket: a tile's predecessors are under way before it.  (Taking the next ticket while a tile is worked on
+// saves its way to memory, and makes the tiles that wait for the one behind it wait for both: 298 us for 242, 65536 x 2048 forward.)
 template <int W> __device__ __forceinline__ unsigned sc_ticket(const sc_args &a, sc_room<W> &room) {
     if (a.tiles == 1) return blockIdx.x;
     if (!threadIdx.x) room.ticket = atomicAdd(a.ticket, 1u);
@@ -267,7 +302,14 @@ template <int W> __device__ __forceinline__ unsigned sc_ticket(const sc_args &a,
     return __builtin_amdgcn_readfirstlane(room.ticket);
 }
 
-// a and 1 - a of a token from s, the smaller one, negative where that is a
+// a and 1 - a of a gate, both right to a few units of themselves
+__device__ __forceinline__ void sc_open(float gate, float &a, float &u) {
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(gate)), large = __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
+    const bool keeps = gate >= 0.0f;
+    a = keeps ? large : small;
+    u = keeps ? small : large;
+}
+// the same from s, the smaller one, negative where that is a
 __device__ __forceinline__ void sc_sides(float s, float &a, float &u) {
     const float m = __builtin_fabsf(s), r = 1.0f - m;
     const bool keeps = !(pp_bits(s) >> 31);
@@ -275,30 +317,25 @@ __device__ __forceinline__ void sc_sides(float s, float &a, float &u) {
     u = keeps ? m : r;
 }
 
+// Tokens in the midst of a sequence take the short way: PLAIN says that no sequence begins or ends among a wave's tokens.
 template <class Y, int W>
-__global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_forward(sc_args a, const typename Y::T *__restrict__ gate, long long ld_gate,
+__global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_forward(sc_args a, const typename Y::T *__restrict__ gate, long long ld_gate,
                                                                        const typename Y::T *__restrict__ v, long long ld_v, const float *__restrict__ h0,
                                                                        typename Y::T *__restrict__ h, long long ld_h, float *__restrict__ h_last,
                                                                        float *__restrict__ kept) {
     __shared__ sc_room<W> room;
     const unsigned ticket = sc_ticket(a, room);
+    const int order = ticket / (unsigned)a.lanes_tiles, lanes_tile = ticket % (unsigned)a.lanes_tiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PP_WAVE), lane = threadIdx.x & (PP_WAVE - 1);
-    const int order = ticket / a.lanes_tiles, lanes_tile = ticket % a.lanes_tiles;
     const long long t0 = (long long)order * SC_TILE + wave * SC_CHUNK;
     const sc_lane<Y, W> lanes(lanes_tile, (unsigned)a.cols);
     unsigned f[SC_CHUNK], x[SC_CHUNK];
-#pragma unroll
-    for (int i = 0; i < SC_CHUNK; ++i) {
-        const long long t = t0 + i < a.rows ? t0 + i : a.rows - 1;
-        f[i] = lanes.load(gate + t * ld_gate);
-        x[i] = lanes.load(v + t * ld_v);
-    }
+    lanes.load_all(f, gate, ld_gate, t0, a.rows);
+    lanes.load_all(x, v, ld_v, t0, a.rows);
     const sc_marks m = sc_mark(a.starts, a.rows, (int)a.seqs, t0);
-    if (!lanes.full)
-#pragma unroll
-        for (int i = 0; i < SC_CHUNK; ++i) f[i] >>= lanes.shift, x[i] >>= lanes.shift;
-    float s[SC_CHUNK][W], H[W], A[W], D[W], from[W];
-    // the wave's own stretch; of the sequences that start in it the last one counts
+    const bool plain = m.in == ~sc_from(SC_CHUNK) && !m.first && !m.last;
+    // a and (1 - a) v of the wave's tokens, and its own stretch; of the sequences that start in it the last one counts
+    float keep[SC_CHUNK][W], bring[SC_CHUNK][W], H[W], A[W], D[W], from[W];
     const int cut = m.first ? 31 - __builtin_clz(m.first) : -1;
     if (cut >= 0) {
         int n = m.seq;
@@ -307,24 +344,28 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_forward(sc_args a, c
     }
 #pragma unroll
     for (int w = 0; w < W; ++w) H[w] = 0.0f, A[w] = 1.0f, D[w] = 0.0f;
+    auto stretch = [&](auto is_plain) {
 #pragma unroll
-    for (int i = 0; i < SC_CHUNK; ++i) {
-        if (!(m.in >> i & 1)) continue;
-        if (i == cut)
+        for (int i = 0; i < SC_CHUNK; ++i) {
+            if constexpr (!decltype(is_plain)::value) {
+                if (!(m.in >> i & 1)) continue;
+                if (i == cut)
 #pragma unroll
-            for (int w = 0; w < W; ++w) H[w] = from[w];
+                    for (int w = 0; w < W; ++w) H[w] = from[w];
+            }
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const float g = lanes.get(f[i], w), e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e);
-            const float small = e * r;
-            const bool keeps = g >= 0.0f;
-            s[i][w] = keeps ? small : -small;
-            const float ka = keeps ? r : small, ku = keeps ? small : r;
-            H[w] = __builtin_fmaf(ka, H[w], ku * lanes.get(x[i], w));
-            D[w] = __builtin_fmaf(ka, D[w], ku);
-            A[w] *= ka;
+            for (int w = 0; w < W; ++w) {
+                float u;
+                sc_open(lanes.get(f[i], w), keep[i][w], u);
+                bring[i][w] = u * lanes.get(x[i], w);
+                H[w] = __builtin_fmaf(keep[i][w], H[w], bring[i][w]);
+                D[w] = __builtin_fmaf(keep[i][w], D[w], u);
+                A[w] *= keep[i][w];
+            }
         }
-    }
+    };
+    if (plain) stretch(std::true_type());
+    else stretch(std::false_type());
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         room.x[wave][lane * W + w] = cut >= 0 ? SC_CUT : sc_share(A[w], D[w]);
@@ -333,6 +374,17 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_forward(sc_args a, c
     __syncthreads();
     sc_carry<W>(a, room, order, lanes_tile, wave, H);
     if (kept && t0 < a.rows) lanes.put_floats(kept + t0 / SC_CHUNK * a.cols, H);
+    typename Y::T *row = h + t0 * ld_h;
+    if (plain) {
+#pragma unroll
+        for (int i = 0; i < SC_CHUNK; ++i) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) H[w] = __builtin_fmaf(keep[i][w], H[w], bring[i][w]);
+            lanes.store(row, H);
+            row += ld_h;
+        }
+        return;
+    }
     int n = m.seq;
 #pragma unroll
     for (int i = 0; i < SC_CHUNK; ++i) {
@@ -342,19 +394,15 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_forward(sc_args a, c
             lanes.get_floats(h0 ? h0 + n * a.cols : NULL, H);
         }
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            float ka, ku;
-            sc_sides(s[i][w], ka, ku);
-            H[w] = __builtin_fmaf(ka, H[w], ku * lanes.get(x[i], w));
-        }
-        lanes.store(h + (t0 + i) * ld_h, H);
+        for (int w = 0; w < W; ++w) H[w] = __builtin_fmaf(keep[i][w], H[w], bring[i][w]);
+        lanes.store(row + i * ld_h, H);
         if (h_last && (m.last >> i & 1)) lanes.put_floats(h_last + n * a.cols, H);
     }
 }
 
-// The same from the last tile to the first, for c = a_t g_t; the state before every 32 tokens was kept.
+// The same from the last tile to the first, for c = a_t g_t; the state before every SC_CHUNK tokens was kept.
 template <class Y, int W>
-__global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_backward(sc_args a, const typename Y::T *__restrict__ dh, long long ld_dh,
+__global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_backward(sc_args a, const typename Y::T *__restrict__ dh, long long ld_dh,
                                                                         const typename Y::T *__restrict__ gate, long long ld_gate,
                                                                         const typename Y::T *__restrict__ v, long long ld_v, const float *__restrict__ h0,
                                                                         const float *__restrict__ kept, const float *__restrict__ dh_last,
@@ -362,25 +410,18 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_backward(sc_args a, 
                                                                         long long ld_dv, float *__restrict__ dh0) {
     __shared__ sc_room<W> room;
     const unsigned ticket = sc_ticket(a, room);
+    const int order = ticket / (unsigned)a.lanes_tiles, lanes_tile = ticket % (unsigned)a.lanes_tiles;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PP_WAVE), lane = threadIdx.x & (PP_WAVE - 1);
-    const int order = ticket / a.lanes_tiles, lanes_tile = ticket % a.lanes_tiles;
     const long long t0 = (long long)(a.tiles - 1 - order) * SC_TILE + (SC_WAVES - 1 - wave) * SC_CHUNK;
     const sc_lane<Y, W> lanes(lanes_tile, (unsigned)a.cols);
     unsigned f[SC_CHUNK], x[SC_CHUNK], d[SC_CHUNK];
-#pragma unroll
-    for (int i = 0; i < SC_CHUNK; ++i) {
-        const long long t = t0 + i < a.rows ? t0 + i : a.rows - 1;
-        f[i] = lanes.load(gate + t * ld_gate);
-        d[i] = lanes.load(dh + t * ld_dh);
-        x[i] = lanes.load(v + t * ld_v);
-    }
     float state[W];
     lanes.get_floats(t0 < a.rows ? kept + t0 / SC_CHUNK * a.cols : NULL, state);
+    lanes.load_all(f, gate, ld_gate, t0, a.rows);
+    lanes.load_all(x, v, ld_v, t0, a.rows);
+    lanes.load_all(d, dh, ld_dh, t0, a.rows);
     const sc_marks m = sc_mark(a.starts, a.rows, (int)a.seqs, t0);
-    if (!lanes.full)
-#pragma unroll
-        for (int i = 0; i < SC_CHUNK; ++i) f[i] >>= lanes.shift, x[i] >>= lanes.shift, d[i] >>= lanes.shift;
-    float s[SC_CHUNK][W], C[W], A[W], D[W], from[W];
+    const bool plain = m.in == ~sc_from(SC_CHUNK) && !m.first && !m.last;
     // of the sequences that end in the stretch the first one counts, which may have begun before
     const int cut = m.last ? __builtin_ctz(m.last) : -1;
     int behind = m.seq, ends = m.seq;  // the sequence of the last token, and that of token `cut`
@@ -389,63 +430,72 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_backward(sc_args a, 
         behind = sc_next(a.starts, (int)a.seqs, behind, a.rows, t0 + t);
         if (t <= cut) ends = behind;
     }
+    float s[SC_CHUNK][W], p[SC_CHUNK][W], C[W], A[W], D[W], from[W];
     if (cut >= 0) lanes.get_floats(dh_last ? dh_last + ends * a.cols : NULL, from);
+    // gates, and the states that the tokens find less their values
+    int n = m.seq;
+    auto states = [&](auto is_plain) {
+#pragma unroll
+        for (int i = 0; i < SC_CHUNK; ++i) {
+            if constexpr (!decltype(is_plain)::value) {
+                if (!(m.in >> i & 1)) continue;
+                if (m.first >> i & 1) {
+                    n = sc_next(a.starts, (int)a.seqs, n, a.rows, t0 + i);
+                    lanes.get_floats(h0 ? h0 + n * a.cols : NULL, state);
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                const float value = lanes.get(x[i], w);
+                float ka, ku;
+                const float g = lanes.get(f[i], w), e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(g)), large = __builtin_amdgcn_rcpf(1.0f + e);
+                const float small = e * large;
+                const bool keeps = g >= 0.0f;
+                s[i][w] = keeps ? small : -small;
+                ka = keeps ? large : small;
+                ku = keeps ? small : large;
+                p[i][w] = state[w] - value;
+                state[w] = __builtin_fmaf(ka, state[w], ku * value);
+            }
+        }
+    };
+    // its own stretch, from the last token to the first
 #pragma unroll
     for (int w = 0; w < W; ++w) C[w] = 0.0f, A[w] = 1.0f, D[w] = 0.0f;
+    auto stretch = [&](auto is_plain) {
 #pragma unroll
-    for (int i = SC_CHUNK - 1; i >= 0; --i) {
-        if (!(m.in >> i & 1)) continue;
-        if (i == cut)
+        for (int i = SC_CHUNK - 1; i >= 0; --i) {
+            if constexpr (!decltype(is_plain)::value) {
+                if (!(m.in >> i & 1)) continue;
+                if (i == cut)
 #pragma unroll
-            for (int w = 0; w < W; ++w) C[w] = from[w];
+                    for (int w = 0; w < W; ++w) C[w] = from[w];
+            }
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const float g = lanes.get(f[i], w), e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(g)), r = __builtin_amdgcn_rcpf(1.0f + e);
-            const float small = e * r;
-            const bool keeps = g >= 0.0f;
-            s[i][w] = keeps ? small : -small;
-            const float ka = keeps ? r : small, ku = keeps ? small : r;
-            C[w] = ka * (lanes.get(d[i], w) + C[w]);
-            D[w] = __builtin_fmaf(ka, D[w], ku);
-            A[w] *= ka;
+            for (int w = 0; w < W; ++w) {
+                float ka, ku;
+                sc_sides(s[i][w], ka, ku);
+                C[w] = ka * (lanes.get(d[i], w) + C[w]);
+                D[w] = __builtin_fmaf(ka, D[w], ku);
+                A[w] *= ka;
+            }
         }
+    };
+    if (plain) {
+        states(std::true_type());
+        stretch(std::true_type());
+    } else {
+        states(std::false_type());
+        stretch(std::false_type());
     }
 #pragma unroll
     for (int w = 0; w < W; ++w) {
         room.x[wave][lane * W + w] = cut >= 0 ? SC_CUT : sc_share(A[w], D[w]);
         room.H[wave][lane * W + w] = C[w];
     }
-    // the states that the tokens find, less their values
-    float p[SC_CHUNK][W];
-    int n = m.seq;
-#pragma unroll
-    for (int i = 0; i < SC_CHUNK; ++i) {
-        if (!(m.in >> i & 1)) continue;
-        if (m.first >> i & 1) {
-            n = sc_next(a.starts, (int)a.seqs, n, a.rows, t0 + i);
-            lanes.get_floats(h0 ? h0 + n * a.cols : NULL, state);
-        }
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const float value = lanes.get(x[i], w);
-            float ka, ku;
-            sc_sides(s[i][w], ka, ku);
-            p[i][w] = state[w] - value;
-            state[w] = __builtin_fmaf(ka, state[w], ku * value);
-        }
-    }
     __syncthreads();
     sc_carry<W>(a, room, order, lanes_tile, wave, C);
-    n = behind;
-    bool own = true;  // whether `n` is the sequence of what comes next
-#pragma unroll
-    for (int i = SC_CHUNK - 1; i >= 0; --i) {
-        if (!(m.in >> i & 1)) continue;
-        if (m.last >> i & 1) {
-            if (!own) n = sc_previous(a.starts, n, a.rows, t0 + i);
-            lanes.get_floats(dh_last ? dh_last + n * a.cols : NULL, C);
-        }
-        own = !(m.first >> i & 1);
+    auto gradients = [&](int i, typename Y::T *to_gate, typename Y::T *to_v) {
         float df[W], dx[W];
 #pragma unroll
         for (int w = 0; w < W; ++w) {
@@ -456,9 +506,34 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE) void k_scan_backward(sc_args a, 
             C[w] = ka * g;
             df[w] = p[i][w] * ku * C[w];
         }
-        lanes.store(dgate + (t0 + i) * ld_dgate, df);
-        lanes.store(dv + (t0 + i) * ld_dv, dx);
-        if (dh0 && (m.first >> i & 1)) lanes.put_floats(dh0 + n * a.cols, C);
+        lanes.store(to_gate, df);
+        lanes.store(to_v, dx);
+    };
+    typename Y::T *to_gate = dgate + (t0 + SC_CHUNK - 1) * ld_dgate, *to_v = dv + (t0 + SC_CHUNK - 1) * ld_dv;
+    if (plain) {
+#pragma unroll
+        for (int i = SC_CHUNK - 1; i >= 0; --i) {
+            gradients(i, to_gate, to_v);
+            to_gate -= ld_dgate;
+            to_v -= ld_dv;
+        }
+        return;
+    }
+    n = behind;
+    bool own = true;  // whether `n` is the sequence of what comes next
+#pragma unroll
+    for (int i = SC_CHUNK - 1; i >= 0; --i) {
+        if (m.in >> i & 1) {
+            if (m.last >> i & 1) {
+                if (!own) n = sc_previous(a.starts, n, a.rows, t0 + i);
+                lanes.get_floats(dh_last ? dh_last + n * a.cols : NULL, C);
+            }
+            own = !(m.first >> i & 1);
+            gradients(i, to_gate, to_v);
+            if (dh0 && (m.first >> i & 1)) lanes.put_floats(dh0 + n * a.cols, C);
+        }
+        to_gate -= ld_dgate;
+        to_v -= ld_dv;
     }
 }
 
@@ -541,9 +616,10 @@ static int sc_run(int64_t rows, int64_t cols, int64_t seqs, const int32_t *start
         k_scan_clear<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.ticket, a.stretch, words);
         if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
     }
+    const unsigned grid = (unsigned)(tiles * lanes);
     if (pairs) {
-        if constexpr (sizeof(typename Y::T) == 2) launch(a, (unsigned)(tiles * lanes), std::integral_constant<int, 2>());
-    } else launch(a, (unsigned)(tiles * lanes), std::integral_constant<int, 1>());
+        if constexpr (sizeof(typename Y::T) == 2) launch(a, grid, std::integral_constant<int, 2>());
+    } else launch(a, grid, std::integral_constant<int, 1>());
     return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
 }
 
