@@ -56,21 +56,24 @@ template <class Y> __device__ __forceinline__ PpRaw<Y> ls_load(const typename Y:
     return r;
 }
 
-// A thread's chunks of a segment x[0 .. n); whole segments without a branch, so that all loads are on their way together
-template <class Y, int HELD> __device__ __forceinline__ void ls_load_all(PpRaw<Y> (&raw)[HELD], const typename Y::T *x, long long n) {
-    if (n >= (long long)HELD * LS_STEP) {
+// The chunks of x[0 .. n) that a thread of THREADS holds; all that are whole without a branch, so that their loads are on their way
+// together
+template <class Y, int THREADS, int HELD> __device__ __forceinline__ void ls_load_row(PpRaw<Y> (&raw)[HELD], const typename Y::T *x, long long n) {
+    if (n >= (long long)HELD * THREADS * 8) {
 #pragma unroll
         for (int i = 0; i < HELD; ++i)
 #pragma unroll
-            for (int j = 0; j < PpRaw<Y>::W; ++j)
-                raw[i].w[j] = ((const pp_any16<sizeof(typename Y::T)> *)(x + 8 * (threadIdx.x + i * LS_THREADS)))[j].v;
+            for (int j = 0; j < PpRaw<Y>::W; ++j) raw[i].w[j] = ((const pp_any16<sizeof(typename Y::T)> *)((const char *)(x + 8 * i * THREADS) + threadIdx.x * (unsigned)(8 * sizeof(typename Y::T))))[j].v;
     } else {
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
-            const long long c = 8ll * (threadIdx.x + i * LS_THREADS);
-            raw[i] = ls_load<Y>(x + c, n - c);
+            const int left = (int)n - 8 * ((int)threadIdx.x + i * THREADS);
+            raw[i] = ls_load<Y>((const typename Y::T *)((const char *)(x + 8 * i * THREADS) + threadIdx.x * (unsigned)(8 * sizeof(typename Y::T))), left);
         }
     }
+}
+template <class Y, int HELD> __device__ __forceinline__ void ls_load_all(PpRaw<Y> (&raw)[HELD], const typename Y::T *x, long long n) {
+    ls_load_row<Y, LS_THREADS, HELD>(raw, x, n);
 }
 
 // Makes the compiler convert held values again where they are used again: kept as floats they would take twice the registers.

@@ -30,6 +30,28 @@ __device__ __forceinline__ float pp_wave_max(float v) {
     return pp_wave_all(v, [](float a, float b) { return __builtin_fmaxf(a, b); });
 }
 
+template <int CTRL> __device__ __forceinline__ double pp_moved(double v) {
+    const pp_u2 u = __builtin_bit_cast(pp_u2, v);
+    return __builtin_bit_cast(double, pp_u2{pp_moved<CTRL>(u[0]), pp_moved<CTRL>(u[1])});
+}
+__device__ __forceinline__ double pp_lane(double v, int lane) {
+    const pp_u2 u = __builtin_bit_cast(pp_u2, v);
+    return __builtin_bit_cast(double, pp_u2{(unsigned)__builtin_amdgcn_readlane((int)u[0], lane), (unsigned)__builtin_amdgcn_readlane((int)u[1], lane)});
+}
+template <class F> __device__ __forceinline__ double pp_wave_all(double v, F op) {
+    v = op(v, pp_moved<0xB1>(v));
+    v = op(v, pp_moved<0x4E>(v));
+    v = op(v, pp_moved<0x141>(v));
+    v = op(v, pp_moved<0x140>(v));
+    return op(op(pp_lane(v, 0), pp_lane(v, 16)), op(pp_lane(v, 32), pp_lane(v, 48)));
+}
+__device__ __forceinline__ double pp_wave_sum(double v) {
+    return pp_wave_all(v, [](double a, double b) { return a + b; });
+}
+__device__ __forceinline__ double pp_wave_max(double v) {
+    return pp_wave_all(v, [](double a, double b) { return __builtin_fmax(a, b); });
+}
+
 // The sum over a workgroup of WAVES waves.  `room` holds WAVES floats; whoever calls this again on the same room passes a
 // barrier in between.
 template <int WAVES> __device__ __forceinline__ float pp_group_sum(float v, float *room) {
