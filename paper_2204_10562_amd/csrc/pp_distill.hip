@@ -10,7 +10,9 @@
 // Else three kernels: the sums of segments; a wave to a row for the list; the gradient.
 #include "pp_loss.h"
 
-#define DS_MEET 16  // most segments of a row whose workgroups meet
+#define DS_MEET 16   // most segments of a row whose workgroups meet
+#define DS_MEET_FROM (1ll << 27)  // bytes of logits from which on they are read once
+#define DS_HELD 8    // chunks to a thread
 
 struct ds_args {
     long long rows, cols, size, ld, ld_d;
@@ -426,9 +428,11 @@ template <int HELD, class F> static void by_held(int held, F f) {
 
 static unsigned grid_of(int64_t items) { return (unsigned)(items < LS_MAX_GRID ? items : LS_MAX_GRID); }
 
-// The segments of a call whose workgroups meet, about equally long; segs 0: rows are too few or too long for it.  Few chunks to a
-// thread, so that more workgroups than four are there to work while one waits (8: 329 us for 349, 2048 x 131072 bf16 read twice).
-static ls_plan ds_meeting(int type, int64_t rows, int64_t cols) {
+// The segments of a row whose workgroups meet, about equally long; segs 0: rows are too long for it.  Few chunks to a
+// thread, so that more workgroups than four are there to work while one waits.  What the last cache holds (256 MB, logits and
+// gradient) is as well read twice: 777 x 50001 fp16 80 us in a meeting, 76 read twice, 4096 x 8000 bf16 87 and 63; but
+// 1500 x 50001 fp16 117 and 132, 1024 x 131072 bf16 151 and 173.
+static ls_plan ds_segments(int type, int64_t cols) {
     ls_plan p = {};
     for (int held = type == PP_TYPE_F32 ? 4 : 8; held <= (type == PP_TYPE_F32 ? 8 : 16); held *= 2) {
         const int64_t segs = (cols + (int64_t)held * LS_STEP - 1) / ((int64_t)held * LS_STEP);
@@ -438,15 +442,16 @@ static ls_plan ds_meeting(int type, int64_t rows, int64_t cols) {
         p.segs = (int)((cols + p.size - 1) / p.size);
         break;
     }
-    if (rows * p.segs < LS_ENOUGH || rows * p.segs > (1 << 24)) p.segs = 0;
     return p;
+}
+static bool ds_meets(int type, int64_t rows, int64_t cols, const ls_plan &p) {
+    return p.segs && rows * cols * pp_type_size(type) >= DS_MEET_FROM && rows * p.segs <= 1 << 24;
 }
 
 extern "C" size_t pp_distill_workspace_bytes(int type, int64_t rows, int64_t cols, int top) {
     if (pp_bad_sizes(type, rows, cols) || top < 1 || top > PP_TOP_MAX) return 0;
-    // (of the words: at most DS_MEET segments' of any rows that meet)
-    return 256 + pp_align256((size_t)ls_most(type, rows, cols) * sizeof(pp_f2)) + pp_align256((size_t)rows * sizeof(pp_f2)) + pp_align256((size_t)rows * top * 4) +
-           pp_align256((size_t)rows * DS_MEET * 16);
+    return 256 + pp_align256((size_t)ls_most(type, rows, cols, DS_HELD) * sizeof(pp_f2)) + pp_align256((size_t)rows * sizeof(pp_f2)) + pp_align256((size_t)rows * top * 4) +
+           pp_align256((size_t)rows * ds_segments(type, cols).segs * 16);
 }
 
 extern "C" int pp_distill_loss(int kind, int type, int64_t rows, int64_t cols, const void *logits, int64_t ld, float temperature, int top,
@@ -460,10 +465,10 @@ extern "C" int pp_distill_loss(int kind, int type, int64_t rows, int64_t cols, c
     if (rows && (!top_index || !top_value || !loss)) return PP_ERR_INVALID_ARG;
     if (!rows) return PP_OK;
     if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < pp_distill_workspace_bytes(type, rows, cols, top)) return PP_ERR_WORKSPACE;
-    const ls_plan p = ls_divide(type, rows, cols);
-    const ls_plan meet = dlogits ? ds_meeting(type, rows, cols) : ls_plan();
+    const ls_plan p = ls_divide(type, rows, cols, DS_HELD);
+    const ls_plan meet = ds_segments(type, cols);
     char *ws = (char *)workspace + 256;
-    pp_f2 *sums = (pp_f2 *)ws, *tail = (pp_f2 *)(ws + pp_align256((size_t)ls_most(type, rows, cols) * sizeof(pp_f2)));
+    pp_f2 *sums = (pp_f2 *)ws, *tail = (pp_f2 *)(ws + pp_align256((size_t)ls_most(type, rows, cols, DS_HELD) * sizeof(pp_f2)));
     float *listed = (float *)((char *)tail + pp_align256((size_t)rows * sizeof(pp_f2)));
     unsigned long long *words = (unsigned long long *)((char *)listed + pp_align256((size_t)rows * top * 4));
     ds_args a = {rows, cols, p.size, ld, ld_d, p.segs, top, kind == PP_DISTILL_REST, (float)(1.4426950408889634 / temperature), 1.0 / temperature, top_index,
@@ -472,7 +477,7 @@ extern "C" int pp_distill_loss(int kind, int type, int64_t rows, int64_t cols, c
     return pp_by_type(type, [&](auto tag) {
         typedef decltype(tag) Y;
         typedef typename Y::T T;
-        if (meet.segs) {
+        if (dlogits && ds_meets(type, rows, cols, meet)) {
             a.segs = meet.segs;
             a.size = meet.size;
             const int64_t items = rows * meet.segs, groups = (items * 2 + 1023) / 1024;
@@ -487,9 +492,9 @@ extern "C" int pp_distill_loss(int kind, int type, int64_t rows, int64_t cols, c
             return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
         }
         auto by_plan = [&](auto f) {
-            constexpr int MOST = 32 / sizeof(T);
+            constexpr int MOST = sizeof(T) == 4 ? DS_HELD / 2 : DS_HELD;
             if (p.held == MOST) f(std::integral_constant<int, MOST>());
-            else if (p.held == 4) f(std::integral_constant<int, 4>());
+            else if (p.held == MOST / 2) f(std::integral_constant<int, MOST / 2>());
             else f(std::integral_constant<int, 1>());
         };
         by_plan([&](auto h) {

@@ -12,6 +12,8 @@
 // column is found bit by bit by all threads.  Segments' lists are joined in the same way.
 #include "pp_loss.h"
 
+#define LP_HELD 16  // chunks to a thread: half of it takes a tenth longer (2048 x 131072 bf16 with 64 alternatives), which segments find for themselves
+
 struct lp_args {
     long long rows, cols, size, ld;
     int segs, top;
@@ -331,7 +333,7 @@ static bool bad4(const void *p) { return ((uintptr_t)p & 3) != 0; }
 
 extern "C" size_t pp_logprob_workspace_bytes(int type, int64_t rows, int64_t cols, int top) {
     if (pp_bad_sizes(type, rows, cols) || top < 0 || top > PP_TOP_MAX) return 0;
-    const size_t most = (size_t)ls_most(type, rows, cols);
+    const size_t most = (size_t)ls_most(type, rows, cols, LP_HELD);
     return pp_align256(most * sizeof(pp_f4)) + pp_align256(most * top * sizeof(unsigned long long)) + 256;
 }
 
@@ -342,7 +344,7 @@ extern "C" int pp_logprob_forward(int type, int64_t rows, int64_t cols, const vo
     if (bad4(tokens) || bad4(logp) || bad4(entropy) || ((uintptr_t)norm & 7) || bad4(top_index) || bad4(top_logp)) return PP_ERR_INVALID_ARG;
     if (top < 0 || top > PP_TOP_MAX || (rows && ((logp && !tokens) || (top && (!top_index || !top_logp))))) return PP_ERR_INVALID_ARG;
     if (!rows) return PP_OK;
-    const ls_plan p = ls_divide(type, rows, cols);
+    const ls_plan p = ls_divide(type, rows, cols, LP_HELD);
     if (p.segs > 1)
         if (!workspace || ((uintptr_t)workspace & 255) || workspace_bytes < pp_logprob_workspace_bytes(type, rows, cols, top)) return PP_ERR_WORKSPACE;
     pp_f4 *sums = (pp_f4 *)workspace;

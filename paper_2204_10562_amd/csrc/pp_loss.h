@@ -19,9 +19,12 @@ struct ls_plan {
     long long size;
 };
 
+// Most chunks that a thread holds: a 16-bit type's `most`, half of that in float
+static inline int ls_held(int type, int most) { return type == PP_TYPE_F32 ? most / 2 : most; }
+
 // The largest segments, for their fewer partial results; smaller ones where those are as few, and to spread few rows over the chip.
-static inline ls_plan ls_divide(int type, int64_t rows, int64_t cols) {
-    const int sizes[3] = {type == PP_TYPE_F32 ? 8 : 16, 4, 1};
+static inline ls_plan ls_divide(int type, int64_t rows, int64_t cols, int most) {
+    const int sizes[3] = {ls_held(type, most), most > 8 ? 4 : ls_held(type, most) / 2, 1};
     ls_plan p = {};
     for (int i = 0;; ++i) {
         p.held = sizes[i];
@@ -35,9 +38,9 @@ static inline ls_plan ls_divide(int type, int64_t rows, int64_t cols) {
 
 // No more segments than this of any number of rows up to `rows` (those that are not the largest are less than LS_ENOUGH
 // segments of the size before, of at most four each).
-static inline int64_t ls_most(int type, int64_t rows, int64_t cols) {
-    const int64_t size = (int64_t)(type == PP_TYPE_F32 ? 8 : 16) * LS_STEP, most = rows * ((cols + size - 1) / size);
-    return most > 4 * LS_ENOUGH ? most : 4 * LS_ENOUGH;
+static inline int64_t ls_most(int type, int64_t rows, int64_t cols, int most) {
+    const int64_t size = (int64_t)ls_held(type, most) * LS_STEP, all = rows * ((cols + size - 1) / size);
+    return all > 4 * LS_ENOUGH ? all : 4 * LS_ENOUGH;
 }
 
 // Eight logits as floats, -infinity behind the n-th

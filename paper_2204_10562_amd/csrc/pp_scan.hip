@@ -537,14 +537,11 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_backward(sc_args 
     }
 }
 
-// What tiles wait for is not there yet.
-__global__ __launch_bounds__(256) void k_scan_clear(unsigned *ticket, unsigned long long *words, long long n) {
-    if (blockIdx.x == 0 && !threadIdx.x) *ticket = 0;
-    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < n; i += gridDim.x * 256ll) words[i] = SC_EMPTY;
-}
-
-// Sequences without tokens: what they begin with is what they end with.
-__global__ __launch_bounds__(256) void k_scan_empty(sc_args a, const float *__restrict__ from, float *__restrict__ to) {
+// What tiles wait for is not there yet; and sequences without tokens end with what they begin with.
+__global__ __launch_bounds__(256) void k_scan_begin(sc_args a, long long words, const float *__restrict__ from, float *__restrict__ to) {
+    if (words && blockIdx.x == 0 && !threadIdx.x) *a.ticket = 0;
+    for (long long i = blockIdx.x * 256ll + threadIdx.x; i < words; i += gridDim.x * 256ll) a.stretch[i] = SC_EMPTY;
+    if (!to) return;
     for (long long n = blockIdx.x; n < a.seqs; n += gridDim.x) {
         if (a.starts ? sc_start(a.starts, a.rows, n) < sc_start(a.starts, a.rows, n + 1) : a.rows > 0) continue;
         for (long long c = threadIdx.x; c < a.cols; c += 256) to[n * a.cols + c] = from ? from[n * a.cols + c] : 0.0f;
@@ -598,11 +595,6 @@ extern "C" int64_t pp_scan_kept_rows(int type, int64_t rows, int64_t cols) {
 template <class Y, class F>
 static int sc_run(int64_t rows, int64_t cols, int64_t seqs, const int32_t *starts, void *workspace, hipStream_t st, const float *from, float *to, F launch) {
     sc_args a = {rows, cols, seqs, starts};
-    if (to) {
-        k_scan_empty<<<(unsigned)(seqs < 65536 ? seqs : 65536), 256, 0, st>>>(a, from, to);
-        if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
-    }
-    if (!rows) return PP_OK;
     const bool pairs = sizeof(typename Y::T) == 2 && cols > 1;
     const int64_t per = pairs ? 2 * PP_WAVE : PP_WAVE, lanes = (cols + per - 1) / per, tiles = sc_tiles(rows);
     a.tiles = (int)tiles;
@@ -611,11 +603,14 @@ static int sc_run(int64_t rows, int64_t cols, int64_t seqs, const int32_t *start
     a.ticket = (unsigned *)workspace;
     a.stretch = (unsigned long long *)((char *)workspace + 256);
     a.whole = a.stretch + tiles * a.width;
-    if (tiles > 1) {
-        const int64_t words = (tiles + tiles / SC_GROUP + 1) * a.width, groups = (words + 1023) / 1024;
-        k_scan_clear<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(a.ticket, a.stretch, words);
+    const int64_t words = tiles > 1 ? (tiles + tiles / SC_GROUP + 1) * a.width : 0;
+    if (words || to) {
+        int64_t groups = (words + 1023) / 1024;
+        if (to && groups < seqs) groups = seqs;
+        k_scan_begin<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(a, words, from, to);
         if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
     }
+    if (!rows) return PP_OK;
     const unsigned grid = (unsigned)(tiles * lanes);
     if (pairs) {
         if constexpr (sizeof(typename Y::T) == 2) launch(a, grid, std::integral_constant<int, 2>());

@@ -341,6 +341,53 @@ def test_distill_rows_at_their_ends(t, cols):
         assert_within(np.nan_to_num(dx, nan=9.0), np.nan_to_num(wx, nan=9.0), 400 * U * (1 + np.abs(np.nan_to_num(wx))), t)
 
 
+@pytest.mark.parametrize("t, rows, cols, pad", [("bf16", 1101, 61007, 1), ("bf16", 257, 262144, 0), ("f16", 517, 131071, 0), ("f32", 300, 120001, 3), ("f32", 5000, 7001, 0), ("f32", 120, 300001, 0)])
+@pytest.mark.parametrize("kind", ["top", "rest"])
+def test_distill_of_many(t, rows, cols, pad, kind):
+    """So many logits that they are read once, by workgroups that meet (the last ones have rows too long for it): some rows against the formula,
+    among them such as have nothing to learn or are no numbers, and all of them again in place."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    assert rows * cols * (4 if t == "f32" else 2) >= 1 << 27
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    top = 30
+    room = torch.empty(rows, cols + pad, dtype=torch_type(t), device="cuda")
+    x = room[:, :cols]
+    for r in range(0, rows, 64):
+        n = min(64, rows - r)
+        x[r:r + n] = torch.randn(n, cols, generator=g, device="cuda") * 3
+    x[1::7, cols - cols // 3:] = -float("inf")
+    index = torch.randint(0, cols // 2, (rows, top), generator=g, device="cuda", dtype=torch.int32)
+    index[::3, :5] = torch.arange(5, dtype=torch.int32, device="cuda") * (cols // 5) + 3
+    value = torch.log(torch.rand(rows, top, generator=g, device="cuda") * 0.02 + 0.005)
+    weight = torch.rand(rows, generator=g, device="cuda") + 0.1
+    weight[2::9] = 0
+    bad, none, empty, lost = 10, 12, 16, 18          # a NaN, no list, nothing but -infinity, +infinity in a listed column
+    x[bad, cols - 2], x[lost, 3] = float("nan"), float("inf")
+    x[empty] = -float("inf")
+    index[none], index[lost, 0] = -1, 3
+    weight[[bad, none, empty, lost]] = 1.0
+    loss, dx = torch.empty(rows, device="cuda"), torch.full_like(room, 77)
+    ws = work(pp.pp_distill_workspace_bytes(torch_type(t), rows, cols, top), t)
+    k = {"top": 0, "rest": 1}[kind]
+    pp.pp_distill_loss(k, x, 1.0, index, value, weight, loss, dx[:, :cols], ws)
+    assert pad == 0 or (dx[:, cols:] == 77).all()
+    picked = sorted(set(range(0, 24)) | set(range(0, rows, rows // 12)) | {rows - 1})
+    fine = [r for r in picked if r not in (bad, none, empty, lost)]
+    host = lambda v, at: v[at].double().cpu().numpy()  # noqa: E731
+    check_distill(kind, host(x, fine), 1.0, index[fine].cpu().numpy(), value[fine].cpu().numpy(), host(weight, fine).astype(np.float32), host(loss, fine),
+                  host(dx[:, :cols], fine), t)
+    assert torch.isnan(loss[[bad, lost]]).all() and torch.isnan(dx[[bad, lost], :cols]).all()
+    assert torch.isinf(loss[empty]) and (dx[empty, :cols] == 0).all()
+    if kind == "top":
+        assert loss[none] == 0 and (dx[none, :cols] == 0).all()
+    else:                                            # everything is the rest: no divergence (r - p_rest is a rounding)
+        assert abs(loss[none]) <= 400 * U and (dx[none, :cols].float().abs() <= 400 * U).all()
+    again = torch.empty_like(loss)
+    pp.pp_distill_loss(k, x, 1.0, index, value, weight, again, x, ws)
+    assert torch.equal(again.nan_to_num(5.0), loss.nan_to_num(5.0)) and torch.equal(x.nan_to_num(5.0), dx[:, :cols].nan_to_num(5.0))
+
+
 def test_large_offsets():
     """Rows whose offsets pass 2^32 bytes, and 2^31 values."""
     import torch
