@@ -87,11 +87,15 @@ template <class Y, int N> __device__ __forceinline__ void ls_hold(PpRaw<Y> (&raw
         for (int j = 0; j < PpRaw<Y>::W; ++j) asm volatile("" : "+v"(raw[i].w[j]));
 }
 
+// (The compiler's fmax quiets each operand first, which is an instruction to a logit.  A NaN may be passed over or not: a row that has
+// one has a sum that is none.)
+__device__ __forceinline__ float ls_max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 __device__ __forceinline__ float ls_max8(const float *v) {
-    float m = __builtin_fmaxf(__builtin_fmaxf(v[0], v[1]), v[2]);
-    m = __builtin_fmaxf(__builtin_fmaxf(m, v[3]), v[4]);
-    m = __builtin_fmaxf(__builtin_fmaxf(m, v[5]), v[6]);
-    return __builtin_fmaxf(m, v[7]);
+    return ls_max3(ls_max3(ls_max3(v[0], v[1], v[2]), v[3], v[4]), ls_max3(v[5], v[6], v[7]), v[7]);
 }
 
 // What a maximum is subtracted as: 0 where there is nothing but -infinity (then every term is 0)
