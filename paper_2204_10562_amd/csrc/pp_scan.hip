@@ -57,59 +57,71 @@ struct sc_args {
     long long width;
 };
 
-// What a wave's tokens t0 .. t0 + SC_CHUNK - 1 have to do with sequences, a bit each: whether a sequence has them, starts with them,
-// ends with them; and the last sequence that starts before them (-1: none).
-struct sc_marks {
-    unsigned in, first, last;
-    int seq;
-};
 __device__ __forceinline__ long long sc_start(const int *starts, long long rows, long long n) {
     const long long t = starts[n];
     return t < 0 ? 0 : t > rows ? rows : t;
 }
 __device__ __forceinline__ unsigned sc_from(long long t) { return t <= 0 ? ~0u : t >= 32 ? 0u : ~0u << t; }  // bits t and above
 
+// What a wave's tokens t0 .. t0 + SC_CHUNK - 1 have to do with sequences, a bit each: whether a sequence has them, starts with them,
+// ends with them.  The lanes look at 64 starts at a time.
+struct sc_marks {
+    unsigned in, first, last;
+    int base, next;  // sequences that start before the tokens; of 64 behind those, the lane's start from t0 on
+    bool more;       // there are yet others among the tokens
+    // the sequence of token t0 + i
+    __device__ __forceinline__ int of(const int *starts, long long rows, int seqs, long long t0, int i) const {
+        int n = base + __popcll(__ballot(next <= i));
+        if (more)
+            while (n < seqs && sc_start(starts, rows, n) <= t0 + i) ++n;
+        return n > 0 ? n - 1 : 0;
+    }
+};
+
 __device__ __forceinline__ sc_marks sc_mark(const int *__restrict__ starts, long long rows, int seqs, long long t0) {
+    const int lane = threadIdx.x & (PP_WAVE - 1), far = 0x7fffffff;
+    long long begin = 0, end = rows;
     sc_marks m;
-    const unsigned all = ~sc_from(SC_CHUNK);
-    const long long begin = starts ? sc_start(starts, rows, 0) : 0, end = starts ? sc_start(starts, rows, seqs) : rows;
-    m.in = sc_from(begin - t0) & ~sc_from(end - t0) & all;
-    m.last = end - t0 > 0 && end - t0 <= SC_CHUNK ? 1u << (end - t0 - 1) : 0u;
-    if (!starts) {
-        m.first = t0 == 0;
-        m.seq = 0;
-        return m;
+    m.base = 0;
+    m.more = false;
+    m.next = lane || t0 ? far : 0;
+    if (!starts) m.base = t0 > 0;
+    else if (seqs < PP_WAVE) {
+        const int at = (int)sc_start(starts, rows, lane < seqs ? lane : seqs);
+        begin = __builtin_amdgcn_readlane(at, 0);
+        end = __builtin_amdgcn_readlane(at, seqs);
+        m.base = __popcll(__ballot(lane < seqs && at < t0));
+        m.next = lane >= m.base && lane < seqs ? (int)(at - t0) : far;
+    } else {
+        begin = sc_start(starts, rows, 0);
+        end = sc_start(starts, rows, seqs);
+        int lo = 0, hi = seqs;  // the first n with starts[n] >= t0 is not before lo, and not behind hi
+        while (lo < hi) {
+            const int step = (hi - lo + PP_WAVE - 1) / PP_WAVE, at = lo + lane * step;
+            const int below = __popcll(__ballot(lane <= (hi - 1 - lo) / step && sc_start(starts, rows, at < hi ? at : hi - 1) < t0));
+            hi = below * (long long)step < hi - lo ? lo + below * step : hi;
+            lo = below ? lo + (below - 1) * step + 1 : lo;
+        }
+        m.base = lo;
+        m.next = lo + lane < seqs ? (int)(sc_start(starts, rows, lo + lane) - t0) : far;
+        m.more = __builtin_amdgcn_readlane(m.next, PP_WAVE - 1) <= SC_CHUNK;
     }
-    int lo = 0, hi = seqs;  // the first n with starts[n] >= t0, seqs if none before
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (sc_start(starts, rows, mid) >= t0) hi = mid;
-        else lo = mid + 1;
-    }
-    m.seq = lo - 1;
-    m.first = 0;
-    for (int n = lo; n < seqs; ++n) {
-        const long long t = sc_start(starts, rows, n) - t0;
-        if (t < 0 || t > SC_CHUNK) break;
-        m.first |= 1u << t;  // (bit SC_CHUNK: the next wave's first token)
-    }
-    m.last = (m.last | m.first >> 1) & m.in;
-    m.first &= m.in;
+    m.in = sc_from(begin - t0) & ~sc_from(end - t0) & ~sc_from(SC_CHUNK);
+    unsigned bits = m.next >= 0 && m.next <= SC_CHUNK ? 1u << m.next : 0u;  // (bit SC_CHUNK: the next wave's first token)
+    if (m.more)
+        for (long long n = (long long)m.base + PP_WAVE + lane; n < seqs; n += PP_WAVE) {
+            const long long t = sc_start(starts, rows, n) - t0;
+            if (t < 0 || t > SC_CHUNK) break;
+            bits |= 1u << t;
+        }
+    bits |= pp_moved<0xB1>(bits);
+    bits |= pp_moved<0x4E>(bits);
+    bits |= pp_moved<0x141>(bits);
+    bits |= pp_moved<0x140>(bits);
+    bits = __builtin_amdgcn_readlane(bits, 0) | __builtin_amdgcn_readlane(bits, 16) | __builtin_amdgcn_readlane(bits, 32) | __builtin_amdgcn_readlane(bits, 48);
+    m.first = bits & m.in;
+    m.last = ((end - t0 > 0 && end - t0 <= SC_CHUNK ? 1u << (end - t0 - 1) : 0u) | bits >> 1) & m.in;
     return m;
-}
-// the sequence that starts with token t, where `n` is that of a token before (or -1)
-__device__ __forceinline__ int sc_next(const int *__restrict__ starts, int seqs, int n, long long rows, long long t) {
-    if (!starts) return 0;
-    do ++n;
-    while (n < seqs - 1 && sc_start(starts, rows, n + 1) <= t);
-    return n < seqs ? n : seqs - 1;
-}
-// the one that ends with token t, where `n` is that of a token behind (or seqs)
-__device__ __forceinline__ int sc_previous(const int *__restrict__ starts, int n, long long rows, long long t) {
-    if (!starts) return 0;
-    do --n;
-    while (n > 0 && sc_start(starts, rows, n) > t);
-    return n < 0 ? 0 : n;
 }
 
 // W channels of a token to a lane: two 16-bit values of a word, or one value.  A row's address is the same for all lanes, a lane's
@@ -337,11 +349,8 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_forward(sc_args a
     // a and (1 - a) v of the wave's tokens, and its own stretch; of the sequences that start in it the last one counts
     float keep[SC_CHUNK][W], bring[SC_CHUNK][W], H[W], A[W], D[W], from[W];
     const int cut = m.first ? 31 - __builtin_clz(m.first) : -1;
-    if (cut >= 0) {
-        int n = m.seq;
-        for (unsigned left = m.first; left; left &= left - 1) n = sc_next(a.starts, (int)a.seqs, n, a.rows, t0 + __builtin_ctz(left));
-        lanes.get_floats(h0 ? h0 + n * a.cols : NULL, from);
-    }
+    auto sequence = [&](int i) { return (long long)m.of(a.starts, a.rows, (int)a.seqs, t0, i); };
+    if (cut >= 0) lanes.get_floats(h0 ? h0 + sequence(cut) * a.cols : NULL, from);
 #pragma unroll
     for (int w = 0; w < W; ++w) H[w] = 0.0f, A[w] = 1.0f, D[w] = 0.0f;
     auto stretch = [&](auto is_plain) {
@@ -385,18 +394,14 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_forward(sc_args a
         }
         return;
     }
-    int n = m.seq;
 #pragma unroll
     for (int i = 0; i < SC_CHUNK; ++i) {
         if (!(m.in >> i & 1)) continue;
-        if (m.first >> i & 1) {
-            n = sc_next(a.starts, (int)a.seqs, n, a.rows, t0 + i);
-            lanes.get_floats(h0 ? h0 + n * a.cols : NULL, H);
-        }
+        if (m.first >> i & 1) lanes.get_floats(h0 ? h0 + sequence(i) * a.cols : NULL, H);
 #pragma unroll
         for (int w = 0; w < W; ++w) H[w] = __builtin_fmaf(keep[i][w], H[w], bring[i][w]);
         lanes.store(row + i * ld_h, H);
-        if (h_last && (m.last >> i & 1)) lanes.put_floats(h_last + n * a.cols, H);
+        if (h_last && (m.last >> i & 1)) lanes.put_floats(h_last + sequence(i) * a.cols, H);
     }
 }
 
@@ -424,25 +429,16 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_backward(sc_args 
     const bool plain = m.in == ~sc_from(SC_CHUNK) && !m.first && !m.last;
     // of the sequences that end in the stretch the first one counts, which may have begun before
     const int cut = m.last ? __builtin_ctz(m.last) : -1;
-    int behind = m.seq, ends = m.seq;  // the sequence of the last token, and that of token `cut`
-    for (unsigned left = m.first; left; left &= left - 1) {
-        const int t = __builtin_ctz(left);
-        behind = sc_next(a.starts, (int)a.seqs, behind, a.rows, t0 + t);
-        if (t <= cut) ends = behind;
-    }
+    auto sequence = [&](int i) { return (long long)m.of(a.starts, a.rows, (int)a.seqs, t0, i); };
     float s[SC_CHUNK][W], p[SC_CHUNK][W], C[W], A[W], D[W], from[W];
-    if (cut >= 0) lanes.get_floats(dh_last ? dh_last + ends * a.cols : NULL, from);
+    if (cut >= 0) lanes.get_floats(dh_last ? dh_last + sequence(cut) * a.cols : NULL, from);
     // gates, and the states that the tokens find less their values
-    int n = m.seq;
     auto states = [&](auto is_plain) {
 #pragma unroll
         for (int i = 0; i < SC_CHUNK; ++i) {
             if constexpr (!decltype(is_plain)::value) {
                 if (!(m.in >> i & 1)) continue;
-                if (m.first >> i & 1) {
-                    n = sc_next(a.starts, (int)a.seqs, n, a.rows, t0 + i);
-                    lanes.get_floats(h0 ? h0 + n * a.cols : NULL, state);
-                }
+                if (m.first >> i & 1) lanes.get_floats(h0 ? h0 + sequence(i) * a.cols : NULL, state);
             }
 #pragma unroll
             for (int w = 0; w < W; ++w) {
@@ -519,18 +515,12 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_backward(sc_args 
         }
         return;
     }
-    n = behind;
-    bool own = true;  // whether `n` is the sequence of what comes next
 #pragma unroll
     for (int i = SC_CHUNK - 1; i >= 0; --i) {
         if (m.in >> i & 1) {
-            if (m.last >> i & 1) {
-                if (!own) n = sc_previous(a.starts, n, a.rows, t0 + i);
-                lanes.get_floats(dh_last ? dh_last + n * a.cols : NULL, C);
-            }
-            own = !(m.first >> i & 1);
+            if (m.last >> i & 1) lanes.get_floats(dh_last ? dh_last + sequence(i) * a.cols : NULL, C);
             gradients(i, to_gate, to_v);
-            if (dh0 && (m.first >> i & 1)) lanes.put_floats(dh0 + n * a.cols, C);
+            if (dh0 && (m.first >> i & 1)) lanes.put_floats(dh0 + sequence(i) * a.cols, C);
         }
         to_gate -= ld_dgate;
         to_v -= ld_dv;

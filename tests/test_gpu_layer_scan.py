@@ -23,6 +23,9 @@ def lists(rows, kind, rng):
         lo, hi = rows // 7, rows - rows // 5
         cuts = sorted(int(x) for x in rng.integers(lo, hi + 1, 5))
         return [lo, lo] + cuts + [cuts[-1], hi, hi]
+    if kind == "crowded":       # a hundred empty sequences at some places
+        cuts = sorted([int(x) for x in rng.integers(0, rows + 1, 9)] * 100 + [int(x) for x in rng.integers(0, rows + 1, 30)])
+        return [0] + cuts + [rows]
     if kind == "tokens":        # every sequence one token
         return list(range(rows + 1))
     cuts = sorted(set(int(x) for x in rng.integers(0, rows + 1, max(1, rows // 9))))
@@ -120,7 +123,7 @@ def run(t, starts, gate, v, h0, dh, dh_last, carried=True, pad=0, off=0, null=Fa
     assert all((x[:front] == 7).all() and (x[front + size:] == 7).all() for x in (last, dh0))
 
 
-@pytest.mark.parametrize("kind", ["one", "padded", "tokens", "mixed"])
+@pytest.mark.parametrize("kind", ["one", "padded", "tokens", "mixed", "crowded"])
 @pytest.mark.parametrize("rows, cols", [(1, 1), (2, 70), (31, 8), (33, 130), (64, 64), (127, 5), (200, 300), (513, 129), (1000, 66)])
 @pytest.mark.parametrize("t", ["bf16", "f16", "f32"])
 def test_sequences(t, rows, cols, kind):
