@@ -62,7 +62,7 @@ struct lp_room {
     float wave[8];
     unsigned max[LS_THREADS];
     unsigned found, tau, count[4];
-    lp_entry entry[LS_CAP + 8];
+    lp_entry entry[LS_CAP + 32];
 };
 
 // The K-th largest of the 256 keys in room.max, by one wave: bits below `low` are the same for all.  0 if there are fewer.
@@ -119,16 +119,40 @@ template <class F> __device__ __forceinline__ void narrow(lp_room &room, int top
     __syncthreads();
 }
 
+// A long list once more: where fewer threads than `top` had anything, all of it is there.  Of four entries to a thread the
+// maxima give a threshold as those of a segment do.
+__device__ __forceinline__ void shorten(lp_room &room, int top) {
+    const int t = threadIdx.x, found = (int)room.found;
+    lp_entry mine[LS_CAP / LS_THREADS];
+    unsigned most = 0;
+#pragma unroll
+    for (int i = 0; i < LS_CAP / LS_THREADS; ++i) {
+        mine[i] = t + i * LS_THREADS < found ? room.entry[t + i * LS_THREADS] : 0;
+        most = lp_key(mine[i]) > most ? lp_key(mine[i]) : most;
+    }
+    room.max[t] = most;
+    __syncthreads();
+    find_threshold(room, top, 0);
+    __syncthreads();
+    const unsigned tau = room.tau > 1 ? room.tau : 1;
+#pragma unroll
+    for (int i = 0; i < LS_CAP / LS_THREADS; ++i) append(room, lp_key(mine[i]) >= tau, [&](auto put) { put(mine[i]); });
+    __syncthreads();
+}
+
 // The list's first `top` entries in order into put(rank, entry), and none behind them.  Four lanes to an entry, each with a
 // quarter of the others.
 template <class F> __device__ __forceinline__ void rank_list(lp_room &room, int top, F put) {
-    const int t = threadIdx.x, found = (int)(room.found < LS_CAP ? room.found : LS_CAP), ends = (found + 7) & ~7;
+    if (room.found > LS_THREADS) shorten(room, top);
+    const int t = threadIdx.x, found = (int)room.found, ends = (found + 31) & ~31;
     if (t < ends - found) room.entry[found + t] = 0;
     __syncthreads();
     for (int i = t >> 2; i < ends; i += LS_THREADS / 4) {
         const lp_entry mine = room.entry[i];
         unsigned rank = 0;
-        for (int o = t & 3; o < ends; o += 8) rank += (room.entry[o] > mine) + (room.entry[o + 4] > mine);
+        for (int o = t & 3; o < ends; o += 32)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) rank += room.entry[o + 4 * k] > mine;
         rank += pp_moved<0xB1>(rank);
         rank += pp_moved<0x4E>(rank);
         if (!(t & 3) && mine && rank < (unsigned)top) put((int)rank, mine);

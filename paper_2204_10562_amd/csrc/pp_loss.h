@@ -10,7 +10,7 @@
 #define LS_STEP (LS_THREADS * 8)  // logits that a workgroup reads at a time
 #define LS_MAX_GRID (1 << 22)
 #define LS_ENOUGH 1024           // workgroups that fill the chip
-#define LS_CAP 512                // candidates of a segment that are ranked at once
+#define LS_CAP 1024               // candidates of a segment that are kept: what fewer threads than PP_TOP_MAX have at least
 
 // Rows of `cols` in `segs` segments of `size` (the last shorter), `held` chunks of eight to a thread.
 struct ls_plan {

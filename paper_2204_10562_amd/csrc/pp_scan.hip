@@ -5,6 +5,7 @@
 #define SC_WAVES 8                // of a workgroup, one behind the other in time
 #define SC_TILE (SC_CHUNK * SC_WAVES)
 #define SC_GROUP 16               // tiles between states that are passed on whole
+#define SC_EMPTIES 256            // most sequences that the only tile looks after itself
 #define SC_MAX_TILES (1 << 24)    // of a launch
 #define SC_MAX_SEQS (1 << 30)
 
@@ -51,6 +52,7 @@ struct sc_args {
     long long rows, cols, seqs;
     const int *starts;
     int tiles, lanes_tiles;         // in time, and over the channels
+    bool empties;                   // the tiles look after sequences without tokens too
     unsigned *ticket;
     unsigned long long *stretch;    // [tiles][width] what a tile makes of the state before it
     unsigned long long *whole;      // [tiles / SC_GROUP][width] the state before a group of tiles
@@ -314,6 +316,17 @@ template <int W> __device__ __forceinline__ unsigned sc_ticket(const sc_args &a,
     return __builtin_amdgcn_readfirstlane(room.ticket);
 }
 
+// Sequences without tokens end with what they begin with: by the waves of the only tile in time, where sequences are few.
+template <class L> __device__ __forceinline__ void sc_empties(const sc_args &a, const L &lanes, int wave, const float *from, float *to) {
+    if (!a.empties || !to) return;
+    for (long long n = wave; n < a.seqs; n += SC_WAVES) {
+        if (sc_start(a.starts, a.rows, n) < sc_start(a.starts, a.rows, n + 1)) continue;
+        float h[2];
+        lanes.get_floats(from ? from + n * a.cols : NULL, h);
+        lanes.put_floats(to + n * a.cols, h);
+    }
+}
+
 // a and 1 - a of a gate, both right to a few units of themselves
 __device__ __forceinline__ void sc_open(float gate, float &a, float &u) {
     const float e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(gate)), large = __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
@@ -383,6 +396,7 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_forward(sc_args a
     __syncthreads();
     sc_carry<W>(a, room, order, lanes_tile, wave, H);
     if (kept && t0 < a.rows) lanes.put_floats(kept + t0 / SC_CHUNK * a.cols, H);
+    sc_empties(a, lanes, wave, h0, h_last);
     typename Y::T *row = h + t0 * ld_h;
     if (plain) {
 #pragma unroll
@@ -491,6 +505,7 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_backward(sc_args 
     }
     __syncthreads();
     sc_carry<W>(a, room, order, lanes_tile, wave, C);
+    sc_empties(a, lanes, wave, dh_last, dh0);
     auto gradients = [&](int i, typename Y::T *to_gate, typename Y::T *to_v) {
         float df[W], dx[W];
 #pragma unroll
@@ -594,7 +609,8 @@ static int sc_run(int64_t rows, int64_t cols, int64_t seqs, const int32_t *start
     a.stretch = (unsigned long long *)((char *)workspace + 256);
     a.whole = a.stretch + tiles * a.width;
     const int64_t words = tiles > 1 ? (tiles + tiles / SC_GROUP + 1) * a.width : 0;
-    if (words || to) {
+    a.empties = tiles == 1 && starts && seqs <= SC_EMPTIES;
+    if (words || (to && !a.empties && (starts || !rows))) {
         int64_t groups = (words + 1023) / 1024;
         if (to && groups < seqs) groups = seqs;
         k_scan_begin<<<(unsigned)(groups < 4096 ? groups : 4096), 256, 0, st>>>(a, words, from, to);
