@@ -438,7 +438,7 @@ static ls_plan ds_segments(int type, int64_t cols) {
         const int64_t segs = (cols + (int64_t)held * LS_STEP - 1) / ((int64_t)held * LS_STEP);
         if (segs > DS_MEET) continue;
         p.held = (int)(((cols + segs - 1) / segs + LS_STEP - 1) / LS_STEP);
-        p.size = (long long)p.held * LS_STEP;
+        p.size = ls_even(cols, (int)segs);
         p.segs = (int)((cols + p.size - 1) / p.size);
         break;
     }

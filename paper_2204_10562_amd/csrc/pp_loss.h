@@ -22,6 +22,9 @@ struct ls_plan {
 // Most chunks that a thread holds: a 16-bit type's `most`, half of that in float
 static inline int ls_held(int type, int most) { return type == PP_TYPE_F32 ? most / 2 : most; }
 
+// The size of segments that are about equally long, at multiples of 128 bytes or more
+static inline long long ls_even(int64_t cols, int segs) { return ((cols + segs - 1) / segs + 63) & ~63ll; }
+
 // The largest segments, for their fewer partial results; smaller ones where those are as few, and to spread few rows over the chip.
 static inline ls_plan ls_divide(int type, int64_t rows, int64_t cols, int most) {
     const int sizes[3] = {ls_held(type, most), most > 8 ? 4 : ls_held(type, most) / 2, 1};
@@ -30,10 +33,11 @@ static inline ls_plan ls_divide(int type, int64_t rows, int64_t cols, int most) 
         p.held = sizes[i];
         p.size = (long long)sizes[i] * LS_STEP;
         p.segs = (int)((cols + p.size - 1) / p.size);
-        if (i == 2) return p;
-        const int64_t next = (cols + (int64_t)sizes[i + 1] * LS_STEP - 1) / ((int64_t)sizes[i + 1] * LS_STEP);
-        if (next > p.segs && (next > 64 || rows * p.segs >= LS_ENOUGH)) return p;
+        const int64_t next = i < 2 ? (cols + (int64_t)sizes[i + 1] * LS_STEP - 1) / ((int64_t)sizes[i + 1] * LS_STEP) : 0;
+        if (i == 2 || (next > p.segs && (next > 64 || rows * p.segs >= LS_ENOUGH))) break;
     }
+    p.size = ls_even(cols, p.segs);
+    return p;
 }
 
 // No more segments than this of any number of rows up to `rows` (those that are not the largest are less than LS_ENOUGH
