@@ -327,12 +327,12 @@ template <class L> __device__ __forceinline__ void sc_empties(const sc_args &a, 
     }
 }
 
-// a and 1 - a of a gate, both right to a few units of themselves
+// a = 1 / (1 + e) and 1 - a = e / (1 + e) of a gate, e = exp(-gate), both right to a few units of themselves.  Where e is infinite a
+// is 0, and 0 times it no number, for which the smaller of it and 1 is 1; a gate that is none leaves a none.
 __device__ __forceinline__ void sc_open(float gate, float &a, float &u) {
-    const float e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(gate)), large = __builtin_amdgcn_rcpf(1.0f + e), small = e * large;
-    const bool keeps = gate >= 0.0f;
-    a = keeps ? large : small;
-    u = keeps ? small : large;
+    const float e = __builtin_amdgcn_exp2f(-1.44269504f * gate);
+    a = __builtin_amdgcn_rcpf(1.0f + e);
+    u = __builtin_fminf(e * a, 1.0f);
 }
 // the same from s, the smaller one, negative where that is a
 __device__ __forceinline__ void sc_sides(float s, float &a, float &u) {
@@ -457,13 +457,11 @@ __global__ __launch_bounds__(SC_WAVES *PP_WAVE, 4) void k_scan_backward(sc_args 
 #pragma unroll
             for (int w = 0; w < W; ++w) {
                 const float value = lanes.get(x[i], w);
-                float ka, ku;
                 const float g = lanes.get(f[i], w), e = __builtin_amdgcn_exp2f(-1.44269504f * __builtin_fabsf(g)), large = __builtin_amdgcn_rcpf(1.0f + e);
                 const float small = e * large;
                 const bool keeps = g >= 0.0f;
                 s[i][w] = keeps ? small : -small;
-                ka = keeps ? large : small;
-                ku = keeps ? small : large;
+                const float ka = keeps ? large : small, ku = keeps ? small : large;
                 p[i][w] = state[w] - value;
                 state[w] = __builtin_fmaf(ka, state[w], ku * value);
             }
