@@ -153,7 +153,7 @@ int pp_norm_forward(int type, int64_t rows, int64_t cols, const void *x, int64_t
  *   s      the matrix `total` of `type`, or total_codes/total_scales; one of the two, the other NULL
  *   inv    float [rows], as pp_norm_forward gave it
  *   dgain  float [cols], or NULL = not wanted; dgain_in NULL = zero; may be dgain
- * The workspace (256-byte aligned; not needed where dgain is NULL and a row has at most 32768 columns) need not be kept.
+ * The workspace (256-byte aligned; not needed where dgain is NULL and a row has at most 16384 columns) need not be kept.
  * What so many rows need serves fewer.  With rows = 0, dgain = dgain_in.
  */
 size_t pp_norm_workspace_bytes(int type, int64_t rows, int64_t cols);

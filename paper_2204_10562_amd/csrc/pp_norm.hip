@@ -11,7 +11,8 @@
 #define NM_MAX_GRID (1 << 20)
 #define NM_CHUNKS 8          // most chunks of eight columns that a thread holds
 #define NM_PART_WAVES 4096   // most waves of a backward pass (16 to a unit); each workgroup has its own part of dg
-#define NM_WIDE (1024 * 4)   // most chunks of a row in the backward pass that holds it
+#define NM_WIDE 2048         // most chunks of a row in the backward pass that holds it (16384 columns)
+#define NM_WIDE_GROUPS 2048  // workgroups of one that does not
 
 // A row's values: a matrix of type Y, or what PP_PACK_INT8 left of one.
 template <class Y> struct nm_matrix {
@@ -157,11 +158,11 @@ extern "C" int pp_norm_forward(int type, int64_t rows, int64_t cols, const void 
         else if (chunks <= 128 && rows >= 1024) go(I(1), I(2));
         else if (chunks <= 256 && rows >= 1024) go(I(1), I(4));
         else if (chunks <= 256) go(I(4), I(1));
-        else if (chunks <= 512) go(I(4), I(2));
+        else if (chunks <= 512) go(I(8), I(1));
         else if (chunks <= 768) go(I(4), I(3));
-        else if (chunks <= 1024) go(I(4), I(4));
-        else if (chunks <= 1536) go(I(4), I(6));
-        else if (chunks <= 2048) go(I(4), I(8));
+        else if (chunks <= 1024) go(I(8), I(2));
+        else if (chunks <= 1536) go(I(8), I(3));
+        else if (chunks <= 2048) go(I(8), I(4));
         else if (chunks <= 4096) go(I(16), I(4));
         else go(I(16), I(0));
         return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
@@ -340,7 +341,9 @@ __global__ __launch_bounds__(256) void k_norm_gain(long long cols, int parts, co
 // Waves to a row of the backward pass that holds it, and workgroups that have parts of dg
 static int nm_waves(int64_t chunks) { return chunks <= 64 ? 1 : chunks <= 256 ? 4 : chunks <= 512 ? 8 : 16; }
 static int64_t nm_parts(int64_t rows, int64_t cols) {
-    const int64_t chunks = nm_chunks(cols), most = chunks > NM_WIDE ? 16 : NM_PART_WAVES / nm_waves(chunks);
+    const int64_t chunks = nm_chunks(cols), columns = (chunks + 255) / 256;  // (of workgroups beside each other, for rows that are not held)
+    const int64_t wide = columns >= NM_WIDE_GROUPS ? 1 : columns * 256 <= NM_WIDE_GROUPS ? 256 : NM_WIDE_GROUPS / columns;
+    const int64_t most = chunks > NM_WIDE ? wide : NM_PART_WAVES / nm_waves(chunks);
     return rows < most ? rows : most;
 }
 
@@ -384,8 +387,7 @@ extern "C" int pp_norm_backward(int type, int64_t rows, int64_t cols, const void
             else if (chunks <= 256) go(I(4), I(1));
             else if (chunks <= 512) go(I(8), I(1));
             else if (chunks <= 1024) go(I(16), I(1));
-            else if (chunks <= 2048) go(I(16), I(2));
-            else go(I(16), I(4));
+            else go(I(16), I(2));
             return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
         });
     if (rc != PP_OK || !dgain) return rc;
