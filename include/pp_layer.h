@@ -15,7 +15,8 @@
  *     `ld` values apart (ld >= cols; ld is not read where there is one row); its base has its
  *     type's alignment.  rows >= 0 (0: nothing is enqueued but what has to be written all the
  *     same), 1 <= cols <= PP_LAYER_MAX_COLS, rows <= PP_LAYER_MAX_ROWS.
- *   - Inputs and outputs must not overlap unless said otherwise.
+ *   - Inputs and outputs must not overlap unless said otherwise.  A workspace serves one call at a
+ *     time: calls that may run at once, on two streams or in two graphs, have one each.
  *   - Sums and the functions are computed in 32 bits and rounded once, to the nearest.
  *
  * Packed matrix of R rows and C columns: G = ceil(C / 128) groups to a row.

@@ -65,8 +65,9 @@ struct lp_room {
     lp_entry entry[LS_CAP + 32];
 };
 
-// The K-th largest of the 256 keys in room.max, by one wave: bits below `low` are the same for all.  0 if there are fewer.
-__device__ __forceinline__ void find_threshold(lp_room &room, int top, int low) {
+// The K-th largest of the 256 keys in room.max, by one wave.  0 if there are fewer.
+template <class Y> __device__ __forceinline__ void find_threshold(lp_room &room, int top) {
+    const int low = sizeof(typename Y::T) == 4 ? 0 : __is_same(Y, PpBF16) ? 16 : 13;  // (bits below are the same for all)
     if (threadIdx.x >= PP_WAVE) return;
     unsigned key[4], tau = 0;
 #pragma unroll
@@ -121,7 +122,7 @@ template <class F> __device__ __forceinline__ void narrow(lp_room &room, int top
 
 // A long list once more: where fewer threads than `top` had anything, all of it is there.  Of four entries to a thread the
 // maxima give a threshold as those of a segment do.
-__device__ __forceinline__ void shorten(lp_room &room, int top) {
+template <class Y> __device__ __forceinline__ void shorten(lp_room &room, int top) {
     const int t = threadIdx.x, found = (int)room.found;
     lp_entry mine[LS_CAP / LS_THREADS];
     unsigned most = 0;
@@ -132,7 +133,7 @@ __device__ __forceinline__ void shorten(lp_room &room, int top) {
     }
     room.max[t] = most;
     __syncthreads();
-    find_threshold(room, top, 0);
+    find_threshold<Y>(room, top);
     __syncthreads();
     const unsigned tau = room.tau > 1 ? room.tau : 1;
 #pragma unroll
@@ -142,8 +143,8 @@ __device__ __forceinline__ void shorten(lp_room &room, int top) {
 
 // The list's first `top` entries in order into put(rank, entry), and none behind them.  Four lanes to an entry, each with a
 // quarter of the others.
-template <class F> __device__ __forceinline__ void rank_list(lp_room &room, int top, F put) {
-    if (room.found > LS_THREADS) shorten(room, top);
+template <class Y, class F> __device__ __forceinline__ void rank_list(lp_room &room, int top, F put) {
+    if (room.found > LS_THREADS) shorten<Y>(room, top);
     const int t = threadIdx.x, found = (int)room.found, ends = (found + 31) & ~31;
     if (t < ends - found) room.entry[found + t] = 0;
     __syncthreads();
@@ -167,7 +168,7 @@ __device__ __forceinline__ void select_top(lp_room &room, const typename Y::T *x
     const int t = threadIdx.x;
     room.max[t] = ls_key(thread_max);
     __syncthreads();
-    find_threshold(room, top, sizeof(typename Y::T) == 4 ? 0 : __is_same(Y, PpBF16) ? 16 : 13);
+    find_threshold<Y>(room, top);
     __syncthreads();
     const unsigned low = 0x00800000u;  // the key of the lowest float
     const float tau = ls_value(room.tau > low ? room.tau : low);
@@ -201,7 +202,7 @@ __device__ __forceinline__ void select_top(lp_room &room, const typename Y::T *x
                     if (v[j] == v[j]) f(lp_make(ls_key(v[j]), first + c + j));
             }
         });
-    rank_list(room, top, put);
+    rank_list<Y>(room, top, put);
 }
 
 template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS, 4) void k_logprob(lp_args a, const typename Y::T *__restrict__ logits) {
@@ -286,7 +287,7 @@ template <class Y> __global__ __launch_bounds__(LS_THREADS) void k_logprob_join(
             }
             room.max[t] = most;
             __syncthreads();
-            find_threshold(room, a.top, 0);
+            find_threshold<Y>(room, a.top);
             __syncthreads();
             const unsigned tau = room.tau > 1 ? room.tau : 1;
             for (int c = t; c < n; c += LS_THREADS) {
@@ -298,7 +299,7 @@ template <class Y> __global__ __launch_bounds__(LS_THREADS) void k_logprob_join(
                 narrow(room, a.top, [&](auto f) {
                     for (int c = t; c < n; c += LS_THREADS) f(kept[c]);
                 });
-            rank_list(room, a.top, [&](int rank, lp_entry e) { put_top(a, row, rank, e, r); });
+            rank_list<Y>(room, a.top, [&](int rank, lp_entry e) { put_top(a, row, rank, e, r); });
         }
         __syncthreads();
     }

@@ -339,7 +339,7 @@ __global__ __launch_bounds__(256) void k_norm_gain(long long cols, int parts, co
 }
 
 // Waves to a row of the backward pass that holds it, and workgroups that have parts of dg
-static int nm_waves(int64_t chunks) { return chunks <= 64 ? 1 : chunks <= 256 ? 4 : chunks <= 512 ? 8 : 16; }
+static int nm_waves(int64_t chunks) { return chunks <= 64 ? 1 : chunks <= 128 ? 2 : chunks <= 256 ? 4 : chunks <= 512 ? 8 : 16; }
 static int64_t nm_parts(int64_t rows, int64_t cols) {
     const int64_t chunks = nm_chunks(cols), columns = (chunks + 255) / 256;  // (of workgroups beside each other, for rows that are not held)
     const int64_t wide = columns >= NM_WIDE_GROUPS ? 1 : columns * 256 <= NM_WIDE_GROUPS ? 256 : NM_WIDE_GROUPS / columns;
@@ -384,6 +384,7 @@ extern "C" int pp_norm_backward(int type, int64_t rows, int64_t cols, const void
                 if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
                 k_norm_wide<Y><<<dim3((unsigned)((chunks + 255) / 256), (unsigned)parts), 256, 0, st>>>(b, means, md, ms, mt, (T *)dx, ld_dx);
             } else if (chunks <= 64) go(I(1), I(1));
+            else if (chunks <= 128) go(I(2), I(1));
             else if (chunks <= 256) go(I(4), I(1));
             else if (chunks <= 512) go(I(8), I(1));
             else if (chunks <= 1024) go(I(16), I(1));

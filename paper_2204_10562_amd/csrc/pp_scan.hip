@@ -74,8 +74,10 @@ struct sc_marks {
     // the sequence of token t0 + i
     __device__ __forceinline__ int of(const int *starts, long long rows, int seqs, long long t0, int i) const {
         int n = base + __popcll(__ballot(next <= i));
-        if (more)
-            while (n < seqs && sc_start(starts, rows, n) <= t0 + i) ++n;
+        for (int some = more ? PP_WAVE : 0; some == PP_WAVE; n += some) {
+            const int at = n + (int)(threadIdx.x & (PP_WAVE - 1));
+            some = __popcll(__ballot(at < seqs && sc_start(starts, rows, at < seqs ? at : seqs) <= t0 + i));
+        }
         return n > 0 ? n - 1 : 0;
     }
 };
