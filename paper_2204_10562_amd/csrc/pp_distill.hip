@@ -100,8 +100,8 @@ struct ds_list {
     int none, empty;
 };
 
-// The entries of this lane
-#define DS_EACH(e) for (int e = threadIdx.x & (PP_WAVE - 1); e < PP_TOP_MAX; e += PP_WAVE)
+// The entries of this lane (all lanes have as many: an exponential in 64 bits is a hundred instructions, whoever needs it)
+#define DS_EACH(e) for (int e = threadIdx.x & (PP_WAVE - 1); e - (int)(threadIdx.x & (PP_WAVE - 1)) < a.top; e += PP_WAVE)
 
 // The teacher's side, and the listed logits, logit(entry, column).  Entries without a column or with a value of -infinity have no q (a column of
 // theirs is listed all the same).
@@ -128,7 +128,7 @@ template <class F> __device__ __forceinline__ void ds_teacher(const ds_args &a, 
     if (most == -inf) most = 0.0;
 #pragma unroll
     for (int i = 0; i < DS_PER; ++i) {
-        q[i] = exp(lq[i] - most);
+        q[i] = i * PP_WAVE < a.top ? exp(lq[i] - most) : 0.0;
         sum += q[i];
     }
     sum = pp_wave_sum(sum);
