@@ -6,8 +6,12 @@
 // p_rest is the sum over what is not listed and not 1 less what is: a student that is nearly sure of the listed entries keeps the
 // digits of the rest.  So the pass over a row leaves the listed entries out (a bit each in LDS), and they are added afterwards.
 //
-// Where rows are many and not too long, workgroups hold a row's segments until they know each other's sums, so that logits are read once.
-// Else three kernels: the sums of segments; a wave to a row for the list; the gradient.
+// From 128 MiB of logits on workgroups hold a row's segments until they know each other's sums, so that logits are read once; else (and for rows
+// of more than 524288 columns, 262144 in float32) three kernels: the sums of segments; a wave to a row for the list; the gradient.
+//
+// 2048 x 131072 bf16 with 64 entries (1.07 GB) 246 us, 4.4 TB/s where a copy reaches 5.1 to 5.2, and 13 for the lists, which are exponentials in 64 bits and
+// the way there and back; read twice 142 and 195 and the lists.  A workgroup to a whole row, in up to 16 waves' registers, took 369: nothing is read while
+// it computes.  777 x 50001 fp16 with 20 entries 29, 8 and 34 us: logits and gradient, 155 MB, mostly in the last cache.
 #include "pp_loss.h"
 
 #define DS_MEET 16   // most segments of a row whose workgroups meet
@@ -426,19 +430,18 @@ template <int HELD, class F> static void by_held(int held, F f) {
     else if constexpr (HELD > 1) by_held<HELD - 1>(held, f);
 }
 
-static unsigned grid_of(int64_t items) { return (unsigned)(items < LS_MAX_GRID ? items : LS_MAX_GRID); }
-
 // The segments of a row whose workgroups meet, about equally long; segs 0: rows are too long for it.  Few chunks to a
 // thread, so that more workgroups than four are there to work while one waits.  What the last cache holds (256 MB, logits and
 // gradient) is as well read twice: 777 x 50001 fp16 80 us in a meeting, 76 read twice, 4096 x 8000 bf16 87 and 63; but
 // 1500 x 50001 fp16 117 and 132, 1024 x 131072 bf16 151 and 173.
 static ls_plan ds_segments(int type, int64_t cols) {
     ls_plan p = {};
-    for (int held = type == PP_TYPE_F32 ? 4 : 8; held <= (type == PP_TYPE_F32 ? 8 : 16); held *= 2) {
+    const int most = ls_held(type, DS_HELD);
+    for (int held = most; held <= 2 * most; held += most) {
         const int64_t segs = (cols + (int64_t)held * LS_STEP - 1) / ((int64_t)held * LS_STEP);
         if (segs > DS_MEET) continue;
-        p.held = (int)(((cols + segs - 1) / segs + LS_STEP - 1) / LS_STEP);
         p.size = ls_even(cols, (int)segs);
+        p.held = held > most ? held : (int)((p.size + LS_STEP - 1) / LS_STEP);
         p.segs = (int)((cols + p.size - 1) / p.size);
         break;
     }
@@ -483,29 +486,22 @@ extern "C" int pp_distill_loss(int kind, int type, int64_t rows, int64_t cols, c
             const int64_t items = rows * meet.segs, groups = (items * 2 + 1023) / 1024;
             k_distill_clear<<<(unsigned)(groups < 1024 ? groups : 1024), 256, 0, st>>>(a.ticket, a.words, items * 2);
             if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
-            by_held<32 / sizeof(T)>(meet.held, [&](auto h) {
-                k_distill_meet<Y, decltype(h)::value><<<(unsigned)items, LS_THREADS, 0, st>>>(a, (const T *)logits, (T *)dlogits);
-            });
+            constexpr int MOST = sizeof(T) == 4 ? DS_HELD / 2 : DS_HELD;
+            auto go = [&](auto h) { k_distill_meet<Y, decltype(h)::value><<<(unsigned)items, LS_THREADS, 0, st>>>(a, (const T *)logits, (T *)dlogits); };
+            if (meet.held > MOST) go(std::integral_constant<int, 2 * MOST>());
+            else by_held<MOST>(meet.held, go);
             if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
             a.segs = 1;  // (the list finds the row's sums in one place)
-            k_distill_list<Y, true><<<grid_of(rows), PP_WAVE, 0, st>>>(a, (const T *)logits, (T *)dlogits);
+            k_distill_list<Y, true><<<ls_grid(rows), PP_WAVE, 0, st>>>(a, (const T *)logits, (T *)dlogits);
             return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
         }
-        auto by_plan = [&](auto f) {
-            constexpr int MOST = sizeof(T) == 4 ? DS_HELD / 2 : DS_HELD;
-            if (p.held == MOST) f(std::integral_constant<int, MOST>());
-            else if (p.held == MOST / 2) f(std::integral_constant<int, MOST / 2>());
-            else f(std::integral_constant<int, 1>());
-        };
-        by_plan([&](auto h) {
-            k_distill_sums<Y, decltype(h)::value><<<grid_of(rows * p.segs), LS_THREADS, 0, st>>>(a, (const T *)logits);
-        });
+        ls_by_held<Y, DS_HELD>(p.held, [&](auto h) { k_distill_sums<Y, decltype(h)::value><<<ls_grid(rows * p.segs), LS_THREADS, 0, st>>>(a, (const T *)logits); });
         if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
-        k_distill_list<Y, false><<<grid_of(rows), PP_WAVE, 0, st>>>(a, (const T *)logits, (T *)dlogits);
+        k_distill_list<Y, false><<<ls_grid(rows), PP_WAVE, 0, st>>>(a, (const T *)logits, (T *)dlogits);
         if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
         if (dlogits)
-            by_plan([&](auto h) {
-                k_distill_grad<Y, decltype(h)::value><<<grid_of(rows * p.segs), LS_THREADS, 0, st>>>(a, (const T *)logits, (T *)dlogits);
+            ls_by_held<Y, DS_HELD>(p.held, [&](auto h) {
+                k_distill_grad<Y, decltype(h)::value><<<ls_grid(rows * p.segs), LS_THREADS, 0, st>>>(a, (const T *)logits, (T *)dlogits);
             });
         return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
     });

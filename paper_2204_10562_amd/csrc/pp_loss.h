@@ -63,24 +63,19 @@ template <class Y> __device__ __forceinline__ PpRaw<Y> ls_load(const typename Y:
     return r;
 }
 
-// The chunks of x[0 .. n) that a thread of THREADS holds; all that are whole without a branch, so that their loads are on their way
+// A thread's chunks of a segment x[0 .. n), -infinity behind it; of a whole one without a branch, so that all loads are on their way
 // together
-template <class Y, int THREADS, int HELD> __device__ __forceinline__ void ls_load_row(PpRaw<Y> (&raw)[HELD], const typename Y::T *x, long long n) {
-    if (n >= (long long)HELD * THREADS * 8) {
+template <class Y, int HELD> __device__ __forceinline__ void ls_load_all(PpRaw<Y> (&raw)[HELD], const typename Y::T *x, long long n) {
+    const unsigned lane = threadIdx.x * (unsigned)(8 * sizeof(typename Y::T));
+    if (n >= (long long)HELD * LS_STEP) {
 #pragma unroll
         for (int i = 0; i < HELD; ++i)
 #pragma unroll
-            for (int j = 0; j < PpRaw<Y>::W; ++j) raw[i].w[j] = ((const pp_any16<sizeof(typename Y::T)> *)((const char *)(x + 8 * i * THREADS) + threadIdx.x * (unsigned)(8 * sizeof(typename Y::T))))[j].v;
+            for (int j = 0; j < PpRaw<Y>::W; ++j) raw[i].w[j] = ((const pp_any16<sizeof(typename Y::T)> *)((const char *)(x + i * LS_STEP) + lane))[j].v;
     } else {
 #pragma unroll
-        for (int i = 0; i < HELD; ++i) {
-            const int left = (int)n - 8 * ((int)threadIdx.x + i * THREADS);
-            raw[i] = ls_load<Y>((const typename Y::T *)((const char *)(x + 8 * i * THREADS) + threadIdx.x * (unsigned)(8 * sizeof(typename Y::T))), left);
-        }
+        for (int i = 0; i < HELD; ++i) raw[i] = ls_load<Y>((const typename Y::T *)((const char *)(x + i * LS_STEP) + lane), (int)n - 8 * (int)threadIdx.x - i * LS_STEP);
     }
-}
-template <class Y, int HELD> __device__ __forceinline__ void ls_load_all(PpRaw<Y> (&raw)[HELD], const typename Y::T *x, long long n) {
-    ls_load_row<Y, LS_THREADS, HELD>(raw, x, n);
 }
 
 // Makes the compiler convert held values again where they are used again: kept as floats they would take twice the registers.
@@ -101,6 +96,15 @@ __device__ __forceinline__ float ls_max3(float a, float b, float c) {
 __device__ __forceinline__ float ls_max8(const float *v) {
     return ls_max3(ls_max3(ls_max3(v[0], v[1], v[2]), v[3], v[4]), ls_max3(v[5], v[6], v[7]), v[7]);
 }
+
+// Calls f with the chunks that a thread holds in a division with this `most` as a constant.
+template <class Y, int MOST, class F> static inline void ls_by_held(int held, F f) {
+    constexpr int LARGE = sizeof(typename Y::T) == 4 ? MOST / 2 : MOST, MIDDLE = MOST > 8 ? 4 : LARGE / 2;
+    if (held == LARGE) f(std::integral_constant<int, LARGE>());
+    else if (held == MIDDLE) f(std::integral_constant<int, MIDDLE>());
+    else f(std::integral_constant<int, 1>());
+}
+static inline unsigned ls_grid(int64_t items) { return (unsigned)(items < LS_MAX_GRID ? items : LS_MAX_GRID); }
 
 // What a maximum is subtracted as: 0 where there is nothing but -infinity (then every term is 0)
 __device__ __forceinline__ float ls_base(float m) { return m == -__builtin_inff() ? 0.0f : m; }

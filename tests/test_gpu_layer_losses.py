@@ -341,10 +341,10 @@ def test_distill_rows_at_their_ends(t, cols):
         assert_within(np.nan_to_num(dx, nan=9.0), np.nan_to_num(wx, nan=9.0), 400 * U * (1 + np.abs(np.nan_to_num(wx))), t)
 
 
-@pytest.mark.parametrize("t, rows, cols, pad", [("bf16", 1101, 61007, 1), ("bf16", 257, 262144, 0), ("f16", 517, 131071, 0), ("f32", 300, 120001, 3), ("f32", 5000, 7001, 0), ("f32", 120, 300001, 0)])
+@pytest.mark.parametrize("t, rows, cols, pad", [("bf16", 1101, 61007, 1), ("bf16", 257, 262144, 0), ("f16", 517, 131071, 0), ("f32", 300, 120001, 3), ("f32", 5000, 7001, 0), ("f32", 120, 300001, 0), ("bf16", 170, 400001, 2)])
 @pytest.mark.parametrize("kind", ["top", "rest"])
 def test_distill_of_many(t, rows, cols, pad, kind):
-    """So many logits that they are read once, by workgroups that meet (the last ones have rows too long for it): some rows against the formula,
+    """So many logits that they are read once, by workgroups that meet (300001 float32 columns are too long for it): some rows against the formula,
     among them such as have nothing to learn or are no numbers, and all of them again in place."""
     import torch
     from paper_2204_10562_amd import layer as pp
