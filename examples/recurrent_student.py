@@ -4,7 +4,7 @@ A block norms the stream, makes gates and values of it with packed linear layers
 gated recurrence and adds the result to the stream.  The first stage of a pipeline would hold the embedding, the last one the
 head and the loss; what a block keeps of a microbatch until its backward pass is in 8 bits (and the states of every 16th token).
 
-    python examples/recurrent_student.py [--vocab 32768] [--width 1024] [--blocks 4] [--tokens 4096] [--sequences 8] [--top 20] [--steps 5]
+    python examples/recurrent_student.py [--vocab 32768] [--width 1024] [--blocks 4] [--tokens 4096] [--sequences 8] [--top 20] [--steps 5] [--rate 100]
 """
 import argparse
 import os
@@ -155,6 +155,7 @@ def main(argv=None):
     p.add_argument("--sequences", type=int, default=8)
     p.add_argument("--top", type=int, default=20)
     p.add_argument("--steps", type=int, default=5)
+    p.add_argument("--rate", type=float, default=100.0)
     p.add_argument("--type", choices=("bf16", "f32"), default="bf16")
     a = p.parse_args(argv)
     dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[a.type]
@@ -168,7 +169,7 @@ def main(argv=None):
         start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
         start.record()
         loss = student.distill(tokens, starts, index, logp, weight)
-        student.update(1.0)
+        student.update(a.rate)
         end.record()
         end.synchronize()
         print("step %d: divergence %.4f, %.2f ms" % (k, loss.sum().item(), start.elapsed_time(end)))
