@@ -323,19 +323,21 @@ __global__ __launch_bounds__(256) void k_norm_gain(long long cols, int parts, co
     __shared__ float room[32][33];
     const int t = threadIdx.x & 7, w = threadIdx.x >> 3;
     const long long c = blockIdx.x * 32ll + 4 * t;
+    // The last columns' four end with the last one, and some are added by two threads: one by one they took 60 us of 11953 x 394.  (Of fewer than
+    // four columns a part is read with what lies behind it in the workspace.)
+    const long long from = c + 4 <= cols || cols < 4 ? c : cols - 4;
     float sum[4] = {};
-    if (c + 4 <= cols) {
+    if (c < cols) {
 #pragma unroll 8
         for (int p = w; p < parts; p += 32) {
-            const pp_u4 v = ((const pp_any16<4> *)(part + p * cols + c))->v;
+            const pp_u4 v = ((const pp_any16<4> *)(part + p * cols + from))->v;
 #pragma unroll
             for (int k = 0; k < 4; ++k) sum[k] += pp_bits(v[k]);
         }
-    } else
-        for (int k = 0; c + k < cols; ++k)
-            for (int p = w; p < parts; p += 32) sum[k] += part[p * cols + c + k];
+    }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) room[w][4 * t + k] = sum[k];
+    for (int k = 0; k < 4; ++k)
+        if (from + k >= c) room[w][from + k - blockIdx.x * 32ll] = sum[k];
     __syncthreads();
     const long long col = blockIdx.x * 32ll + threadIdx.x;
     if (threadIdx.x >= 32 || col >= cols) return;
