@@ -225,11 +225,24 @@ __device__ __forceinline__ void sc_carry(const sc_args &a, sc_room<W> &room, int
         if (wave < 4 * W) {
             const int l = threadIdx.x >> 2, part = threadIdx.x & 3;
             const long long col = lanes_tile * (W * PP_WAVE) + l;
-            float x = room.x[2 * part][l], H = room.H[2 * part][l];
+            const float x0 = room.x[2 * part][l], H0 = room.H[2 * part][l];
+            float x = x0, H = H0;
             sc_join(x, H, room.x[2 * part + 1][l], room.H[2 * part + 1][l]);
-            sc_join_quad(x, H);
+            const float left_x = pp_moved<0xA0>(x), left_H = pp_moved<0xA0>(H);  // lanes 0 0 2 2
+            const float x1 = pp_moved<0xF5>(x), H1 = pp_moved<0xF5>(H);          // lanes 1 1 3 3
+            sc_join(x, H, x1, H1);
+            const float half_x = pp_moved<0x00>(x), half_H = pp_moved<0x00>(H), x2 = pp_moved<0xAA>(x), H2 = pp_moved<0xAA>(H);
+            sc_join(x, H, x2, H2);
             if (!part) sc_tell(a.stretch + order * a.width + col, sc_word(x, H));
-            // the tiles before it in its group; a word of zeros leaves a state as it is
+            // in the stretches' places: what the waves before each of them make of a state (zeros leave it as it is)
+            float ex = part > 1 ? half_x : 0.0f, eH = part > 1 ? half_H : 0.0f;
+            sc_join(ex, eH, part & 1 ? left_x : 0.0f, part & 1 ? left_H : 0.0f);
+            room.x[2 * part][l] = ex;
+            room.H[2 * part][l] = eH;
+            sc_join(ex, eH, x0, H0);
+            room.x[2 * part + 1][l] = ex;
+            room.H[2 * part + 1][l] = eH;
+            // the tiles before it in its group
             unsigned long long word[4];
             bool wait = true;
             while (wait) {
@@ -266,7 +279,8 @@ __device__ __forceinline__ void sc_carry(const sc_args &a, sc_room<W> &room, int
         }
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < W; ++w) h[w] = room.before[lane * W + w];
+        for (int w = 0; w < W; ++w) h[w] = sc_after(room.x[wave][lane * W + w], room.H[wave][lane * W + w], room.before[lane * W + w]);
+        return;
     }
 #pragma unroll
     for (int k = 0; k < SC_WAVES; ++k) {
