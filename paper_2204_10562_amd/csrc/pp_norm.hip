@@ -11,7 +11,8 @@
 // 8 bits as well 62 to 66 (338 MB, 5.3); backward 52 (268 MB, 5.2), from s in 8 bits 53 to 58 (236 MB, 4.2) of which 4.7 are the second
 // kernel, which adds the parts of dg.  Small ones are launches: one row of 4096 3.1 us.
 // Waves to a row, by eight chunks of columns: with more chunks to a thread and fewer waves less is on its way, 2048 x 16384 bf16 forward 77 us with
-// four waves and 57 with eight, 4096 x 8192 with copies 86 and 71; sixteen 59 and 74.
+// four waves and 57 with eight, 4096 x 8192 with copies 86 and 71; sixteen 59 and 74; 8192 x 6144 with four
+// 89, with twelve 79.  (Backward twelve instead of sixteen give nothing.)
 #include "pp_rows.h"
 
 #define NM_MAX_GRID (1 << 20)
@@ -166,7 +167,7 @@ extern "C" int pp_norm_forward(int type, int64_t rows, int64_t cols, const void 
         else if (chunks <= 256 && rows >= 1024) go(I(1), I(4));
         else if (chunks <= 256) go(I(4), I(1));
         else if (chunks <= 512) go(I(8), I(1));
-        else if (chunks <= 768) go(I(4), I(3));
+        else if (chunks <= 768) go(I(12), I(1));
         else if (chunks <= 1024) go(I(8), I(2));
         else if (chunks <= 1536) go(I(8), I(3));
         else if (chunks <= 2048) go(I(8), I(4));
