@@ -6,11 +6,12 @@
 // byte is read and written once, but for the states before every 16th token that the backward pass begins from (1/32 of the floats'
 // bytes each way), and 8 bytes a channel and tile between the tiles.
 //
-// What bounds it (a copy reaches 5.1 to 5.2 TB/s): 65536 x 1024 float32 forward 165 us, backward 256 (155 and 258 by bytes).  65536 x 2048 bf16 forward 237, backward
-// 318 (the same bytes): twice the exponentials and reciprocals to a byte, and the 16-bit values take twice their room as floats, so that two
-// workgroups fit on a unit where three do in float32; with all tiles beside each other (2048 x 65536) 193 and 286.  Few channels wait for the chain of
-// tiles: 65536 x 256 54 and 67 us, 1.7 us for 16 tiles.  5003 x 1000 fp16 in 23 sequences 21 and 29, about as long as one tile takes.
-// Sizes of 12 tokens to a wave 272 us forward (for 237), four waves 255, with 32 tokens to a wave 260 and 434 for 285 and 372 of an earlier state.
+// What bounds it (a copy reaches 5.1 to 5.2 TB/s): 65536 x 1024 float32 forward 161 us, backward 251 (155 and 258 by bytes).  65536 x 2048 bf16 forward 206,
+// backward 311 (the same bytes): twice the exponentials and reciprocals to a byte, and the 16-bit values take twice their room as floats, so that two
+// workgroups fit on a unit where three do in float32 (gates made again instead: three, and 224); with all tiles beside each other (2048 x 65536) 187 and 290.
+// Of a tile's 13 us there 6 are tickets, loads and its stretch, 5 the wait for the state, 2 the rest.  Few channels wait for the chain of
+// tiles: 65536 x 256 47 and 62 us, 1.5 us for 16 tiles.  5003 x 1000 fp16 in 23 sequences 20 and 29, less than two tiles one behind the other.
+// Before the waits were shortened, sizes of 12 tokens to a wave took 272 us forward (for 237), four waves 255, 32 tokens to a wave 260 and 434 for 285 and 372.
 #include "pp_rows.h"
 
 #define SC_CHUNK 16               // tokens that a wave holds, and between kept states
