@@ -311,12 +311,13 @@ template <class L> __device__ __forceinline__ void sc_empties(const sc_args &a, 
     }
 }
 
-// a = 1 / (1 + e) and 1 - a = e / (1 + e) of a gate, e = exp(-gate), both right to a few units of themselves.  Where e is infinite a
-// is 0, and 0 times it no number, for which the smaller of it and 1 is 1; a gate that is none leaves a none.
+// a = 1 / (1 + e) and 1 - a = e / (1 + e) of a gate, e = exp(-gate).  The exponent is a product that was rounded, so the smaller of the two is right to
+// (8 + 2 |gate|) 2^-24 of itself, and exp2 and the reciprocal give 0 for what is no normal number: a is 0 from a gate of -87.34 on, where e times it is
+// nothing, and 1 - a is 1 from far before.  A gate that is none leaves both none.
 __device__ __forceinline__ void sc_open(float gate, float &a, float &u) {
     const float e = __builtin_amdgcn_exp2f(-1.44269504f * gate);
     a = __builtin_amdgcn_rcpf(1.0f + e);
-    u = __builtin_fminf(e * a, 1.0f);
+    u = e > 0x1p125f ? 1.0f : e * a;
 }
 // the same from s, the smaller one, negative where that is a
 __device__ __forceinline__ void sc_sides(float s, float &a, float &u) {
