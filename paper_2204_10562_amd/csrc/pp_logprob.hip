@@ -325,7 +325,7 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_log
         const float m = a.norm[2 * row], s = a.norm[2 * row + 1];
         const long long tok = a.tokens ? a.tokens[row] : -1;
         float g = a.dlogp && tok >= 0 ? a.dlogp[row] * a.inv_t : 0.0f;
-        if (tok >= a.cols) g = __builtin_nanf("");
+        if (a.dlogp && tok >= a.cols) g = __builtin_nanf("");
         const float dh = a.dentropy ? a.dentropy[row] * a.inv_t : 0.0f, h = a.dentropy ? a.entropy[row] : 0.0f;
         // p (-g - dh (ln p + H)), with ln p = ln 2 (d - log2 s)
         const float scale = s == 0.0f ? 0.0f : 1.0f / s, log2_s = __builtin_amdgcn_logf(s);
