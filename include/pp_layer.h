@@ -231,7 +231,8 @@ int pp_logprob_forward(int type, int64_t rows, int64_t cols, const void *logits,
  * The gradient of logp and entropy (dlogp, dentropy float [rows]; NULL = zero; entropy is needed with dentropy alone):
  *   dlogits_j = (dlogp ([j = token] - p_j) - dentropy p_j (ln p_j + entropy)) / temperature
  * dlogits of `type`, may be logits (same base and ld).  Rows without a token take no dlogp, and one of a token >= cols is NaN where
- * dlogp is given; rows of nothing but -infinity have gradient 0.
+ * dlogp is given; rows of nothing but -infinity have gradient 0.  A row with neither a token's dlogp nor a dentropy (NULL or 0) has
+ * gradient 0 whatever it holds.
  */
 int pp_logprob_backward(int type, int64_t rows, int64_t cols, const void *logits, int64_t ld_logits, float temperature,
                         const int32_t *tokens, const float *norm, const float *dlogp, const float *entropy, const float *dentropy,

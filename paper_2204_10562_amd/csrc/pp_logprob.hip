@@ -327,6 +327,8 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_log
         float g = a.dlogp && tok >= 0 ? a.dlogp[row] * a.inv_t : 0.0f;
         if (a.dlogp && tok >= a.cols) g = __builtin_nanf("");
         const float dh = a.dentropy ? a.dentropy[row] * a.inv_t : 0.0f, h = a.dentropy ? a.entropy[row] : 0.0f;
+        // (of padding nothing is asked, and what it holds may be no numbers)
+        const bool asked = (a.dlogp && tok >= 0) || dh != 0.0f;
         // p (-g - dh (ln p + H)), with ln p = ln 2 (d - log2 s)
         const float scale = s == 0.0f ? 0.0f : 1.0f / s, log2_s = __builtin_amdgcn_logf(s);
         const float slope = -dh * 0.69314718f * scale, level = s == 0.0f ? 0.0f : (-g - dh * (h - 0.69314718f * log2_s)) * scale;
@@ -335,13 +337,15 @@ template <class Y, int HELD> __global__ __launch_bounds__(LS_THREADS) void k_log
         for (int i = 0; i < HELD; ++i) {
             const long long c = first + 8ll * (threadIdx.x + i * LS_THREADS), left = end - c;
             if (left <= 0) break;
-            float v[8];
-            pp_values<Y>(ls_load<Y>(logits + row * a.ld + c, left), v);
+            float v[8] = {};
+            if (asked) {
+                pp_values<Y>(ls_load<Y>(logits + row * a.ld + c, left), v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float d = (v[j] - m) * a.k, e = __builtin_amdgcn_exp2f(d);
-                v[j] = e * __builtin_fmaf(__builtin_fmaxf(d, -256.0f), slope, level);
-                if (c + j == tok && s != 0.0f) v[j] += g;
+                for (int j = 0; j < 8; ++j) {
+                    const float d = (v[j] - m) * a.k, e = __builtin_amdgcn_exp2f(d);
+                    v[j] = e * __builtin_fmaf(__builtin_fmaxf(d, -256.0f), slope, level);
+                    if (c + j == tok && s != 0.0f) v[j] += g;
+                }
             }
             pp_store8<Y>(dlogits + row * a.ld_d + c, left, v);
         }
