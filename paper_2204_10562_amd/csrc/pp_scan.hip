@@ -19,7 +19,8 @@
 #define SC_TILE (SC_CHUNK * SC_WAVES)
 #define SC_GROUP 16               // tiles between states that are passed on whole
 #define SC_EMPTIES 256            // most sequences that the only tile looks after itself
-#define SC_MAX_TILES (1 << 24)    // of a launch
+#define SC_MAX_TILES (1 << 24)    // of a call
+#define SC_MAX_GRID ((1ll << 32) / (SC_WAVES * 64) - 1)  // workgroups of a launch, which has fewer than 2^32 threads
 #define SC_MAX_SEQS (1 << 30)
 
 // A stretch of tokens as what it makes of the state before it, h -> A h + H.  x says A: 1 - A where that is below 1/2 (so that a
@@ -606,11 +607,16 @@ static int sc_run(int64_t rows, int64_t cols, int64_t seqs, const int32_t *start
         if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
     }
     if (!rows) return PP_OK;
-    const unsigned grid = (unsigned)(tiles * lanes);
-    if (pairs) {
-        if constexpr (sizeof(typename Y::T) == 2) launch(a, grid, std::integral_constant<int, 2>());
-    } else launch(a, grid, std::integral_constant<int, 1>());
-    return hipGetLastError() == hipSuccess ? PP_OK : PP_ERR_HIP;
+    // More tiles than a launch has workgroups take another launch, whose tickets go on where the first one's ended.  (Those are many tiles in
+    // time, which go by tickets: one tile in time has 2^16 workgroups at most.)
+    for (int64_t left = tiles * lanes; left > 0; left -= SC_MAX_GRID) {
+        const unsigned grid = (unsigned)(left < SC_MAX_GRID ? left : SC_MAX_GRID);
+        if (pairs) {
+            if constexpr (sizeof(typename Y::T) == 2) launch(a, grid, std::integral_constant<int, 2>());
+        } else launch(a, grid, std::integral_constant<int, 1>());
+        if (hipGetLastError() != hipSuccess) return PP_ERR_HIP;
+    }
+    return PP_OK;
 }
 
 extern "C" int pp_scan_forward(int type, int64_t rows, int64_t cols, const void *gate, int64_t ld_gate, const void *v, int64_t ld_v, int64_t seqs,
