@@ -447,8 +447,9 @@ static ls_plan ds_segments(int type, int64_t cols) {
     }
     return p;
 }
+// (A launch has fewer than 2^32 threads: of 2^24 workgroups and more, rows are read twice, in loops.)
 static bool ds_meets(int type, int64_t rows, int64_t cols, const ls_plan &p) {
-    return p.segs && rows * cols * pp_type_size(type) >= DS_MEET_FROM && rows * p.segs <= 1 << 24;
+    return p.segs && rows * cols * pp_type_size(type) >= DS_MEET_FROM && rows * p.segs < 1 << 24;
 }
 
 extern "C" size_t pp_distill_workspace_bytes(int type, int64_t rows, int64_t cols, int top) {

@@ -1,0 +1,60 @@
+"""Distillation of more rows than a launch has workgroups, of few columns (marker gpu): every loop over rows takes a second turn.
+
+Bounds, with u = 2^-24 and |d| <= 16 the distance of a logit from its row's largest: a sum of exponentials is right to (180 + 2.5 mean |d|) u,
+at most 220 u, and so are ln p and ln p_rest.
+"""
+import pytest
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+STEP = 1 << 20
+
+
+def logits(rows, cols, seed):
+    """Float32 logits of 16ths, so that some of a row are equal; some masked."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = (torch.randn(rows, cols, generator=g, device="cuda").clamp_(-4, 4) * 32).round_() / 16
+    x[3::8, cols - 1] = -float("inf")
+    return g, x
+
+
+def room(nbytes):
+    import torch
+    return torch.full((nbytes,), 255, dtype=torch.uint8, device="cuda")
+
+
+def within(got, want, bound):
+    return bool(((got.double() - want).abs() <= bound + U * want.abs()).all())
+
+
+@pytest.mark.parametrize("kind", ["top", "rest"])
+def test_distillation(kind):
+    """2^24 rows of 268 MB: as many workgroups that meet would be more than a launch has."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    rows, cols, top = 1 << 24, 4, 2
+    print("[case] distill", kind, rows, flush=True)
+    g, x = logits(rows, cols, 2)
+    index = torch.randint(0, cols // 2, (rows, 1), generator=g, device="cuda", dtype=torch.int32) + torch.tensor([[0, 1]], dtype=torch.int32, device="cuda")
+    value = torch.log(torch.rand(rows, top, generator=g, device="cuda") * 0.4 + 0.05)
+    weight = torch.rand(rows, generator=g, device="cuda")
+    weight[5::16] = 0
+    loss, dx = torch.empty(rows, device="cuda"), torch.empty_like(x)
+    pp.pp_distill_loss({"top": 0, "rest": 1}[kind], x, 1.0, index, value, weight, loss, dx, room(pp.pp_distill_workspace_bytes(x.dtype, rows, cols, top)))
+    for at in range(0, rows, STEP):
+        part = slice(at, at + STEP)
+        lp, w, i, lq = torch.log_softmax(x[part].double(), 1), weight[part].double(), index[part].long(), value[part].double()
+        if kind == "top":
+            lq = torch.log_softmax(lq, 1)
+        q, dz = lq.exp(), lp.exp()
+        want = (q * (lq - lp.gather(1, i))).sum(1)
+        if kind == "rest":
+            rest, beside = 1 - q.sum(1), torch.ones_like(dz).scatter_(1, i, 0.0)
+            mass = (dz * beside).sum(1)
+            want += rest * (rest.log() - mass.log())
+            dz = dz - dz * beside * (rest / mass)[:, None]
+        dz.scatter_add_(1, i, -q)
+        fine = torch.isfinite(want) | (w == 0)
+        assert within(loss[part][fine], torch.where(w > 0, want * w, 0.0)[fine], 440 * U) and torch.equal(loss[part][~fine], want[~fine].float()), at
+        assert within(dx[part], torch.where(w[:, None] > 0, dz * w[:, None], 0.0), 660 * U), at
