@@ -1,7 +1,10 @@
-"""Distillation of more rows than a launch has workgroups, of few columns (marker gpu): every loop over rows takes a second turn.
+"""Losses of more rows than a launch has workgroups, of few columns (marker gpu): every loop over rows takes a second turn.
 
 Bounds, with u = 2^-24 and |d| <= 16 the distance of a logit from its row's largest: a sum of exponentials is right to (180 + 2.5 mean |d|) u,
-at most 220 u, and so are ln p and ln p_rest.
+at most 220 u, and so is ln p, with 4 u of itself and of d: 400 u.  The mean |d| of a row of six is at most its entropy, 1.8, and the mean d^2 at
+most 6 max(p ln^2 p) = 3.3: the entropy is right to (180 + 4.5 + 190 * 1.8 + 5 * 3.3 + 4 * 1.8) u < 600 u.  A gradient, for |dlogp| and
+|dentropy| of 1: p (203 + 2.5 d) u + 8 u < 215 u for the first; for the second p (|ln p| + H) <= 2.2 times 203 u, 2.5 p d (|ln p| + H) <= 3 u, p times the
+entropy's own 600 u and p's 200 u, and 10 u: 1260 u.  A distillation's loss has ln p and ln p_rest each off by 220 u and its gradient p and p_rest.
 """
 import pytest
 
@@ -26,6 +29,34 @@ def room(nbytes):
 
 def within(got, want, bound):
     return bool(((got.double() - want).abs() <= bound + U * want.abs()).all())
+
+
+def test_log_probabilities():
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    rows, cols, top = (1 << 22) + 5, 6, 3
+    print("[case] logprob", rows, flush=True)
+    g, x = logits(rows, cols, 1)
+    tokens = torch.randint(-1, cols - 1, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    dlogp, dentropy = (torch.rand(rows, generator=g, device="cuda") * 2 - 1 for _ in range(2))
+    logp, entropy, norm, dx = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, 2, device="cuda"), torch.empty_like(x)
+    index, value = torch.empty(rows, top, dtype=torch.int32, device="cuda"), torch.empty(rows, top, device="cuda")
+    pp.pp_logprob_forward(x, 1.0, tokens, logp, entropy, norm, index, value, room(pp.pp_logprob_workspace_bytes(x.dtype, rows, cols, top)))
+    pp.pp_logprob_backward(x, 1.0, tokens, norm, dlogp, entropy, dentropy, dx)
+    for at in range(0, rows, STEP):
+        part = slice(at, at + STEP)
+        lp = torch.log_softmax(x[part].double(), 1)
+        p = lp.exp()
+        plp = torch.where(p > 0, p * lp, 0.0)
+        h = -plp.sum(1)
+        tok, have = tokens[part].long().clamp(min=0)[:, None], tokens[part] >= 0
+        assert within(logp[part], torch.where(have, lp.gather(1, tok)[:, 0], 0.0), 400 * U) and within(entropy[part], h, 600 * U), at
+        order = torch.sort(x[part], dim=1, descending=True, stable=True).indices[:, :top]
+        assert torch.equal(index[part].long(), order) and within(value[part], lp.gather(1, order), 400 * U), at
+        dl, dh = (dlogp[part].double() * have)[:, None], dentropy[part].double()[:, None]
+        want = -p * dl - dh * (plp + p * h[:, None])
+        want.scatter_add_(1, tok, dl)
+        assert within(dx[part], want, (215 + 1260) * U), at
 
 
 @pytest.mark.parametrize("kind", ["top", "rest"])

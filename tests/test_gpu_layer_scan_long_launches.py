@@ -44,3 +44,19 @@ def test_as_many_rows_as_there_may_be():
     assert near(last[0], h[-1].float(), HALF * h[-1].float().abs()) and near(dh0[0], dv[0].float(), HALF * dv[0].float().abs())
     del gate, v, dh, h, dgate, dv, kept, ws
     torch.cuda.empty_cache()
+
+
+def test_more_single_tokens_than_threads():
+    """With a gate of 0 h is (state + v) / 2, rounded once; slots from the last to the first."""
+    import torch
+    from paper_2204_10562_amd import layer as pp
+    rows = (1 << 28) + 5
+    print("[case] step", rows, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    gate, v, state = torch.zeros(rows, 1, device="cuda"), torch.randn(rows, 1, generator=g, device="cuda"), torch.randn(rows, 1, generator=g, device="cuda")
+    slots, h = torch.arange(rows - 1, -1, -1, dtype=torch.int32, device="cuda"), torch.empty_like(v)
+    want = (state.flip(0) + v) / 2
+    pp.pp_scan_step(gate, v, slots, state, h)
+    assert torch.equal(h, want) and torch.equal(state.flip(0), want)
+    del gate, v, state, slots, h, want
+    torch.cuda.empty_cache()
