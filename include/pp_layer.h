@@ -253,7 +253,9 @@ int pp_logprob_backward(int type, int64_t rows, int64_t cols, const void *logits
  *   loss      float [rows] out
  *   dlogits   [rows][cols] of `type` out, or NULL = not wanted; may be logits (same base and ld)
  * In a row of nothing but -infinity the loss is infinite (0 if the list has no q) and the gradient 0; one that holds a NaN or
- * +infinity gives NaN.  The workspace (256-byte aligned) need not be kept; what so many rows, or a longer list, needs serves fewer.
+ * +infinity gives NaN.  Calls with a gradient that have 128 MiB of logits or more go another way through them: the gradient beside the list is
+ * rounded otherwise, and p_rest - r is a difference in 32 bits.  The workspace (256-byte aligned) need not be kept; what so many rows, or a longer
+ * list, needs serves fewer.
  */
 #define PP_DISTILL_TOP 0
 #define PP_DISTILL_REST 1

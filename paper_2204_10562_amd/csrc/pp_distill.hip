@@ -9,9 +9,9 @@
 // From 128 MiB of logits on workgroups hold a row's segments until they know each other's sums, so that logits are read once; else (and for rows
 // of more than 524288 columns, 262144 in float32) three kernels: the sums of segments; a wave to a row for the list; the gradient.
 //
-// 2048 x 131072 bf16 with 64 entries (1.07 GB) 246 us, 4.4 TB/s where a copy reaches 5.1 to 5.2, and 13 for the lists, which are exponentials in 64 bits and
+// 2048 x 131072 bf16 with 64 entries: the loss alone 110 us (537 MB, 4.9 TB/s), with the gradient (1.07 GB) 246 us, 4.4 TB/s where a copy reaches 5.1 to 5.2, and 13 for the lists, which are exponentials in 64 bits and
 // the way there and back; read twice 142 and 195 and the lists.  A workgroup to a whole row, in up to 16 waves' registers, took 369: nothing is read while
-// it computes.  777 x 50001 fp16 with 20 entries 29, 8 and 34 us: logits and gradient, 155 MB, mostly in the last cache.
+// it computes.  777 x 50001 fp16 with 20 entries 28, 8 and 34 us: logits and gradient, 155 MB, mostly in the last cache.
 #include "pp_loss.h"
 
 #define DS_MEET 16   // most segments of a row whose workgroups meet
@@ -261,7 +261,8 @@ __device__ __forceinline__ unsigned long long ds_word(float m, float s) {
 
 // From logits to the gradient beside the list in one reading: a workgroup holds a segment until the sums of all of the row's are known.
 // The sums of what is listed and of what is not are made apart, so p_rest keeps its digits; of the teacher only r is needed, and
-// whether there is one.
+// whether there is one.  (p_rest - r is a
+// difference in 32 bits here, and one in 64 in k_distill_list.)
 //
 // The workgroups of a row wait for one another, each after it has told its own sums.  Tickets are drawn at the start of a workgroup, so
 // all below the highest one run or have ended, and only the row of the highest ticket, of at most DS_MEET workgroups, can wait for one

@@ -9,7 +9,9 @@
 //
 // Bytes bound both passes.  8192 x 4096 bf16, where a copy of 1 GiB reaches 5.1 to 5.2 TB/s: forward 50 us (268 MB, 5.3 TB/s), with s and y in
 // 8 bits as well 62 to 66 (338 MB, 5.3); backward 52 (268 MB, 5.2), from s in 8 bits 53 to 58 (236 MB, 4.2) of which 4.7 are the second
-// kernel, which adds the parts of dg.  Small ones are launches: one row of 4096 3.1 us.
+// kernel, which adds the parts of dg.  Small ones are launches: one row of 4096 3.1 us.  Rows below 512 columns have a wave each all the same, and leave
+// most of its lanes idle: 262144 x 128 bf16 139 and 152 us (52 by bytes), x 64 113 and 143 (26).  The backward pass of float32 rows of 8193 to 16384
+// columns from 8 bits wants 7 registers more than there are.
 // Waves to a row, by eight chunks of columns: with more chunks to a thread and fewer waves less is on its way, 2048 x 16384 bf16 forward 77 us with
 // four waves and 57 with eight, 4096 x 8192 with copies 86 and 71; sixteen 59 and 74; 8192 x 6144 with four
 // 89, with twelve 79.  (Backward twelve instead of sixteen give nothing.)

@@ -3,14 +3,17 @@
 // One pass over the tokens: a workgroup's eight waves hold 16 tokens each, one behind the other, of 64 lanes' channels (two 16-bit ones to a
 // lane).  A wave makes of its tokens what they do to any state, (A, H); the workgroup joins and publishes that, looks at what the tiles
 // before it have published, and then every wave goes over its tokens again, from registers, with the state that they find.  Every
-// byte is read and written once, but for the states before every 16th token that the backward pass begins from (1/32 of the floats'
-// bytes each way), and 8 bytes a channel and tile between the tiles.
+// byte is read and written once, but for the states before every 16th token that the backward pass begins from (1/16 of one float matrix, an eighth
+// of a 16-bit one, written by the forward pass and read by the backward pass), 8 bytes a channel and tile between the tiles, and in 16 bits what
+// the backward pass puts away: it has 128 registers and wants 6 more in bf16, 10 in fp16 (34 MB written beside 537, 65536 x 2048).
 //
-// What bounds it (a copy reaches 5.1 to 5.2 TB/s): 65536 x 1024 float32 forward 161 us, backward 251 (155 and 258 by bytes).  65536 x 2048 bf16 forward 206,
-// backward 311 (the same bytes): twice the exponentials and reciprocals to a byte, and the 16-bit values take twice their room as floats, so that two
-// workgroups fit on a unit where three do in float32 (gates made again instead: three, and 224); with all tiles beside each other (2048 x 65536) 187 and 290.
+// What bounds it (a copy reaches 5.1 to 5.2 TB/s): 65536 x 1024 float32 forward 160 us, backward 253 (155 and 258 by bytes).  65536 x 2048 bf16 forward 206
+// to 211, backward 302 to 311 (the same bytes): twice the exponentials and reciprocals to a byte, and the 16-bit values take twice their room as floats,
+// so that two workgroups fit on a unit where three do in float32 (gates made again instead: three, and 224 for 206); with all tiles beside each other
+// (2048 x 65536) 185 to 189 and 292.  Vector instructions take 68 and 73 % of the units' time.
 // Of a tile's 13 us there 6 are tickets, loads and its stretch, 5 the wait for the state, 2 the rest.  Few channels wait for the chain of
-// tiles: 65536 x 256 47 and 62 us, 1.5 us for 16 tiles.  5003 x 1000 fp16 in 23 sequences 20 and 29, less than two tiles one behind the other.
+// tiles: 65536 x 256 48 and 63 us, 1.5 us for 16 tiles; 2^30 x 1 395 and 376 ms, of 2^23 tiles.  5003 x 1000 fp16 in 23 sequences 20 and 30,
+// less than two tiles one behind the other.
 // Before the waits were shortened, sizes of 12 tokens to a wave took 272 us forward (for 237), four waves 255, 32 tokens to a wave 260 and 434 for 285 and 372.
 #include "pp_rows.h"
 
