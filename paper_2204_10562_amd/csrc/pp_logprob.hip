@@ -13,7 +13,7 @@
 // Alternatives: each thread knows its chunks' maxima.  The K-th largest of the 256 threads' maxima, found bit by bit by one wave,
 // is at most the K-th largest logit, and the logits from there on lie in the chunks of at most K threads (or tie with them): they
 // are read again, ranked by counting and written in order.  Where ties make them too many, the K-th largest pair of logit and
-// column is found bit by bit by all threads, each of whom reads his part of the segment 64 times more: 2048 x 131072 bf16 with 64 takes 7.8 ms in place
+// column is found bit by bit by all threads, in 64 more readings of the segment: 2048 x 131072 bf16 with 64 takes 7.8 ms in place
 // of 0.14 to 0.16 where half of every row is a mask of the lowest value, or all of it is one value (with a mask of -infinity 0.14); one row of them
 // 71 us for 12.  Segments' lists are joined in the same way.
 #include "pp_loss.h"
